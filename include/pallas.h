@@ -17,6 +17,11 @@
  *   pallas_pack_suffix_blocks  gather suffix pages into transfer chunks
  *   pallas_assemble_kv         scatter chunks into the target block table
  *   pallas_decode_step         one decode step over an assembled cache
+ *   pallas_rope_*              rotary positions of Q and K rows
+ *   pallas_quant_store, _load  an 8-bit cache: rows quantised as they are
+ *                              written, and read back
+ *   pallas_attend_*            attention of one new token per sequence over a
+ *                              paged cache, bf16 or 8-bit
  *   pallas_check_coverage      host-only [0, n) coverage check
  *   pallas_window_*, pallas_ewma_update, pallas_admit, pallas_waste_bound
  *                              host-only Scheduler Engine (when to migrate)
@@ -75,6 +80,8 @@ typedef enum {
                                   that position was skipped */
 #define PALLAS_DEVERR_TOKEN 2u /* a token id outside [0, vocab) (prefill and
                                   decode); token 0's embedding row was used */
+#define PALLAS_DEVERR_LENGTH 4u /* a length outside [0, max_length] (attend): cut
+                                   to it */
 
 /* Decoder shape (Qwen3/Llama-style pre-norm decoder, Section 6.1 models). */
 typedef struct {
@@ -320,6 +327,174 @@ int pallas_decode_step_static(pallas_model* m, int32_t num_seqs, const int32_t* 
                               int32_t max_pages, const pallas_kv_pool* pool, float* d_logits,
                               int32_t* d_err, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Operators on the cache, for callers that run a decoder's layers themselves
+ * (another architecture, a long-context rotary, an 8-bit cache).  A new token
+ * of each sequence takes pallas_rope_apply on its Q and K heads, the store
+ * (pallas_quant_store, or the caller's own into a bf16 pool) and
+ * pallas_attend_*; a prompt's rows take the first two.  Per-row arguments
+ * (positions, sequence indices, lengths) live in device memory, so a captured
+ * graph can be replayed as they grow.  Their launches are timed with the
+ * classes PALLAS_K_QKV_EPI (rope, store), PALLAS_K_PACK (load) and
+ * PALLAS_K_DECODE_ATTN (attend).
+ * ------------------------------------------------------------------------ */
+
+/* Rotary positions.  Pair i < r / 2 of a head's first r = rotary_dim elements
+ * turns by p f_i radians at position p:
+ *   y0 = m (x0 cos - x1 sin),  y1 = m (x1 cos + x0 sin),  f_i = theta^(-2i/r),
+ * (x0, x1) = elements (i, i + r/2) in the half layout, (2i, 2i + 1) in the
+ * interleaved one; elements from r on are copied.  For contexts `factor` (s >= 1)
+ * times as long as the `trained_len` (L) positions a model was trained on, f_i
+ * becomes
+ *   LINEAR  f_i / s
+ *   NTK     (theta s^(r / (r - 2)))^(-2i/r)                     (r > 2, else f_i)
+ *   YARN    (1 - w) f_i + w f_i / s,  w = clamp((i - a) / max(b - a, 0.001), 0, 1),
+ *           a = max(floor(c(fast)), 0), b = min(ceil(c(slow)), r - 1), where
+ *           c(t) = r ln(L / (2 pi t)) / (2 ln theta) is the pair that makes t
+ *           turns over L; and m = 0.1 ln s + 1
+ *   BANDS   w f_i + (1 - w) f_i / s,
+ *           w = clamp((L f_i / (2 pi) - slow) / (fast - slow), 0, 1)
+ * m is 1 otherwise, and `magnitude` where that is not 0. */
+typedef enum { PALLAS_ROPE_HALF = 0, PALLAS_ROPE_INTERLEAVED = 1 } pallas_rope_layout;
+typedef enum {
+  PALLAS_ROPE_UNSCALED = 0,
+  PALLAS_ROPE_LINEAR = 1,
+  PALLAS_ROPE_NTK = 2,
+  PALLAS_ROPE_YARN = 3,
+  PALLAS_ROPE_BANDS = 4
+} pallas_rope_scaling;
+#define PALLAS_ROPE_MAX_DIM 256
+
+typedef struct {
+  int32_t rotary_dim;  /* r: even, 2 .. PALLAS_ROPE_MAX_DIM */
+  int32_t layout;      /* pallas_rope_layout */
+  int32_t scaling;     /* pallas_rope_scaling */
+  int32_t trained_len; /* L >= 1 (YARN, BANDS) */
+  double theta;        /* > 1 */
+  double factor;       /* s >= 1 (all but UNSCALED) */
+  double fast, slow;   /* turns over L, fast > slow > 0 (YARN, BANDS) */
+  double magnitude;    /* m > 0, or 0: as above */
+} pallas_rope_config;
+
+/* Filled by pallas_rope_init, owned by the caller, read during a call. */
+typedef struct {
+  int32_t rotary_dim;
+  int32_t layout;
+  float magnitude;
+  int32_t reserved;
+  uint64_t turns[PALLAS_ROPE_MAX_DIM / 2]; /* f_i / (2 pi) in units of 2^-64 turn */
+} pallas_rope_plan;
+
+/* Host only.  INVALID_ARG on a null pointer or a parameter outside its range. */
+int pallas_rope_init(const pallas_rope_config* cfg, pallas_rope_plan* plan);
+
+/* Rotates num_tokens x n_heads bf16 heads of head_dim (>= rotary_dim) contiguous
+ * elements: head h of token t is at d_x + t * x_token_stride + h * x_head_stride
+ * (elements, >= 0) and goes to the same place of d_y and its strides.  d_y may be
+ * d_x with the same strides (in place); otherwise heads read and heads written
+ * must not overlap.  d_positions (int32, device, [num_tokens]) may hold any
+ * int32; angles are exact to 2^-32 turn at every one.  inverse = 1 takes a
+ * rotation by the same plan and position back (angle -p f_i, factor 1 / m), so
+ * it also moves a cached K row: back from p, then on to q.  Rounded once, from
+ * float32.  2-byte alignment suffices; pointers 16-byte aligned, strides and
+ * head_dim multiples of 8 and rotary_dim a multiple of 8 are faster. */
+int pallas_rope_apply(const pallas_rope_plan* plan, int32_t inverse, int32_t num_tokens,
+                      int32_t n_heads, int32_t head_dim, const int32_t* d_positions,
+                      const void* d_x, int64_t x_token_stride, int64_t x_head_stride, void* d_y,
+                      int64_t y_token_stride, int64_t y_head_stride, void* stream);
+
+/* An 8-bit paged KV pool.  A row (one token's K or V of one KV head) is head_dim
+ * codes and one float32 scale, and stands for code * scale:
+ *   codes  [n_layers][2 (K, V)][num_pages][page_size][n_kv_heads][head_dim] bytes
+ *   scales [n_layers][2][num_pages][page_size][n_kv_heads] float32
+ * (device, 16-byte aligned).  With a = the row's largest magnitude:
+ *   E4M3  scale = 2^e, the least power of two (at least 2^-126) with a / scale <=
+ *         448; code = x / scale rounded to nearest even (OCP 8-bit float, 4
+ *         exponent and 3 mantissa bits): reading back rounds nothing more
+ *   INT8  scale = a / 127; code = x * (127 / a) rounded to nearest even in
+ *         [-127, 127] (float32 arithmetic); rows with a < 2^-100 count as zero
+ * A row of zeros has scale 0.  A row with an infinity or a NaN has scale NaN and
+ * codes 0: it reads back, and attends, as NaN.
+ *   Codes and scales are moved by pallas_pack_suffix_blocks and
+ * pallas_assemble_kv, which copy bits: the codes as a pallas_kv_pool of head_dim
+ * / 2, the scales as one of head_dim 2 (n_kv_heads a multiple of 4). */
+typedef enum { PALLAS_QUANT_E4M3 = 1, PALLAS_QUANT_INT8 = 2 } pallas_quant_format;
+typedef struct {
+  void* codes;
+  float* scales;
+  int32_t num_pages;
+  int32_t page_size;  /* 16 */
+  int32_t n_layers;
+  int32_t n_kv_heads;
+  int32_t head_dim;   /* 64 or 128 */
+  int32_t format;     /* pallas_quant_format */
+} pallas_quant_pool;
+
+/* Quantises the K and V of num_tokens (>= 0) tokens into one layer of the pool.
+ * Token t is position d_positions[t] of sequence d_seq_ids[t] (int32, device;
+ * d_seq_ids null: of sequence t, one new token each), whose block table is
+ * d_block_tables + sequence * max_pages.  Its K, bf16 [n_kv_heads][head_dim],
+ * is at d_k + t * k_stride (elements), its V likewise: both 16-byte aligned,
+ * strides a multiple of 8 and at least n_kv_heads * head_dim.
+ *   A token of negative position is padding and is skipped.  A sequence outside
+ * [0, num_seqs), a position beyond the table, or an entry outside [0, num_pages)
+ * is skipped too and raises PALLAS_DEVERR_PAGE in *d_err (nullable).  Nothing
+ * else of the pool is written.  What a slot gets that two tokens of one call
+ * name is undefined. */
+int pallas_quant_store(const pallas_quant_pool* pool, int32_t layer, int32_t num_tokens,
+                       const int32_t* d_seq_ids, const int32_t* d_positions, const void* d_k,
+                       int64_t k_stride, const void* d_v, int64_t v_stride, int32_t num_seqs,
+                       const int32_t* d_block_tables, int32_t max_pages, int32_t* d_err,
+                       void* stream);
+
+/* Reads rows back as bf16 (code * scale in float32, rounded to nearest even), with
+ * pallas_quant_store's arguments and checks; d_k and d_v are written.  Rows of
+ * skipped tokens are left as they were. */
+int pallas_quant_load(const pallas_quant_pool* pool, int32_t layer, int32_t num_tokens,
+                      const int32_t* d_seq_ids, const int32_t* d_positions, void* d_k,
+                      int64_t k_stride, void* d_v, int64_t v_stride, int32_t num_seqs,
+                      const int32_t* d_block_tables, int32_t max_pages, int32_t* d_err,
+                      void* stream);
+
+/* Attention of one new token per sequence over one layer of a paged cache.
+ * Sequence i has d_lengths[i] keys (int32, device), positions [0, length), its
+ * own included once it is stored.  Query head h reads KV head h / (n_q_heads /
+ * n_kv_heads):
+ *   out = sum_j p_j v_j,  p = softmax over j of (scale q . k_j)
+ * d_q and d_out: bf16 [num_seqs] rows of [n_q_heads][head_dim], q_stride and
+ * out_stride elements apart (multiples of 8, 16-byte aligned pointers; d_out may
+ * not overlap d_q).  d_lse (nullable): float32 [num_seqs][n_q_heads], the natural
+ * logarithm of sum_j exp(scale q . k_j), with which results over parts of a
+ * cache are joined.  A row without keys gives zeros and -infinity.
+ *   head_dim 64 or 128 (UNSUPPORTED otherwise), page_size 16, any number of
+ * query heads per KV head, num_seqs up to 65535, max_length (the longest length
+ * the call can meet) at least 1 and at most max_pages * page_size.  A length
+ * outside [0, max_length] is cut to it and raises PALLAS_DEVERR_LENGTH; keys on
+ * pages outside [0, num_pages) are masked and raise PALLAS_DEVERR_PAGE, in *d_err
+ * (nullable).  What is in slots behind a length has no effect.
+ *   Scores, softmax statistics and sums are float32.  A row's results depend, to
+ * the bit, on its own query, keys and length and on num_seqs and n_q_heads alone.
+ * The workspace (device, 256-byte aligned, pallas_attend_workspace_size bytes)
+ * holds nothing between calls. */
+int pallas_attend_kv(const pallas_kv_pool* pool, int32_t layer, int32_t num_seqs, int32_t n_q_heads,
+                     const void* d_q, int64_t q_stride, const int32_t* d_lengths,
+                     int32_t max_length, const int32_t* d_block_tables, int32_t max_pages,
+                     float scale, void* d_out, int64_t out_stride, float* d_lse, void* d_workspace,
+                     size_t ws_bytes, int32_t* d_err, void* stream);
+
+/* The same over an 8-bit pool. */
+int pallas_attend_quant(const pallas_quant_pool* pool, int32_t layer, int32_t num_seqs,
+                        int32_t n_q_heads, const void* d_q, int64_t q_stride,
+                        const int32_t* d_lengths, int32_t max_length,
+                        const int32_t* d_block_tables, int32_t max_pages, float scale, void* d_out,
+                        int64_t out_stride, float* d_lse, void* d_workspace, size_t ws_bytes,
+                        int32_t* d_err, void* stream);
+
+/* Bytes of workspace of a pallas_attend_* call; enough for fewer sequences and a
+ * shorter max_length too.  0 where the call would be refused. */
+size_t pallas_attend_workspace_size(int32_t num_seqs, int32_t n_q_heads, int32_t n_kv_heads,
+                                    int32_t head_dim, int32_t max_length);
+
 /* Coverage check (Section 4.3, "State consistency"), host only: returns
  * PALLAS_OK iff [0, prefix_len) and the ranges [h_starts[j], h_starts[j] +
  * h_lens[j]) together cover [0, n) exactly once (empty ranges are ignored),
@@ -407,15 +582,15 @@ typedef enum {
   PALLAS_K_RMSNORM = 1,    /* prefill only: decode folds its norms into the projections */
   PALLAS_K_ROPE_TABLE = 2, /* none: the rotary factors come with PALLAS_K_EMBED */
   PALLAS_K_GEMM_QKV = 3,   /* prefill Q|K|V projection (K|V only in the last layer) */
-  PALLAS_K_QKV_EPI = 4,    /* prefill QK-norm, rotary, paged K/V store */
+  PALLAS_K_QKV_EPI = 4,    /* prefill QK-norm, rotary, paged K/V store; pallas_rope_apply, pallas_quant_store */
   PALLAS_K_ATTN = 5,       /* prefill causal attention */
   PALLAS_K_GEMM_O = 6,     /* prefill output projection + residual */
   PALLAS_K_GEMM_GATE_UP = 7, /* prefill gate|up projection + SwiGLU */
   PALLAS_K_GEMM_DOWN = 8,  /* prefill down projection + residual */
-  PALLAS_K_PACK = 9,
+  PALLAS_K_PACK = 9,       /* and pallas_quant_load */
   PALLAS_K_ASSEMBLE = 10,
   PALLAS_K_DECODE_PROJ = 11, /* decode projections and lm_head */
-  PALLAS_K_DECODE_ATTN = 12, /* with QK-norm, rotary and the K/V store */
+  PALLAS_K_DECODE_ATTN = 12, /* with QK-norm, rotary and the K/V store; pallas_attend_* */
   PALLAS_K_COUNT = 13
 } pallas_kernel_class;
 

@@ -15,8 +15,10 @@ reconstruction computes, written from the paper:
 * ``scheduler`` -- the prefetching-window model and its online selection,
                    admission, rate smoothing and the stale-preparation bound
                    (Sections 4.1, 4.2 and 4.4).
+* ``cache_ops`` -- operators on the cache: rotary positions, 8-bit rows,
+                   attention of one new token.
 
 It shares no code with the HIP library or its Python binding.  Inputs
 (weights, ids, tables) come from the seeded generators in ``workloads``.
 """
-from . import footprint, numerics, model, paged, scheduler  # noqa: F401
+from . import cache_ops, footprint, numerics, model, paged, scheduler  # noqa: F401

@@ -83,7 +83,29 @@ class Ewma(C.Structure):
     _fields_ = [("value", C.c_double), ("primed", C.c_int32)]
 
 
+ROPE_LAYOUTS = ("half", "interleaved")
+ROPE_SCALINGS = ("none", "linear", "ntk", "yarn", "bands")
+ROPE_MAX_DIM = 256
+
+
+class RopeConfigC(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32), ("trained_len", C.c_int32),
+                ("theta", C.c_double), ("factor", C.c_double), ("fast", C.c_double), ("slow", C.c_double),
+                ("magnitude", C.c_double)]
+
+
+class RopePlan(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32), ("layout", C.c_int32), ("magnitude", C.c_float), ("reserved", C.c_int32),
+                ("turns", C.c_uint64 * (ROPE_MAX_DIM // 2))]
+
+
+class QuantPoolC(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("num_pages", C.c_int32), ("page_size", C.c_int32),
+                ("n_layers", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("format", C.c_int32)]
+
+
 _vp, _i32, _u64, _sz = C.c_void_p, C.c_int32, C.c_uint64, C.c_size_t
+_i64 = C.c_int64
 _pi32 = C.POINTER(C.c_int32)
 
 # name -> (restype, argtypes); mirrors include/pallas.h
@@ -105,6 +127,18 @@ EXPORTS = {
                                      _vp, _sz, _vp, _vp]),
     "pallas_decode_step_static": (C.c_int, [_vp, _i32, _vp, _pi32, _vp, _i32, C.POINTER(KVPoolC), _vp,
                                             _vp, _vp]),
+    "pallas_rope_init": (C.c_int, [C.POINTER(RopeConfigC), C.POINTER(RopePlan)]),
+    "pallas_rope_apply": (C.c_int, [C.POINTER(RopePlan), _i32, _i32, _i32, _i32, _vp, _vp, _i64, _i64, _vp, _i64,
+                                    _i64, _vp]),
+    "pallas_quant_store": (C.c_int, [C.POINTER(QuantPoolC), _i32, _i32, _vp, _vp, _vp, _i64, _vp, _i64, _i32, _vp,
+                                     _i32, _vp, _vp]),
+    "pallas_quant_load": (C.c_int, [C.POINTER(QuantPoolC), _i32, _i32, _vp, _vp, _vp, _i64, _vp, _i64, _i32, _vp,
+                                    _i32, _vp, _vp]),
+    "pallas_attend_kv": (C.c_int, [C.POINTER(KVPoolC), _i32, _i32, _i32, _vp, _i64, _vp, _i32, _vp, _i32, C.c_float,
+                                   _vp, _i64, _vp, _vp, _sz, _vp, _vp]),
+    "pallas_attend_quant": (C.c_int, [C.POINTER(QuantPoolC), _i32, _i32, _i32, _vp, _i64, _vp, _i32, _vp, _i32,
+                                      C.c_float, _vp, _i64, _vp, _vp, _sz, _vp, _vp]),
+    "pallas_attend_workspace_size": (_sz, [_i32, _i32, _i32, _i32, _i32]),
     "pallas_check_coverage": (C.c_int, [_i32, _pi32, _pi32, _i32, _i32]),
     "pallas_window_evaluate": (C.c_int, [C.POINTER(WindowParams), C.c_double, C.c_double, C.c_double,
                                          C.POINTER(WindowDecision)]),
@@ -270,6 +304,154 @@ def pallas_decode_step_static(h, tokens, positions: Sequence[int], block_tables,
     _check(lib().pallas_decode_step_static(h, len(positions), _ptr(tokens), _i32_array(positions),
                                            _ptr(block_tables), block_tables.shape[-1], C.byref(ps),
                                            _ptr(logits), _ptr(err), _stream(stream)))
+
+
+# ------------------------------------------------------------ cache operators
+def _bad(msg: str):
+    raise PallasError(Status.INVALID_ARG, msg)
+
+
+def _want(t, what: str, dtype, ndim: int, device, whole: bool = True):
+    """A tensor on the call's device, of the type and rank that the kernels take:
+    contiguous, or (``whole`` false) contiguous in its last dimension."""
+    if t.dtype != dtype or t.dim() != ndim or t.device != device:
+        _bad(f"{what}: {t.dtype} of rank {t.dim()} on {t.device}, wanted {dtype} of rank {ndim} on {device}")
+    if whole and not t.is_contiguous() or t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
+        _bad(f"{what}: strides {tuple(t.stride())}")
+
+
+def _device_call(device, stream, call):
+    """``call(stream handle)`` with the tensors' device current, on its current stream unless one is given."""
+    import torch
+    if device.type != "cuda":
+        _bad(f"tensors on {device}, wanted a GPU")
+    with torch.cuda.device(device):
+        _check(call(_stream(stream)))
+
+
+def _opt(t, what, dtype, ndim, device):
+    if t is not None:
+        _want(t, what, dtype, ndim, device)
+    return _ptr(t)
+
+
+def pallas_rope_init(rotary_dim: int, theta: float, layout: str = "half", scaling: str = "none", factor: float = 1.0,
+                     trained_len: int = 0, fast: float = 0.0, slow: float = 0.0, magnitude: float = 0.0) -> RopePlan:
+    """The plan of a rotary embedding: ``layout`` of ROPE_LAYOUTS, ``scaling`` of ROPE_SCALINGS."""
+    if layout not in ROPE_LAYOUTS or scaling not in ROPE_SCALINGS:
+        _bad(f"rope: layout {layout!r}, scaling {scaling!r}")
+    cfg = RopeConfigC(rotary_dim, ROPE_LAYOUTS.index(layout), ROPE_SCALINGS.index(scaling), trained_len, theta, factor,
+                      fast, slow, magnitude)
+    plan = RopePlan()
+    _check(lib().pallas_rope_init(C.byref(cfg), C.byref(plan)))
+    return plan
+
+
+def pallas_rope_apply(plan: RopePlan, x, positions, out=None, inverse: bool = False, stream=None):
+    """``x``, ``out``: bf16 [tokens, heads, head_dim] of any token and head strides; in place without ``out``."""
+    import torch
+    out = x if out is None else out
+    T, H, d = x.shape if x.dim() == 3 else (-1, -1, -1)
+    _want(x, "rope: x", torch.bfloat16, 3, x.device, whole=False)
+    _want(out, "rope: out", torch.bfloat16, 3, x.device, whole=False)
+    _want(positions, "rope: positions", torch.int32, 1, x.device)
+    if out.shape != x.shape or positions.shape[0] != T:
+        _bad(f"rope: {tuple(x.shape)} to {tuple(out.shape)} at {positions.shape[0]} positions")
+    if T == 0 or H == 0:
+        return out
+    _device_call(x.device, stream, lambda s: lib().pallas_rope_apply(
+        C.byref(plan), int(bool(inverse)), T, H, d, _ptr(positions), _ptr(x), x.stride(0), x.stride(1), _ptr(out),
+        out.stride(0), out.stride(1), s))
+    return out
+
+
+def quant_pool_struct(codes, scales) -> QuantPoolC:
+    """``codes``: float8_e4m3fn or int8 [L, 2, P, page, Hkv, d]; ``scales``: float32 [L, 2, P, page, Hkv]."""
+    import torch
+    fmt = {torch.float8_e4m3fn: 1, torch.int8: 2}.get(codes.dtype)
+    if fmt is None:
+        _bad(f"quant pool: codes of {codes.dtype}, wanted float8_e4m3fn or int8")
+    _want(codes, "quant pool: codes", codes.dtype, 6, codes.device)
+    _want(scales, "quant pool: scales", torch.float32, 5, codes.device)
+    if codes.shape[1] != 2 or codes.shape[:5] != scales.shape:
+        _bad(f"quant pool: codes {tuple(codes.shape)}, scales {tuple(scales.shape)}")
+    L, _, P, page, hkv, d = codes.shape
+    return QuantPoolC(codes.data_ptr(), scales.data_ptr(), P, page, L, hkv, d, fmt)
+
+
+def _quant_call(name, codes, scales, layer, k, v, positions, block_tables, seq_ids, err, stream):
+    import torch
+    dev = codes.device
+    ps = quant_pool_struct(codes, scales)
+    T = positions.shape[0]
+    for t, what in ((k, "k"), (v, "v")):
+        _want(t, f"{name}: {what}", torch.bfloat16, 3, dev, whole=False)
+        if tuple(t.shape) != (T, ps.n_kv_heads, ps.head_dim) or T and t.stride(1) != ps.head_dim and t.shape[1] > 1:
+            _bad(f"{name}: {what} {tuple(t.shape)}, strides {tuple(t.stride())}")
+    _want(positions, f"{name}: positions", torch.int32, 1, dev)
+    _want(block_tables, f"{name}: block tables", torch.int32, 2, dev)
+    if seq_ids is not None and tuple(seq_ids.shape) != (T,):
+        _bad(f"{name}: {tuple(seq_ids.shape)} sequence ids of {T} tokens")
+    if T == 0:
+        return
+    row = ps.n_kv_heads * ps.head_dim           # (the stride of a single token says nothing)
+    ks, vs = (t.stride(0) if T > 1 else row for t in (k, v))
+    seq, e = _opt(seq_ids, f"{name}: sequence ids", torch.int32, 1, dev), _opt(err, f"{name}: err", torch.int32, 1, dev)
+    _device_call(dev, stream, lambda s: getattr(lib(), f"pallas_{name}")(
+        C.byref(ps), layer, T, seq, _ptr(positions), _ptr(k), ks, _ptr(v), vs, block_tables.shape[0],
+        _ptr(block_tables), block_tables.shape[1], e, s))
+
+
+def pallas_quant_store(codes, scales, layer: int, k, v, positions, block_tables, seq_ids=None, err=None, stream=None):
+    """Quantises ``k``, ``v`` (bf16 [tokens, Hkv, d], any token stride) into a layer of the pool (quant_pool_struct)."""
+    _quant_call("quant_store", codes, scales, layer, k, v, positions, block_tables, seq_ids, err, stream)
+
+
+def pallas_quant_load(codes, scales, layer: int, k, v, positions, block_tables, seq_ids=None, err=None, stream=None):
+    """Reads rows of a layer back into ``k``, ``v`` (bf16 [tokens, Hkv, d], any token stride)."""
+    _quant_call("quant_load", codes, scales, layer, k, v, positions, block_tables, seq_ids, err, stream)
+
+
+def pallas_attend_workspace_size(num_seqs: int, n_q_heads: int, n_kv_heads: int, head_dim: int, max_length: int) -> int:
+    return int(lib().pallas_attend_workspace_size(num_seqs, n_q_heads, n_kv_heads, head_dim, max_length))
+
+
+def _attend_call(name, ps, dev, layer, q, lengths, max_length, block_tables, scale, out, workspace, lse, err, stream):
+    import torch
+    for t, what in ((q, "q"), (out, "out")):
+        _want(t, f"{name}: {what}", torch.bfloat16, 3, dev, whole=False)
+        if t.shape != q.shape or t.shape[2] != ps.head_dim or t.shape[1] > 1 and t.stride(1) != ps.head_dim:
+            _bad(f"{name}: {what} {tuple(t.shape)}, strides {tuple(t.stride())}")
+    S, H, d = q.shape
+    _want(lengths, f"{name}: lengths", torch.int32, 1, dev)
+    _want(block_tables, f"{name}: block tables", torch.int32, 2, dev)
+    if lengths.shape[0] != S or block_tables.shape[0] != S:
+        _bad(f"{name}: {S} queries, {lengths.shape[0]} lengths, {block_tables.shape[0]} tables")
+    if lse is not None and tuple(lse.shape) != (S, H):
+        _bad(f"{name}: lse {tuple(lse.shape)}")
+    if workspace.device != dev or not workspace.is_contiguous():
+        _bad(f"{name}: workspace")
+    qs, os = (t.stride(0) if S > 1 else H * d for t in (q, out))
+    ls, e = _opt(lse, f"{name}: lse", torch.float32, 2, dev), _opt(err, f"{name}: err", torch.int32, 1, dev)
+    _device_call(dev, stream, lambda s: getattr(lib(), f"pallas_{name}")(
+        C.byref(ps), layer, S, H, _ptr(q), qs, _ptr(lengths), max_length, _ptr(block_tables), block_tables.shape[1],
+        scale, _ptr(out), os, ls, _ptr(workspace), workspace.numel() * workspace.element_size(), e, s))
+
+
+def pallas_attend_kv(pool, layer: int, q, lengths, max_length: int, block_tables, scale: float, out, workspace, lse=None,
+                     err=None, stream=None):
+    """One new token per sequence: ``q``, ``out`` bf16 [num_seqs, Hq, d] (any row stride) over a bf16 pool."""
+    import torch
+    _want(pool, "attend_kv: pool", torch.bfloat16, 6, pool.device)
+    _attend_call("attend_kv", kv_pool_struct(pool), pool.device, layer, q, lengths, max_length, block_tables, scale, out,
+                 workspace, lse, err, stream)
+
+
+def pallas_attend_quant(codes, scales, layer: int, q, lengths, max_length: int, block_tables, scale: float, out,
+                        workspace, lse=None, err=None, stream=None):
+    """The same over an 8-bit pool (quant_pool_struct)."""
+    _attend_call("attend_quant", quant_pool_struct(codes, scales), codes.device, layer, q, lengths, max_length,
+                 block_tables, scale, out, workspace, lse, err, stream)
 
 
 def _window_params(r_p, r_d, goodput, s_kv, t_load=0.0, t_0=0.0, alpha=0.8, t_max=5.0, dt=0.01):

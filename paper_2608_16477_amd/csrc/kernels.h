@@ -5,6 +5,10 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
+#include "pallas.h"
+
 namespace pallas {
 
 // ----------------------------------------------------------------- KV copies
@@ -349,6 +353,94 @@ struct DecodeRuns {
 bool plan_decode_runs(const RowMap& rm, int Hkv, DecodeRuns& runs);
 hipError_t launch_attention_decode(const DecodeAttnParams& p, const RowMap& rm, const DecodeRuns& runs, float* part,
                                    int max_splits, hipStream_t s);
+
+// ------------------------------------------------------------ cache operators
+// rope.hip: rows of heads rotated by pos * turns[i] (units of 2^-64 turn).
+struct RopeParams {
+  const uint16_t* x;
+  uint16_t* y;
+  int64_t x_token, x_head, y_token, y_head;   // strides, elements
+  const int32_t* pos;
+  int tokens, heads, d, r;
+  int interleaved;
+  int negate;                                 // 1: by the negative angle
+  float magnitude;
+  uint64_t turns[PALLAS_ROPE_MAX_DIM / 2];
+};
+hipError_t launch_rope(const RopeParams& p, hipStream_t s);
+
+// quant_kv.hip: rows of one layer of an 8-bit pool, written and read back.
+struct QuantParams {
+  uint8_t* codes;          // [2][num_pages][16][Hkv][d], K and V planes of the layer
+  float* scales;           // [2][num_pages][16][Hkv]
+  int num_pages, Hkv, d;
+  int int8;                // else E4M3
+  const int32_t* seq;      // [tokens] or null (token t: sequence t)
+  const int32_t* pos;      // [tokens]
+  const int32_t* bt;       // [seqs][max_pages]
+  int tokens, seqs, max_pages;
+  const uint16_t* k;       // store: rows in
+  const uint16_t* v;
+  uint16_t* k_out;         // load: rows out
+  uint16_t* v_out;
+  int64_t k_stride, v_stride;
+  int32_t* err;
+};
+hipError_t launch_quant_store(const QuantParams& p, hipStream_t s);
+hipError_t launch_quant_load(const QuantParams& p, hipStream_t s);
+
+// attend.hip: one new token per sequence over a paged cache.
+enum CacheType { kCacheBf16 = 0, kCacheE4m3 = 1, kCacheInt8 = 2 };
+struct AttendParams {
+  const void* k;           // [num_pages][16][Hkv][d] of the layer
+  const void* v;
+  const float* k_scale;    // [num_pages][16][Hkv] (8-bit)
+  const float* v_scale;
+  int num_pages, Hkv, Hq, d;
+  int seqs, max_length, max_pages;
+  const uint16_t* q;
+  int64_t q_stride;
+  const int32_t* lengths;
+  const int32_t* bt;
+  float scale_log2;        // scale * log2(e)
+  uint16_t* out;
+  int64_t out_stride;
+  float* lse;              // [seqs][Hq] or null
+  int splits;              // records per row: attend_splits
+  float* part_o;           // [seqs][Hq][splits][d]
+  float* part_ml;          // [seqs][Hq][splits][2]
+  int32_t* err;
+};
+// A row's keys are cut into splits of a length that follows from its own length
+// and the number of (sequence, head group) rows of the call.
+constexpr int kAttendMinSplit = 128;
+constexpr int kAttendMaxSplit = 1024;
+constexpr int kAttendTarget = 1024;      // workgroups that fill the chip
+constexpr int kAttendGroup = 16;         // query heads that share one pass over a KV head
+__host__ __device__ inline int attend_split_keys(int len, int rows) {
+  const int64_t want = (int64_t(len) * rows + kAttendTarget - 1) / kAttendTarget;
+  if (want >= kAttendMaxSplit) return kAttendMaxSplit;
+  return want <= kAttendMinSplit ? kAttendMinSplit : (int(want) + kAttendMinSplit - 1) / kAttendMinSplit * kAttendMinSplit;
+}
+inline int64_t attend_rows(int64_t seqs, int Hq, int Hkv) {
+  return seqs * Hkv * ((Hq / Hkv + kAttendGroup - 1) / kAttendGroup);
+}
+// The most splits a row of up to max_length keys has: attend_split_keys >=
+// len * rows / kAttendTarget unless it is the largest, so len / split <= target / rows.
+inline int attend_splits(int max_length, int64_t rows) {
+  const int64_t by_min = (int64_t(max_length) + kAttendMinSplit - 1) / kAttendMinSplit;
+  const int64_t by_max = (int64_t(max_length) + kAttendMaxSplit - 1) / kAttendMaxSplit;
+  const int64_t by_target = (kAttendTarget + rows - 1) / rows;
+  return int(std::min(by_min, std::max(by_max, by_target)));
+}
+// Records of a call, bounded by something that grows with seqs and max_length
+// (rows * attend_splits does not: ceil(target / rows) falls in steps).
+inline size_t attend_records(int max_length, int64_t rows) {
+  const int64_t by_min = (int64_t(max_length) + kAttendMinSplit - 1) / kAttendMinSplit;
+  const int64_t by_max = (int64_t(max_length) + kAttendMaxSplit - 1) / kAttendMaxSplit;
+  return size_t(std::max(rows * by_max, std::min(rows * by_min, rows + kAttendTarget)));
+}
+hipError_t launch_attend(const AttendParams& p, CacheType type, hipStream_t s);
 
 // ------------------------------------------------------------ skinny GEMM
 // C[m][n] (op) A[m] . B[n] for m < M <= 8 rows (gemv.hip); epilogues as

@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "pallas.h"
+#include "api.h"
 #include "kernels.h"
 #include "model_plan.h"
 
@@ -20,10 +21,11 @@ static_assert(PALLAS_MAX_DECODE_POS == pallas::kDecodeMaxPos - 1, "decode positi
 #include "profile.h"
 
 namespace {
-
 thread_local std::string g_err;
+}
 
-int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+namespace pallas {
+
 int fail(int code, const char* fmt, ...) {
   char buf[512];
   va_list ap;
@@ -52,6 +54,14 @@ int check_pool(const pallas_kv_pool* p, const char* what) {
                 (long long)row);
   return PALLAS_OK;
 }
+
+}  // namespace pallas
+
+namespace {
+
+using pallas::check_pool;
+using pallas::fail;
+using pallas::hip_fail;
 
 pallas::PoolGeom geom_of(const pallas_kv_pool* p) {
   pallas::PoolGeom g;

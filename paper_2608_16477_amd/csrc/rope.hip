@@ -1,0 +1,160 @@
+// Rotary positions of rows of heads: pair i of head h of token t turns by
+// pos[t] * f_i, in the half or the interleaved layout, over the first r
+// elements of the head; the others are copied.
+//
+// Angles are kept in turns, as 64-bit fixed point fractions: pos * turns[i] modulo
+// 2^64 is the angle without its whole turns, exactly, at any position, so far
+// positions lose nothing and nothing needs 64-bit floating point.  The two top bits
+// (rounded) are the quarter, and what is left, within an eighth of a turn,
+// goes through the Taylor polynomials of sine and cosine.
+//
+// The floor is one read and one write of the rows.
+#include "common.h"
+#include "kernels.h"
+
+namespace pallas {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPasses = 5;   // units of a thread whose loads are in flight together
+
+// (cos, sin) of an angle of `a` 2^-64 turns, times m.  |rest| <= pi / 4: the first
+// terms left out are below 2^-29 (sine, x^11 / 11!) and 2^-32 (cosine, x^12 / 12!)
+// of a radian.
+__device__ __forceinline__ void turn_cos_sin(uint64_t a, float m, float& c, float& s) {
+  const uint64_t quarter = (a + (uint64_t(1) << 61)) >> 62;
+  const int32_t rest = static_cast<int32_t>(static_cast<int64_t>(a - (quarter << 62)) >> 32);
+  const float x = static_cast<float>(rest) * 1.46291807926715968e-9f;   // 2 pi 2^-32
+  const float z = x * x;
+  float sp = __builtin_fmaf(z, 2.75573192e-6f, -1.98412698e-4f);
+  sp = __builtin_fmaf(z, sp, 8.33333333e-3f);
+  sp = __builtin_fmaf(z, sp, -1.66666667e-1f);
+  sp = __builtin_fmaf(z * x, sp, x);
+  float cp = __builtin_fmaf(z, -2.75573192e-7f, 2.48015873e-5f);
+  cp = __builtin_fmaf(z, cp, -1.38888889e-3f);
+  cp = __builtin_fmaf(z, cp, 4.16666667e-2f);
+  cp = __builtin_fmaf(z, cp, -0.5f);
+  cp = __builtin_fmaf(z, cp, 1.0f);
+  const bool odd = quarter & 1;
+  const float cm = (quarter + 1) & 2 ? -m : m, sm = quarter & 2 ? -m : m;
+  c = (odd ? sp : cp) * cm;
+  s = (odd ? cp : sp) * sm;
+}
+
+__device__ __forceinline__ uint64_t turned(const RopeParams& p, int pos, int i) {
+  const uint64_t a = static_cast<uint64_t>(static_cast<int64_t>(pos)) * p.turns[i];
+  return p.negate ? 0 - a : a;
+}
+
+// A unit is 16 bytes of a head: four pairs (half layout: two 8-byte halves), or
+// 8 elements behind the rotated ones.  `units` of a head are worked on (the
+// copied ones only where y is not x).  A thread keeps its unit, and so its four
+// angles, for all the heads that it takes: `slots` heads of a token go side by
+// side (several tokens where a token has fewer), kPasses times.
+__global__ __launch_bounds__(kThreads) void rope_kernel(RopeParams p, int units, int slots, int tokens_per, int heads_per) {
+  const int j = threadIdx.x % units, slot = threadIdx.x / units;
+  const int t = blockIdx.x * tokens_per + (tokens_per > 1 ? slot / p.heads : 0);
+  int h = tokens_per > 1 ? slot % p.heads : slot + blockIdx.y * heads_per;
+  const int h1 = tokens_per > 1 ? p.heads : min(p.heads, static_cast<int>(blockIdx.y + 1) * heads_per);
+  if (slot >= (tokens_per > 1 ? tokens_per * p.heads : slots) || t >= p.tokens) return;
+  const bool turn = 8 * j < p.r;
+  const bool half = !p.interleaved && turn;
+  const int lo = half ? 4 * j : 8 * j, hi = half ? p.r / 2 + 4 * j : 8 * j + 4;
+  const uint16_t* x = p.x + t * p.x_token;
+  uint16_t* y = p.y + t * p.y_token;
+  float c[4], s[4];
+  if (turn) {
+    const int pos = p.pos[t];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) turn_cos_sin(turned(p, pos, 4 * j + e), p.magnitude, c[e], s[e]);
+  }
+  for (; h < h1; h += kPasses * slots) {
+    u32x2 a[kPasses], b[kPasses];
+#pragma unroll
+    for (int k = 0; k < kPasses; ++k) {
+      if (h + k * slots >= h1) continue;
+      const uint16_t* src = x + (h + k * slots) * p.x_head;
+      a[k] = *reinterpret_cast<const u32x2*>(src + lo);
+      b[k] = *reinterpret_cast<const u32x2*>(src + hi);
+    }
+#pragma unroll
+    for (int k = 0; k < kPasses; ++k) {
+      if (h + k * slots >= h1) continue;
+      if (turn) {
+        // half: a = x0 of pairs 0 .. 3, b = x1; interleaved: a, b = pairs 0, 1 and 2, 3
+        const float v[8] = {bflo(a[k].x), bfhi(a[k].x), bflo(a[k].y), bfhi(a[k].y),
+                            bflo(b[k].x), bfhi(b[k].x), bflo(b[k].y), bfhi(b[k].y)};
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float x0 = half ? v[e] : v[2 * e], x1 = half ? v[e + 4] : v[2 * e + 1];
+          const float y0 = x0 * c[e] - x1 * s[e], y1 = x1 * c[e] + x0 * s[e];
+          if (half) {
+            w[e] = y0;
+            w[e + 4] = y1;
+          } else {
+            w[2 * e] = y0;
+            w[2 * e + 1] = y1;
+          }
+        }
+        a[k] = u32x2{pack_bf2(w[0], w[1]), pack_bf2(w[2], w[3])};
+        b[k] = u32x2{pack_bf2(w[4], w[5]), pack_bf2(w[6], w[7])};
+      }
+      uint16_t* dst = y + (h + k * slots) * p.y_head;
+      *reinterpret_cast<u32x2*>(dst + lo) = a[k];
+      *reinterpret_cast<u32x2*>(dst + hi) = b[k];
+    }
+  }
+}
+
+// The same a pair (or two copied elements, the last alone in an odd head) at a
+// time, for any alignment.
+__global__ __launch_bounds__(kThreads) void rope_any_kernel(RopeParams p) {
+  const int t = blockIdx.x;
+  const bool copy = p.x != p.y;
+  const int units = p.r / 2 + (copy ? (p.d - p.r + 1) / 2 : 0);
+  const int pos = p.pos[t];
+  for (int e = blockIdx.y * kThreads + threadIdx.x; e < units * p.heads; e += gridDim.y * kThreads) {
+    const int h = e / units, i = e - h * units;
+    const uint16_t* x = p.x + t * p.x_token + h * p.x_head;
+    uint16_t* y = p.y + t * p.y_token + h * p.y_head;
+    if (2 * i < p.r) {
+      const int lo = p.interleaved ? 2 * i : i, hi = p.interleaved ? 2 * i + 1 : i + p.r / 2;
+      float c, s;
+      turn_cos_sin(turned(p, pos, i), p.magnitude, c, s);
+      const float x0 = bf2f(x[lo]), x1 = bf2f(x[hi]);
+      y[lo] = f2bf(x0 * c - x1 * s);
+      y[hi] = f2bf(x1 * c + x0 * s);
+    } else {
+      y[2 * i] = x[2 * i];
+      if (2 * i + 1 < p.d) y[2 * i + 1] = x[2 * i + 1];
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_rope(const RopeParams& p, hipStream_t s) {
+  if (p.tokens == 0) return hipSuccess;
+  auto by = [](const void* q, int64_t a, int64_t b) {
+    return (reinterpret_cast<uintptr_t>(q) & 15) == 0 && a % 8 == 0 && b % 8 == 0;
+  };
+  if (p.r % 8 != 0 || p.d % 8 != 0 || p.d > 8 * kThreads || !by(p.x, p.x_token, p.x_head) ||
+      !by(p.y, p.y_token, p.y_head)) {
+    const int64_t units = (int64_t(p.d) + 1) / 2 * p.heads;
+    const dim3 grid(p.tokens, static_cast<unsigned>(std::min<int64_t>((units + kThreads - 1) / kThreads, 64)));
+    rope_any_kernel<<<grid, kThreads, 0, s>>>(p);
+    return hipGetLastError();
+  }
+  const int units = p.x == p.y ? p.r / 8 : p.d / 8;
+  const int slots = kThreads / units;
+  const int tokens_per = std::max(1, slots / p.heads);
+  // Few tokens: a token's heads over several workgroups.
+  const int heads_per = p.tokens < 512 ? slots : p.heads;
+  const dim3 grid((p.tokens + tokens_per - 1) / tokens_per, tokens_per > 1 ? 1 : (p.heads + heads_per - 1) / heads_per);
+  rope_kernel<<<grid, kThreads, 0, s>>>(p, units, slots, tokens_per, heads_per);
+  return hipGetLastError();
+}
+
+}  // namespace pallas
