@@ -482,7 +482,8 @@ int pallas_attend_kv(const pallas_kv_pool* pool, int32_t layer, int32_t num_seqs
                      float scale, void* d_out, int64_t out_stride, float* d_lse, void* d_workspace,
                      size_t ws_bytes, int32_t* d_err, void* stream);
 
-/* The same over an 8-bit pool. */
+/* The same over an 8-bit pool.  One layer's scales must stay below 4 GiB
+ * (UNSUPPORTED). */
 int pallas_attend_quant(const pallas_quant_pool* pool, int32_t layer, int32_t num_seqs,
                         int32_t n_q_heads, const void* d_q, int64_t q_stride,
                         const int32_t* d_lengths, int32_t max_length,

@@ -303,11 +303,12 @@ int pallas_attend_quant(const pallas_quant_pool* pool, int32_t layer, int32_t nu
   const char* what = "attend (8-bit)";
   if (int rc = check_quant_pool(pool, layer, what)) return rc;
   const int64_t rows = plane_rows(pool);
+  if (2 * rows * 4 > int64_t(0xFFFFFF00))   // addressed with 32-bit offsets
+    return fail(PALLAS_ERR_UNSUPPORTED, "%s: a layer's scales of %lld bytes exceed 4 GiB", what, (long long)(2 * rows * 4));
   pallas::AttendParams p{};
   p.k = static_cast<const uint8_t*>(pool->codes) + 2 * layer * rows * pool->head_dim;
   p.v = static_cast<const uint8_t*>(pool->codes) + (2 * layer + 1) * rows * pool->head_dim;
-  p.k_scale = pool->scales + 2 * layer * rows;
-  p.v_scale = pool->scales + (2 * layer + 1) * rows;
+  p.scales = pool->scales + 2 * layer * rows;
   p.num_pages = pool->num_pages;
   p.Hkv = pool->n_kv_heads;
   p.d = pool->head_dim;

@@ -394,8 +394,7 @@ enum CacheType { kCacheBf16 = 0, kCacheE4m3 = 1, kCacheInt8 = 2 };
 struct AttendParams {
   const void* k;           // [num_pages][16][Hkv][d] of the layer
   const void* v;
-  const float* k_scale;    // [num_pages][16][Hkv] (8-bit)
-  const float* v_scale;
+  const float* scales;     // 8-bit: [2][num_pages][16][Hkv], K and V of the layer, below 4 GiB
   int num_pages, Hkv, Hq, d;
   int seqs, max_length, max_pages;
   const uint16_t* q;

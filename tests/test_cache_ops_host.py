@@ -156,6 +156,10 @@ def test_attend_refusals(P, quant):
         KVPoolC(FAKE, 8, 16, 2, 4, 96), KVPoolC(FAKE, 8, 32, 2, 4, 64), KVPoolC(FAKE, 8, 16, 2, 4, 256)]
     for pool in pools:
         assert attend_rc(P, quant, pool, qs=4096, os=4096) == S.UNSUPPORTED
+    if quant:      # a layer's scales, 2 * 16 * 4 * 4 bytes a page, from 4 GiB on
+        assert attend_rc(P, quant, quant_pool(num_pages=1 << 23)) == S.UNSUPPORTED
+        assert "4 GiB" in P.pallas_last_error()
+        assert attend_rc(P, quant, quant_pool(num_pages=(1 << 23) - 1), ws_bytes=0) == S.WORKSPACE
     need = P.pallas_attend_workspace_size(3, 8, 4, 64, 64)
     assert attend_rc(P, quant, ws_bytes=need - 1) == S.WORKSPACE
     assert attend_rc(P, quant, ws_bytes=0) == S.WORKSPACE
