@@ -307,32 +307,62 @@ def pallas_decode_step_static(h, tokens, positions: Sequence[int], block_tables,
 
 
 # ------------------------------------------------------------ cache operators
+# These check what they are given (type, rank, strides, device), as the library sees
+# addresses alone.  A call's checks cost as much as its launch where tensors are asked
+# more than needed, so each is asked once: shape and stride as tuples, the device as an
+# index (-1: host).
+_torch = None
+
+
+def _load_torch():
+    global _torch
+    import torch
+    _torch = torch
+    return torch
+
+
 def _bad(msg: str):
     raise PallasError(Status.INVALID_ARG, msg)
 
 
-def _want(t, what: str, dtype, ndim: int, device, whole: bool = True):
-    """A tensor on the call's device, of the type and rank that the kernels take:
-    contiguous, or (``whole`` false) contiguous in its last dimension."""
-    if t.dtype != dtype or t.dim() != ndim or t.device != device:
-        _bad(f"{what}: {t.dtype} of rank {t.dim()} on {t.device}, wanted {dtype} of rank {ndim} on {device}")
-    if whole and not t.is_contiguous() or t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
-        _bad(f"{what}: strides {tuple(t.stride())}")
+def _refuse(t, what: str, dtype, ndim: int, dev: int):
+    _bad(f"{what}: {t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}; wanted {dtype} of rank {ndim} on "
+         f"{'GPU ' + str(dev) if dev >= 0 else 'a GPU'}, contiguous (in its last dimension at least)")
 
 
-def _device_call(device, stream, call):
-    """``call(stream handle)`` with the tensors' device current, on its current stream unless one is given."""
-    import torch
-    if device.type != "cuda":
-        _bad(f"tensors on {device}, wanted a GPU")
-    with torch.cuda.device(device):
-        _check(call(_stream(stream)))
+def _whole(t, what: str, dtype, ndim: int, dev: int):
+    """The shape of a contiguous tensor of this type and rank on GPU ``dev``."""
+    shape = t.shape
+    if t.dtype is not dtype or len(shape) != ndim or t.get_device() != dev or dev < 0 or not t.is_contiguous():
+        _refuse(t, what, dtype, ndim, dev)
+    return shape
 
 
-def _opt(t, what, dtype, ndim, device):
-    if t is not None:
-        _want(t, what, dtype, ndim, device)
-    return _ptr(t)
+def _rows(t, what: str, dev: int):
+    """Shape and strides of bf16 rows [tokens, heads, d] whose d elements are contiguous."""
+    shape, stride = t.shape, t.stride()
+    if t.dtype is not (_torch or _load_torch()).bfloat16 or len(shape) != 3 or t.get_device() != dev or dev < 0 or (
+            stride[2] != 1 and shape[2] > 1):
+        _refuse(t, what, "bfloat16", 3, dev)
+    return shape, stride
+
+
+def _packed_rows(t, what: str, dev: int, shape):
+    """The row stride of rows of this shape with their heads one behind the other."""
+    got, stride = _rows(t, what, dev)
+    if got != shape or (stride[1] != shape[2] and shape[1] > 1):
+        _bad(f"{what}: {tuple(got)}, strides {stride}; wanted {tuple(shape)}, its heads contiguous")
+    return stride[0] if shape[0] > 1 else shape[1] * shape[2]     # (the stride of a single row says nothing)
+
+
+def _launch(dev: int, stream, call, *args):
+    """``call(*args, stream)`` with the tensors' GPU current, on its current stream unless one is given."""
+    cuda = _torch.cuda
+    if cuda.current_device() == dev:
+        _check(call(*args, _stream(stream)))
+    else:
+        with cuda.device(dev):
+            _check(call(*args, _stream(stream)))
 
 
 def pallas_rope_init(rotary_dim: int, theta: float, layout: str = "half", scaling: str = "none", factor: float = 1.0,
@@ -349,109 +379,101 @@ def pallas_rope_init(rotary_dim: int, theta: float, layout: str = "half", scalin
 
 def pallas_rope_apply(plan: RopePlan, x, positions, out=None, inverse: bool = False, stream=None):
     """``x``, ``out``: bf16 [tokens, heads, head_dim] of any token and head strides; in place without ``out``."""
-    import torch
-    out = x if out is None else out
-    T, H, d = x.shape if x.dim() == 3 else (-1, -1, -1)
-    _want(x, "rope: x", torch.bfloat16, 3, x.device, whole=False)
-    _want(out, "rope: out", torch.bfloat16, 3, x.device, whole=False)
-    _want(positions, "rope: positions", torch.int32, 1, x.device)
-    if out.shape != x.shape or positions.shape[0] != T:
-        _bad(f"rope: {tuple(x.shape)} to {tuple(out.shape)} at {positions.shape[0]} positions")
-    if T == 0 or H == 0:
-        return out
-    _device_call(x.device, stream, lambda s: lib().pallas_rope_apply(
-        C.byref(plan), int(bool(inverse)), T, H, d, _ptr(positions), _ptr(x), x.stride(0), x.stride(1), _ptr(out),
-        out.stride(0), out.stride(1), s))
+    torch = _torch or _load_torch()
+    dev = x.get_device()
+    shape, xs = _rows(x, "rope: x", dev)
+    if out is None:
+        out, ys = x, xs
+    else:
+        to, ys = _rows(out, "rope: out", dev)
+        if to != shape:
+            _bad(f"rope: {tuple(shape)} to {tuple(to)}")
+    T, H, d = shape
+    if _whole(positions, "rope: positions", torch.int32, 1, dev)[0] != T:
+        _bad(f"rope: {positions.shape[0]} positions of {T} tokens")
+    if T and H:
+        _launch(dev, stream, lib().pallas_rope_apply, C.byref(plan), 1 if inverse else 0, T, H, d, positions.data_ptr(),
+                x.data_ptr(), xs[0], xs[1], out.data_ptr(), ys[0], ys[1])
     return out
 
 
 def quant_pool_struct(codes, scales) -> QuantPoolC:
     """``codes``: float8_e4m3fn or int8 [L, 2, P, page, Hkv, d]; ``scales``: float32 [L, 2, P, page, Hkv]."""
-    import torch
-    fmt = {torch.float8_e4m3fn: 1, torch.int8: 2}.get(codes.dtype)
-    if fmt is None:
-        _bad(f"quant pool: codes of {codes.dtype}, wanted float8_e4m3fn or int8")
-    _want(codes, "quant pool: codes", codes.dtype, 6, codes.device)
-    _want(scales, "quant pool: scales", torch.float32, 5, codes.device)
-    if codes.shape[1] != 2 or codes.shape[:5] != scales.shape:
-        _bad(f"quant pool: codes {tuple(codes.shape)}, scales {tuple(scales.shape)}")
-    L, _, P, page, hkv, d = codes.shape
+    torch = _torch or _load_torch()
+    dtype, dev = codes.dtype, codes.get_device()
+    fmt = 1 if dtype is torch.float8_e4m3fn else 2 if dtype is torch.int8 else 0
+    if not fmt:
+        _bad(f"quant pool: codes of {dtype}, wanted float8_e4m3fn or int8")
+    L, two, P, page, hkv, d = shape = _whole(codes, "quant pool: codes", dtype, 6, dev)
+    if two != 2 or _whole(scales, "quant pool: scales", torch.float32, 5, dev) != shape[:5]:
+        _bad(f"quant pool: codes {tuple(shape)}, scales {tuple(scales.shape)}")
     return QuantPoolC(codes.data_ptr(), scales.data_ptr(), P, page, L, hkv, d, fmt)
 
 
-def _quant_call(name, codes, scales, layer, k, v, positions, block_tables, seq_ids, err, stream):
-    import torch
-    dev = codes.device
+def _quant_call(what, call, codes, scales, layer, k, v, positions, block_tables, seq_ids, err, stream):
     ps = quant_pool_struct(codes, scales)
-    T = positions.shape[0]
-    for t, what in ((k, "k"), (v, "v")):
-        _want(t, f"{name}: {what}", torch.bfloat16, 3, dev, whole=False)
-        if tuple(t.shape) != (T, ps.n_kv_heads, ps.head_dim) or T and t.stride(1) != ps.head_dim and t.shape[1] > 1:
-            _bad(f"{name}: {what} {tuple(t.shape)}, strides {tuple(t.stride())}")
-    _want(positions, f"{name}: positions", torch.int32, 1, dev)
-    _want(block_tables, f"{name}: block tables", torch.int32, 2, dev)
-    if seq_ids is not None and tuple(seq_ids.shape) != (T,):
-        _bad(f"{name}: {tuple(seq_ids.shape)} sequence ids of {T} tokens")
-    if T == 0:
-        return
-    row = ps.n_kv_heads * ps.head_dim           # (the stride of a single token says nothing)
-    ks, vs = (t.stride(0) if T > 1 else row for t in (k, v))
-    seq, e = _opt(seq_ids, f"{name}: sequence ids", torch.int32, 1, dev), _opt(err, f"{name}: err", torch.int32, 1, dev)
-    _device_call(dev, stream, lambda s: getattr(lib(), f"pallas_{name}")(
-        C.byref(ps), layer, T, seq, _ptr(positions), _ptr(k), ks, _ptr(v), vs, block_tables.shape[0],
-        _ptr(block_tables), block_tables.shape[1], e, s))
+    i32, dev = _torch.int32, codes.get_device()
+    T, = n = _whole(positions, what + ": positions", i32, 1, dev)
+    shape = (T, ps.n_kv_heads, ps.head_dim)
+    ks, vs = _packed_rows(k, what + ": k", dev, shape), _packed_rows(v, what + ": v", dev, shape)
+    seqs, pages = _whole(block_tables, what + ": block tables", i32, 2, dev)
+    if seq_ids is not None and _whole(seq_ids, what + ": sequence ids", i32, 1, dev) != n:
+        _bad(f"{what}: {seq_ids.shape[0]} sequence ids of {T} tokens")
+    if err is not None:
+        _whole(err, what + ": err", i32, 1, dev)
+    if T:
+        _launch(dev, stream, call, C.byref(ps), layer, T, _ptr(seq_ids), positions.data_ptr(), k.data_ptr(), ks,
+                v.data_ptr(), vs, seqs, block_tables.data_ptr(), pages, _ptr(err))
 
 
 def pallas_quant_store(codes, scales, layer: int, k, v, positions, block_tables, seq_ids=None, err=None, stream=None):
     """Quantises ``k``, ``v`` (bf16 [tokens, Hkv, d], any token stride) into a layer of the pool (quant_pool_struct)."""
-    _quant_call("quant_store", codes, scales, layer, k, v, positions, block_tables, seq_ids, err, stream)
+    _quant_call("quant store", lib().pallas_quant_store, codes, scales, layer, k, v, positions, block_tables, seq_ids,
+                err, stream)
 
 
 def pallas_quant_load(codes, scales, layer: int, k, v, positions, block_tables, seq_ids=None, err=None, stream=None):
     """Reads rows of a layer back into ``k``, ``v`` (bf16 [tokens, Hkv, d], any token stride)."""
-    _quant_call("quant_load", codes, scales, layer, k, v, positions, block_tables, seq_ids, err, stream)
+    _quant_call("quant load", lib().pallas_quant_load, codes, scales, layer, k, v, positions, block_tables, seq_ids, err,
+                stream)
 
 
 def pallas_attend_workspace_size(num_seqs: int, n_q_heads: int, n_kv_heads: int, head_dim: int, max_length: int) -> int:
     return int(lib().pallas_attend_workspace_size(num_seqs, n_q_heads, n_kv_heads, head_dim, max_length))
 
 
-def _attend_call(name, ps, dev, layer, q, lengths, max_length, block_tables, scale, out, workspace, lse, err, stream):
-    import torch
-    for t, what in ((q, "q"), (out, "out")):
-        _want(t, f"{name}: {what}", torch.bfloat16, 3, dev, whole=False)
-        if t.shape != q.shape or t.shape[2] != ps.head_dim or t.shape[1] > 1 and t.stride(1) != ps.head_dim:
-            _bad(f"{name}: {what} {tuple(t.shape)}, strides {tuple(t.stride())}")
-    S, H, d = q.shape
-    _want(lengths, f"{name}: lengths", torch.int32, 1, dev)
-    _want(block_tables, f"{name}: block tables", torch.int32, 2, dev)
-    if lengths.shape[0] != S or block_tables.shape[0] != S:
-        _bad(f"{name}: {S} queries, {lengths.shape[0]} lengths, {block_tables.shape[0]} tables")
-    if lse is not None and tuple(lse.shape) != (S, H):
-        _bad(f"{name}: lse {tuple(lse.shape)}")
-    if workspace.device != dev or not workspace.is_contiguous():
-        _bad(f"{name}: workspace")
-    qs, os = (t.stride(0) if S > 1 else H * d for t in (q, out))
-    ls, e = _opt(lse, f"{name}: lse", torch.float32, 2, dev), _opt(err, f"{name}: err", torch.int32, 1, dev)
-    _device_call(dev, stream, lambda s: getattr(lib(), f"pallas_{name}")(
-        C.byref(ps), layer, S, H, _ptr(q), qs, _ptr(lengths), max_length, _ptr(block_tables), block_tables.shape[1],
-        scale, _ptr(out), os, ls, _ptr(workspace), workspace.numel() * workspace.element_size(), e, s))
+def _attend_call(call, ps, dev, layer, q, lengths, max_length, block_tables, scale, out, workspace, lse, err, stream):
+    i32, shape = _torch.int32, q.shape
+    qs, os_ = _packed_rows(q, "attend: q", dev, shape), _packed_rows(out, "attend: out", dev, shape)
+    S, H, d = shape
+    seqs, pages = _whole(block_tables, "attend: block tables", i32, 2, dev)
+    if d != ps.head_dim or seqs != S or _whole(lengths, "attend: lengths", i32, 1, dev)[0] != S:
+        _bad(f"attend: {tuple(shape)} queries, {lengths.shape[0]} lengths, {seqs} tables, a pool of head_dim {ps.head_dim}")
+    if lse is not None and _whole(lse, "attend: lse", _torch.float32, 2, dev) != shape[:2]:
+        _bad(f"attend: lse {tuple(lse.shape)}")
+    if err is not None:
+        _whole(err, "attend: err", i32, 1, dev)
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        _bad("attend: workspace on another device, or not contiguous")
+    _launch(dev, stream, call, C.byref(ps), layer, S, H, q.data_ptr(), qs, lengths.data_ptr(), max_length,
+            block_tables.data_ptr(), pages, scale, out.data_ptr(), os_, _ptr(lse), workspace.data_ptr(), workspace.nbytes,
+            _ptr(err))
 
 
 def pallas_attend_kv(pool, layer: int, q, lengths, max_length: int, block_tables, scale: float, out, workspace, lse=None,
                      err=None, stream=None):
     """One new token per sequence: ``q``, ``out`` bf16 [num_seqs, Hq, d] (any row stride) over a bf16 pool."""
-    import torch
-    _want(pool, "attend_kv: pool", torch.bfloat16, 6, pool.device)
-    _attend_call("attend_kv", kv_pool_struct(pool), pool.device, layer, q, lengths, max_length, block_tables, scale, out,
+    dev = pool.get_device()
+    _whole(pool, "attend: pool", (_torch or _load_torch()).bfloat16, 6, dev)
+    _attend_call(lib().pallas_attend_kv, kv_pool_struct(pool), dev, layer, q, lengths, max_length, block_tables, scale, out,
                  workspace, lse, err, stream)
 
 
 def pallas_attend_quant(codes, scales, layer: int, q, lengths, max_length: int, block_tables, scale: float, out,
                         workspace, lse=None, err=None, stream=None):
     """The same over an 8-bit pool (quant_pool_struct)."""
-    _attend_call("attend_quant", quant_pool_struct(codes, scales), codes.device, layer, q, lengths, max_length,
-                 block_tables, scale, out, workspace, lse, err, stream)
+    _attend_call(lib().pallas_attend_quant, quant_pool_struct(codes, scales), codes.get_device(), layer, q, lengths,
+                 max_length, block_tables, scale, out, workspace, lse, err, stream)
 
 
 def _window_params(r_p, r_d, goodput, s_kv, t_load=0.0, t_0=0.0, alpha=0.8, t_max=5.0, dt=0.01):

@@ -122,6 +122,12 @@ __device__ __forceinline__ void write_row(const AttendParams& p, int s, int h, i
   if (i == 0 && p.lse) p.lse[int64_t(s) * p.Hq + h] = l == 0.f ? -INFINITY : (m + __log2f(l)) * 0.693147180559945309f;
 }
 
+// Weight, beside the maximum `top`, of a sum l of exponentials relative to m.  A part
+// without keys (m -infinity, l 0) has none; one of nothing but NaN keeps its NaN.
+__device__ __forceinline__ float join_weight(float m, float l, float top) {
+  return m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m - top);
+}
+
 // What a wave needs to load blocks of its split.
 struct Source {
   const char* k;        // layer planes, at this KV head
@@ -179,16 +185,33 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
   const int t = threadIdx.x, lane = t & 63;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int q4 = lane >> 4, l16 = lane & 15;
-  // Workgroups b, b + 8, .. share an L2: there the heads of one (split, sequence) follow
-  // each other, which share its table entries and the lines of its scales.
+  // Workgroups b, b + 8, .. go to one XCD and share an L2: there the heads of one
+  // (split, sequence) follow each other, which share its table entries and the lines of
+  // its scales.  The splits of a sequence go round the XCDs, which otherwise end up with
+  // unequal sequences: few sequences split by split, others a split of all of them at a
+  // time, each time turned so that a sequence moves on by one XCD; the last splits, which
+  // only long sequences have, first.
   const int heads = p.Hkv * groups;
   const int y = static_cast<int>(blockIdx.x) >> 3;
   const int item = y / heads * 8 + (blockIdx.x & 7);
   if (item >= items) return;
-  const int split = item / p.seqs, s = item - split * p.seqs;
+  int split, s;
+  if (p.seqs < 8) {
+    s = item / p.splits;
+    split = item - s * p.splits;
+  } else {
+    const int turn = item / p.seqs;
+    s = (item - turn * p.seqs + static_cast<int>(int64_t(turn) * ((p.seqs - 1) & 7) % p.seqs)) % p.seqs;
+    split = p.splits - 1 - turn;
+  }
   const int kh = (y % heads) / groups, group = (y % heads) % groups;
   const int G = p.Hq / p.Hkv;
   const int h0 = kh * G + group * kAttendGroup, nh = min(kAttendGroup, G - group * kAttendGroup);
+  // The split's table entries, one per lane.  Those of a split of the least length are
+  // read while the row's length is on its way: a short call is a chain of loads.
+  const int32_t* bt = p.bt + int64_t(s) * p.max_pages;
+  const int first = split * (kAttendMinSplit / kPage) + lane;
+  int entry = lane < kAttendMinSplit / kPage && first < p.max_pages ? bt[first] : -1;
   const int len = row_length(p, s), per = attend_split_keys(len, rows);
   if (split > 0 && int64_t(split) * per >= len) return;
   const int j0 = split * per;
@@ -199,11 +222,10 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
   src.page_bytes = int64_t(kPage) * src.rs;
   src.k = static_cast<const char*>(p.k) + int64_t(kh) * S::kRow;
   src.v = static_cast<const char*>(p.v) + int64_t(kh) * S::kRow;
-  src.entry = -1;
   {
     const bool page = lane * kPage < src.keys;
-    if (page) src.entry = p.bt[int64_t(s) * p.max_pages + j0 / kPage + lane];
-    if (src.entry < 0 || src.entry >= p.num_pages) src.entry = -1;
+    if (per != kAttendMinSplit && page) entry = bt[j0 / kPage + lane];
+    src.entry = page && entry >= 0 && entry < p.num_pages ? entry : -1;
     if (p.err && wave == 0 && kh == 0 && group == 0) {
       if (page && src.entry < 0) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
       if (split == 0 && lane == 0 && len != p.lengths[s]) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_LENGTH));
@@ -381,7 +403,7 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
     f32x4 o{};
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const float f = ml[w].x == -INFINITY ? (ml[w].y == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(ml[w].x - top);   // (all NaN: stays)
+      const float f = join_weight(ml[w].x, ml[w].y, top);
       l += f * ml[w].y;
       o += f * *reinterpret_cast<const f32x4*>(om + (w * kAttendGroup + g) * D + i);
     }
@@ -396,45 +418,65 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
 }
 
 // Joins a row's splits: one workgroup per (query head, sequence) that has several.
-// D / 4 lanes hold a record; as many records side by side as there are lanes for.
-constexpr int kJoinThreads = 256;
-template <int D>
-__global__ __launch_bounds__(kJoinThreads) void join_kernel(AttendParams p, int rows) {
-  constexpr int kLanes = D / 4, kSide = kJoinThreads / kLanes;
+// D / 4 lanes hold a record; a wave takes 256 / D records side by side and kJoinBatch of
+// those in flight.  The first are read before the row's length is known (any record of
+// the call may be read; those that the row does not have are left out), so a row whose
+// splits fit a wave's share costs one trip to memory.  A call whose rows all fit has one
+// wave per workgroup, others four; the further waves find no record of a row that fits,
+// and adding nothing changes no bit, so a row's result does not depend on which it is.
+constexpr int kJoinBatch = 8;
+template <int D, int kThreads>
+__global__ __launch_bounds__(kThreads) void join_kernel(AttendParams p, int rows) {
+  constexpr int kLanes = D / 4, kSide = kThreads / kLanes, kWaveSide = 64 / kLanes;
+  constexpr int kShare = kJoinBatch * kWaveSide, kRound = kThreads / 64 * kShare;
   const int h = blockIdx.x, s = blockIdx.y, t = threadIdx.x;
+  const int side = t / kLanes, i = (t % kLanes) * 4;
+  const int mine = t / 64 * kShare + side % kWaveSide;      // this lane's first record of a round
+  const int64_t rec = (int64_t(s) * p.Hq + h) * p.splits;
+  const f32x2* ml = reinterpret_cast<const f32x2*>(p.part_ml) + rec;
+  const float* po = p.part_o + rec * D + i;
+  f32x2 a[kJoinBatch];
+  f32x4 v[kJoinBatch];
+  auto read = [&](int k0) {
+#pragma unroll
+    for (int b = 0; b < kJoinBatch; ++b) {
+      const int k = min(k0 + b * kWaveSide + mine, p.splits - 1);
+      a[b] = ml[k];
+      v[b] = *reinterpret_cast<const f32x4*>(po + int64_t(k) * D);
+    }
+  };
+  read(0);
+#pragma unroll
+  for (int b = 0; b < kJoinBatch; ++b) asm volatile("" : "+v"(a[b]), "+v"(v[b]));
   const int len = row_length(p, s), per = attend_split_keys(len, rows);
   if (len <= per) return;
   const int n = static_cast<int>((int64_t(len) + per - 1) / per);
-  const int64_t rec = (int64_t(s) * p.Hq + h) * p.splits;
-  const f32x2* ml = reinterpret_cast<const f32x2*>(p.part_ml) + rec;
-  const int side = t / kLanes, i = (t % kLanes) * 4;
-  __shared__ float tops[kJoinThreads / 64], sums[kSide];
-  __shared__ f32x4 os[kSide][kLanes];
-  float top = -INFINITY;
-  for (int k = t; k < n; k += kJoinThreads) top = fmaxf(top, ml[k].x);
-  top = wave_max(top);
-  if ((t & 63) == 0) tops[t >> 6] = top;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kJoinThreads / 64; ++w) top = fmaxf(top, tops[w]);
-  float l = 0.f;
+  float m = -INFINITY, l = 0.f;
   f32x4 o{};
-#pragma unroll 4
-  for (int k = side; k < n; k += kSide) {
-    const f32x2 x = ml[k];
-    const float f = x.x == -INFINITY ? (x.y == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(x.x - top);
-    l += f * x.y;
-    o += f * *reinterpret_cast<const f32x4*>(p.part_o + (rec + k) * D + i);
+  auto add = [&](float mk, float lk, f32x4 ok) {
+    const float top = fmaxf(m, mk);
+    const float keep = join_weight(m, l, top), w = join_weight(mk, lk, top);
+    l = keep * l + w * lk;
+    o = keep * o + w * ok;
+    m = top;
+  };
+  for (int k0 = 0;;) {
+#pragma unroll
+    for (int b = 0; b < kJoinBatch; ++b)
+      if (k0 + b * kWaveSide + mine < n) add(a[b].x, a[b].y, v[b]);
+    k0 += kRound;
+    if (k0 >= n) break;
+    read(k0);
   }
+  __shared__ f32x2 mls[kSide];
+  __shared__ f32x4 os[kSide][kLanes];
   os[side][t % kLanes] = o;
-  if (t % kLanes == 0) sums[side] = l;
+  if (t % kLanes == 0) mls[side] = f32x2{m, l};
   __syncthreads();
   if (t >= kLanes) return;
-  for (int k = 1; k < kSide; ++k) {
-    l += sums[k];
-    o += os[k][t];
-  }
-  write_row(p, s, h, i, o, top, l);
+#pragma unroll
+  for (int k = 1; k < kSide; ++k) add(mls[k].x, mls[k].y, os[k][t]);
+  write_row(p, s, h, i, o, m, l);
 }
 
 template <int D, CacheType T>
@@ -445,7 +487,9 @@ hipError_t launch(const AttendParams& p, hipStream_t s) {
   const int64_t grid = (int64_t(items) + 7) / 8 * 8 * p.Hkv * groups;
   attend_kernel<D, T><<<static_cast<unsigned>(grid), Shape<D, T>::kWaves * 64, 0, s>>>(p, rows, items, groups);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  if (p.splits > 1) join_kernel<D><<<dim3(p.Hq, p.seqs), kJoinThreads, 0, s>>>(p, rows);
+  const dim3 joins(p.Hq, p.seqs);
+  if (p.splits > kJoinBatch * 256 / D) join_kernel<D, 256><<<joins, 256, 0, s>>>(p, rows);
+  else if (p.splits > 1) join_kernel<D, 64><<<joins, 64, 0, s>>>(p, rows);
   return hipGetLastError();
 }
 
