@@ -468,12 +468,14 @@ int pallas_quant_load(const pallas_quant_pool* pool, int32_t layer, int32_t num_
  * cache are joined.  A row without keys gives zeros and -infinity.
  *   head_dim 64 or 128 (UNSUPPORTED otherwise), page_size 16, any number of
  * query heads per KV head, num_seqs up to 65535, max_length (the longest length
- * the call can meet) at least 1 and at most max_pages * page_size.  A length
+ * the call can meet) at least 1 and at most max_pages * page_size; num_seqs *
+ * max_length up to 2^35 (UNSUPPORTED beyond).  A length
  * outside [0, max_length] is cut to it and raises PALLAS_DEVERR_LENGTH; keys on
  * pages outside [0, num_pages) are masked and raise PALLAS_DEVERR_PAGE, in *d_err
  * (nullable).  What is in slots behind a length has no effect.
- *   Scores, softmax statistics and sums are float32.  A row's results depend, to
- * the bit, on its own query, keys and length and on num_seqs and n_q_heads alone.
+ *   Scores, softmax statistics and sums are float32.  The work is divided by the
+ * lengths of the call, so a row's last bits follow them, not the other rows'
+ * queries or keys, nor max_length.  d_lengths may not change during the call.
  * The workspace (device, 256-byte aligned, pallas_attend_workspace_size bytes)
  * holds nothing between calls. */
 int pallas_attend_kv(const pallas_kv_pool* pool, int32_t layer, int32_t num_seqs, int32_t n_q_heads,

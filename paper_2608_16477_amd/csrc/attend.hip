@@ -1,21 +1,27 @@
 // Attention of one new token per sequence over a paged KV cache (bf16, E4M3 or
 // INT8 rows).
 //
-// A row's keys are cut into splits of a length that its own length and the call's
-// size give (attend_split_keys); a workgroup takes one split of one (sequence, KV head)
-// and up to 16 query heads that share it.  Its waves take equal runs of the split's
-// 32-key blocks, each an online softmax of its own; they are merged through LDS, and
-// the splits of a row, where it has several, by a second launch.  Every order is
-// fixed, nothing is counted or accumulated across workgroups.
+// The kernel is bound by the K/V stream, so the stream is what is divided: the 32-key
+// blocks of all sequences, one behind the other, are cut into ranges of equal length,
+// as many as waves are resident at once (attend_plan), and a wave takes a range of one
+// KV head and up to 16 query heads that share it.  It streams its blocks without a
+// pause, also where one sequence ends and the next begins, as an online softmax per
+// sequence, in registers; no wave waits for another.  What it has of a sequence that
+// lies in its range as a whole is the result, anything else a record, which a second
+// launch joins in order.  Ranges follow from the lengths alone and nothing is counted
+// or accumulated across waves.
+//   Against a workgroup per (split of a sequence, KV head), with splits sized by a row's
+// own length (the first form), us: 64 sequences of 500 to 8000 keys, E4M3, 64 / 8 heads,
+// 87 -> XX; 131,071 keys INT8 65 -> XX; 8 sequences bf16 32 -> XX.
 //
-// The kernel is bound by the K/V stream.  Each wave moves its own blocks from memory
-// straight into a private two-stage LDS ring, with the rows' scales.  Scores are
-// S^T = K Q^T with v_mfma_f32_16x16x32_bf16 (the query heads are the columns): lane l
-// holds keys 4 (l / 16) + r of head l mod 16.  O^T = V^T P^T takes those registers as
-// its B operand as they are, with V read transposed from LDS.  8-bit codes are turned
-// into bf16, which holds them exactly, between LDS and the MFMAs; a row's scale
-// multiplies the score of its key (K) or its weight (V), in float32.  Weights go into
-// the MFMA as two bf16 parts, 2^-17 of their value off: below what the sums lose.
+// Each wave moves its blocks from memory straight into a private two-stage LDS ring,
+// with the rows' scales.  Scores are S^T = K Q^T with v_mfma_f32_16x16x32_bf16 (the
+// query heads are the columns): lane l holds keys 4 (l / 16) + r of head l mod 16.
+// O^T = V^T P^T takes those registers as its B operand as they are, with V read
+// transposed from LDS.  8-bit codes are turned into bf16, which holds them exactly,
+// between LDS and the MFMAs; a row's scale multiplies the score of its key (K) or its
+// weight (V), in float32.  Weights go into the MFMA as two bf16 parts, 2^-17 of their
+// value off: below what the sums lose.
 #include "common.h"
 #include "kernels.h"
 #include "paged_attn.h"
@@ -27,6 +33,7 @@ namespace {
 constexpr int kPage = 16;
 constexpr int kBlk = 32;                 // keys per block: two pages
 constexpr int kStages = 2;               // blocks in flight per wave
+constexpr int kWaves = 4;                // per workgroup, each on its own
 constexpr int kBoundThreads = 512;       // (256 registers a wave, no accumulation registers)
 constexpr int kAuxStream = 2;            // nt: K and V are read once
 constexpr uint32_t kRsrcFlags = 0x00020000;
@@ -42,10 +49,9 @@ struct Shape {
   static constexpr int kScaleSlots = T == kCacheBf16 ? 0 : 16;   // 32 K scales, 32 V scales
   static constexpr int kSlots = 2 * kBlk * kCh + kScaleSlots;    // 16-byte slots of a stage
   static constexpr int kLoads = 4 * kPerPage + (T == kCacheBf16 ? 0 : 1);   // instructions per block
-  // bf16 rows of 128: two waves, so that two workgroups (128 KiB of ring) share a CU.
-  static constexpr int kWaves = kRow == 256 ? 2 : 4;
-  static constexpr int kRing = kWaves * kStages * kSlots;
-  static constexpr int kOut = kWaves * kAttendGroup * D / 4;     // the waves' outputs, over the ring
+  static constexpr int kRing = kStages * kSlots;                 // of a wave
+  // attend_plan counts on the waves that a CU's 160 KiB of LDS hold.
+  static_assert(160 * 1024 / (4 * kRing * 16) * 4 >= attend_waves(kRow), "resident waves");
 };
 
 // Chunk swizzles of 8-bit rows of CH chunks (8 rows of 128 bytes, or 16 of 64, fill the
@@ -128,30 +134,31 @@ __device__ __forceinline__ float join_weight(float m, float l, float top) {
   return m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m - top);
 }
 
-// What a wave needs to load blocks of its split.
+// A wave's range: what it takes to load its blocks.  Lane 2 i + h: half h (a page) of
+// block i of the range.
 struct Source {
   const char* k;        // layer planes, at this KV head
   const char* v;
   uint32_t rs;          // bytes between tokens of a page
   int64_t page_bytes;
-  int keys;             // keys of the split
-  int entry;            // lane: page of the split, or -1
+  int page;             // its page
+  int keys;             // keys in it, 0 for a page outside the pool
 };
 
-// Loads of block `blk` of the split into a stage: rows that exist, on pages of the
-// pool; everything else reads zeros.  Every wave issues the loads of every step, so
-// that those in flight can be counted.
+// Loads of block `i` of the range into a stage: rows that exist; everything else reads
+// zeros, as do blocks that are not `in` the range.  Every step issues its loads, so that
+// those in flight can be counted.
 template <int D, CacheType T>
 __device__ __forceinline__ void issue_block(const AttendParams& p, const Source& src, __amdgpu_buffer_rsrc_t scales, int kh,
-                                            int blk, bool in, const uint32_t* koff, const uint32_t* voff, u32x4* st) {
+                                            int i, bool in, const uint32_t* koff, const uint32_t* voff, u32x4* st) {
   using S = Shape<D, T>;
-  int pg[2];
+  int pg[2], nv[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    pg[h] = in ? __builtin_amdgcn_readlane(src.entry, blk * 2 + h) : -1;
-    const int nv = min(kPage, src.keys - (blk * kBlk + h * kPage));
-    const uint32_t range = pg[h] >= 0 && nv > 0 ? static_cast<uint32_t>(nv - 1) * src.rs + S::kRow : 0;
-    const int64_t base = max(pg[h], 0) * src.page_bytes;
+    pg[h] = __builtin_amdgcn_readlane(src.page, (i * 2 + h) & 63);
+    nv[h] = in ? __builtin_amdgcn_readlane(src.keys, (i * 2 + h) & 63) : 0;
+    const uint32_t range = nv[h] > 0 ? static_cast<uint32_t>(nv[h] - 1) * src.rs + S::kRow : 0;
+    const int64_t base = nv[h] > 0 ? pg[h] * src.page_bytes : 0;
     const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc((void*)(src.k + base), 0, range, kRsrcFlags);
     const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void*)(src.v + base), 0, range, kRsrcFlags);
 #pragma unroll
@@ -164,92 +171,66 @@ __device__ __forceinline__ void issue_block(const AttendParams& p, const Source&
   }
   if constexpr (T != kCacheBf16) {
     // Lane l: the K (below 32) or V scale of key l % 32.
-    const int lane = threadIdx.x & 63, key = lane & 31;
-    const int page = key < kPage ? pg[0] : pg[1];
-    const uint32_t row = (static_cast<uint32_t>(lane < 32 ? page : page + p.num_pages) * kPage + key % kPage) * p.Hkv + kh;
-    const bool live = page >= 0 && blk * kBlk + key < src.keys;
+    const int lane = threadIdx.x & 63, key = lane % kPage;
+    const bool second = lane & kPage;
+    const uint32_t page = second ? pg[1] : pg[0];
+    const uint32_t row = ((lane < 32 ? page : page + p.num_pages) * kPage + key) * p.Hkv + kh;
+    const bool live = key < (second ? nv[1] : nv[0]);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(scales, (lds_void*)(st + 2 * kBlk * S::kCh), 4, live ? row * 4 : kOutside, 0, 0, 0);
   }
 }
 
+// Lengths of 64 sequences from `at` on, one per lane, in 32-key blocks (0 behind the last).
+__device__ __forceinline__ int lane_length(const AttendParams& p, int at) {
+  const int s = at + static_cast<int>(threadIdx.x & 63);
+  return s < p.seqs ? row_length(p, s) : 0;
+}
+__device__ __forceinline__ int blocks_of(int len) { return (len + kBlk - 1) / kBlk; }
+
+__device__ __forceinline__ int wave_total(int v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
 template <int D, CacheType T>
-__global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, int rows, int items, int groups) {
+__global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, int groups) {
   using S = Shape<D, T>;
-  constexpr int CH = S::kCh, kWaves = S::kWaves, kThreads = kWaves * 64;
-  constexpr int DT = D / 16;
+  constexpr int CH = S::kCh, DT = D / 16;
   // One array: with several, the compiler's alias scopes make LDS reads of a
   // stage wait for the loads in flight into the other.
-  __shared__ __attribute__((aligned(256))) u32x4 lds[(S::kRing > S::kOut ? S::kRing : S::kOut) + kWaves * kAttendGroup / 2];
-  f32x2(*wave_ml)[kAttendGroup] = reinterpret_cast<f32x2(*)[kAttendGroup]>(lds + (S::kRing > S::kOut ? S::kRing : S::kOut));
+  __shared__ __attribute__((aligned(256))) u32x4 lds[kWaves * S::kRing];
 
   const int t = threadIdx.x, lane = t & 63;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int q4 = lane >> 4, l16 = lane & 15;
-  // Workgroups b, b + 8, .. go to one XCD and share an L2: there the heads of one
-  // (split, sequence) follow each other, which share its table entries and the lines of
-  // its scales.  The splits of a sequence go round the XCDs, which otherwise end up with
-  // unequal sequences: few sequences split by split, others a split of all of them at a
-  // time, each time turned so that a sequence moves on by one XCD; the last splits, which
-  // only long sequences have, first.
+  // Workgroups b, b + 8, .. go to one XCD and share an L2: there the heads of one range
+  // follow each other, which share its table entries and the lines of its scales.
   const int heads = p.Hkv * groups;
-  const int y = static_cast<int>(blockIdx.x) >> 3;
-  const int item = y / heads * 8 + (blockIdx.x & 7);
-  if (item >= items) return;
-  int split, s;
-  if (p.seqs < 8) {
-    s = item / p.splits;
-    split = item - s * p.splits;
-  } else {
-    const int turn = item / p.seqs;
-    s = (item - turn * p.seqs + static_cast<int>(int64_t(turn) * ((p.seqs - 1) & 7) % p.seqs)) % p.seqs;
-    split = p.splits - 1 - turn;
-  }
-  const int kh = (y % heads) / groups, group = (y % heads) % groups;
+  const int worker = static_cast<int>(blockIdx.x >> 3) * kWaves + wave;
+  const int kh = worker % heads / groups, group = worker % heads % groups;
+  const int r0 = worker / heads * 8 + (blockIdx.x & 7);
+  if (r0 >= p.ranges) return;
+
+  // All blocks of the call, and the ranges they make.
+  int lens = lane_length(p, 0);
+  int total = wave_total(blocks_of(lens));
+  for (int at = 64; at < p.seqs; at += 64) total += wave_total(blocks_of(lane_length(p, at)));
+  total = __builtin_amdgcn_readfirstlane(total);
+  const int each = attend_blocks(total, p.ranges);
+  if (p.err && r0 == 0 && worker == 0)
+    for (int s = lane; s < p.seqs; s += 64)
+      if (row_length(p, s) != p.lengths[s]) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_LENGTH));
+
   const int G = p.Hq / p.Hkv;
   const int h0 = kh * G + group * kAttendGroup, nh = min(kAttendGroup, G - group * kAttendGroup);
-  // The split's table entries, one per lane.  Those of a split of the least length are
-  // read while the row's length is on its way: a short call is a chain of loads.
-  const int32_t* bt = p.bt + int64_t(s) * p.max_pages;
-  const int first = split * (kAttendMinSplit / kPage) + lane;
-  int entry = lane < kAttendMinSplit / kPage && first < p.max_pages ? bt[first] : -1;
-  const int len = row_length(p, s), per = attend_split_keys(len, rows);
-  if (split > 0 && int64_t(split) * per >= len) return;
-  const int j0 = split * per;
-
   Source src;
-  src.keys = min(len - j0, per);
   src.rs = static_cast<uint32_t>(p.Hkv) * S::kRow;
   src.page_bytes = int64_t(kPage) * src.rs;
   src.k = static_cast<const char*>(p.k) + int64_t(kh) * S::kRow;
   src.v = static_cast<const char*>(p.v) + int64_t(kh) * S::kRow;
-  {
-    const bool page = lane * kPage < src.keys;
-    if (per != kAttendMinSplit && page) entry = bt[j0 / kPage + lane];
-    src.entry = page && entry >= 0 && entry < p.num_pages ? entry : -1;
-    if (p.err && wave == 0 && kh == 0 && group == 0) {
-      if (page && src.entry < 0) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
-      if (split == 0 && lane == 0 && len != p.lengths[s]) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_LENGTH));
-    }
-  }
-  // Q: the MFMA's B operand, column l16 = a head (repeated where there are fewer).  Its
-  // dimensions follow what a lane reads of K: bf16, chunk 4 kk + q4; 8 bits, half kk % 2
-  // of chunk 4 (kk / 2) + q4.
-  u32x4 qf[D / 32];
-  {
-    const uint16_t* q = p.q + s * p.q_stride + int64_t(h0 + l16 % nh) * D;
-#pragma unroll
-    for (int kk = 0; kk < D / 32; ++kk)
-      qf[kk] = *reinterpret_cast<const u32x4*>(q + (T == kCacheBf16 ? 32 * kk + 8 * q4 : 64 * (kk / 2) + 16 * q4 + 8 * (kk % 2)));
-  }
-  // Loaded, and waited for, before the K/V stream (loads return in order).
-#pragma unroll
-  for (int kk = 0; kk < D / 32; ++kk) asm volatile("" : "+v"(qf[kk]));
-  asm volatile("" : "+v"(src.entry));
-
-  const int blocks = (src.keys + kBlk - 1) / kBlk, each = (blocks + kWaves - 1) / kWaves;
-  const int blk0 = wave * each, blk1 = min(blk0 + each, blocks);
-  u32x4* const ring = lds + wave * kStages * S::kSlots;
-  __amdgpu_buffer_rsrc_t scales = __builtin_amdgcn_make_buffer_rsrc(
+  u32x4* const ring = lds + wave * S::kRing;
+  const __amdgpu_buffer_rsrc_t scales = __builtin_amdgcn_make_buffer_rsrc(
       (void*)p.scales, 0, static_cast<uint32_t>(p.num_pages) * (2 * kPage * 4) * p.Hkv, kRsrcFlags);
   // Byte offset in a page of what this lane loads in instruction v of it.
   uint32_t koff[S::kPerPage], voff[2 * S::kPerPage];
@@ -260,10 +241,6 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
     voff[v] = r * src.rs + static_cast<uint32_t>((c ^ v_slot<T, CH>(r)) * 16);
     voff[S::kPerPage + v] = r * src.rs + static_cast<uint32_t>((c ^ v_slot<T, CH>(kPage + r)) * 16);
   }
-#pragma unroll
-  for (int i = 0; i < kStages; ++i)
-    issue_block<D, T>(p, src, scales, kh, blk0 + i, blk0 + i < blk1, koff, voff, ring + i * S::kSlots);
-
   // Where this lane reads: a K block at (row l16, chunk q4), a V block transposed.
   const uint32_t kb0 = static_cast<uint32_t>(l16 * CH + (q4 ^ k_slot<T, CH>(l16)));
   uint32_t vb0;
@@ -275,13 +252,87 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
     vb0 = static_cast<uint32_t>(key * D + v_slot<T, CH>(key) * 16 + (l16 & 1) * 8);
   }
 
+  int win = 0;                                  // lens: of sequences [win, win + 64)
+  auto length = [&](int s) {
+    if (s >= win + 64) lens = lane_length(p, win = s & ~63);
+    return __builtin_amdgcn_readlane(lens, s & 63);
+  };
+  int s = 0, base = 0;                          // a sequence, and the blocks before it
+  for (int r = r0; int64_t(r) * each < total; r += p.ranges) {
+  const int f0 = r * each, f1 = min(f0 + each, total);
+  // The sequence of the range's first block: whole windows, then in one.
+  while (s < p.seqs) {
+    if (s >= win + 64) lens = lane_length(p, win = s & ~63);
+    const int nb = lane >= (s & 63) ? blocks_of(lens) : 0;
+    int sum = nb;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int up = __shfl_up(sum, o, 64);
+      sum += lane >= o ? up : 0;
+    }
+    const uint64_t behind = __builtin_amdgcn_ballot_w64(base + sum > f0);
+    if (behind != 0) {
+      const int first = __builtin_ctzll(behind);
+      base += __builtin_amdgcn_readlane(sum, first) - __builtin_amdgcn_readlane(nb, first);
+      s = win + first;
+      break;
+    }
+    base += __builtin_amdgcn_readlane(sum, 63);
+    s = win + 64;
+  }
+  // Pages of its blocks.
+  src.page = 0;
+  src.keys = 0;
+  {
+    const int f = f0 + lane / 2;
+    int from = 0, key0 = -1;
+    for (int n = s, at = base; at < f1 && n < p.seqs; ++n) {
+      const int len = length(n), nb = blocks_of(len);
+      if (f >= at && f < at + nb && f < f1) {
+        from = n;
+        key0 = ((f - at) * 2 + lane % 2) * kPage;
+        src.keys = min(max(len - key0, 0), kPage);
+      }
+      at += nb;
+    }
+    if (src.keys > 0) {
+      src.page = p.bt[int64_t(from) * p.max_pages + key0 / kPage];
+      if (src.page < 0 || src.page >= p.num_pages) {
+        src.page = src.keys = 0;
+        if (p.err && kh == 0 && group == 0) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
+      }
+    }
+    if (s < win) lens = lane_length(p, win = s & ~63);
+  }
+  const int blocks = f1 - f0;
+#pragma unroll
+  for (int i = 0; i < kStages; ++i) issue_block<D, T>(p, src, scales, kh, i, i < blocks, koff, voff, ring + i * S::kSlots);
+
+  int i = 0;
+  while (i < blocks && s < p.seqs) {
+  const int nb = blocks_of(length(s));
+  if (nb == 0) {
+    ++s;
+    continue;
+  }
+  const int begin = f0 + i - base, stop = min(blocks, base + nb - f0);    // its block at i; where it or the range ends
+  // Q: the MFMA's B operand, column l16 = a head (repeated where there are fewer).  Its
+  // dimensions follow what a lane reads of K: bf16, chunk 4 kk + q4; 8 bits, half kk % 2
+  // of chunk 4 (kk / 2) + q4.
+  u32x4 qf[D / 32];
+  {
+    const uint16_t* q = p.q + s * p.q_stride + int64_t(h0 + l16 % nh) * D;
+#pragma unroll
+    for (int kk = 0; kk < D / 32; ++kk)
+      qf[kk] = *reinterpret_cast<const u32x4*>(q + (T == kCacheBf16 ? 32 * kk + 8 * q4 : 64 * (kk / 2) + 16 * q4 + 8 * (kk % 2)));
+  }
   f32x4 acc[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) acc[dt] = f32x4{};
   float m = -INFINITY, lsum = 0.f;
 #pragma unroll 1
-  for (int blk = blk0; blk < blk1; ++blk) {
-    u32x4* const Kst = ring + (static_cast<unsigned>(blk - blk0) % kStages) * S::kSlots;
+  for (; i < stop; ++i) {
+    u32x4* const Kst = ring + (static_cast<unsigned>(i) % kStages) * S::kSlots;
     u32x4* const Vst = Kst + kBlk * CH;
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kStages - 1) * S::kLoads) : "memory");   // this block is here
     f32x4 sc[2] = {f32x4{}, f32x4{}};
@@ -319,14 +370,14 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
         }
       }
     }
-    const int pg0 = __builtin_amdgcn_readlane(src.entry, blk * 2), pg1 = __builtin_amdgcn_readlane(src.entry, blk * 2 + 1);
-    if (src.keys - blk * kBlk < kBlk || pg0 < 0 || pg1 < 0) {
+    const int nv0 = __builtin_amdgcn_readlane(src.keys, i * 2), nv1 = __builtin_amdgcn_readlane(src.keys, i * 2 + 1);
+    if (nv0 < kPage || nv1 < kPage) {
       // Keys past the end, and keys on a page outside the pool.
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (blk * kBlk + h * kPage + 4 * q4 + r >= src.keys || (h ? pg1 : pg0) < 0) pr[h * 4 + r] = -INFINITY;
+        for (int e = 0; e < 4; ++e)
+          if (4 * q4 + e >= (h ? nv1 : nv0)) pr[h * 4 + e] = -INFINITY;
     }
     float mx = fmaxf(fmaxf(fmaxf(pr[0], pr[1]), fmaxf(pr[2], pr[3])), fmaxf(fmaxf(pr[4], pr[5]), fmaxf(pr[6], pr[7])));
     mx = rows_max(mx);
@@ -375,82 +426,59 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
       }
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this block's LDS reads are done
-    issue_block<D, T>(p, src, scales, kh, blk + kStages, blk + kStages < blk1, koff, voff, Kst);
+    issue_block<D, T>(p, src, scales, kh, i + kStages, i + kStages < blocks, koff, voff, Kst);
   }
 
-  // Merge the waves through LDS (the ring is free once all are here and nothing is in
-  // flight): om[wave][head][dim].
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-  float* om = reinterpret_cast<float*>(lds);
+  // Lane: dimensions 16 dt + 4 q4 .. + 3 of head l16.
   lsum = rows_sum(lsum);
+  const bool whole = begin == 0 && base + nb <= f1;
   if (l16 < nh) {
-    float* dst = om + (wave * kAttendGroup + l16) * D + 4 * q4;
+    if (whole) {
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(dst + dt * 16) = acc[dt];
-    if (q4 == 0) wave_ml[wave][l16] = f32x2{m, lsum};
-  }
-  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-  for (int e = t; e < nh * D / 4; e += kThreads) {
-    const int g = e / (D / 4), i = (e % (D / 4)) * 4;
-    f32x2 ml[kWaves];
-    float top = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      ml[w] = wave_ml[w][g];
-      top = fmaxf(top, ml[w].x);
-    }
-    float l = 0.f;
-    f32x4 o{};
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float f = join_weight(ml[w].x, ml[w].y, top);
-      l += f * ml[w].y;
-      o += f * *reinterpret_cast<const f32x4*>(om + (w * kAttendGroup + g) * D + i);
-    }
-    if (len <= per) {
-      write_row(p, s, h0 + g, i, o, top, l);
+      for (int dt = 0; dt < DT; ++dt) write_row(p, s, h0 + l16, 16 * dt + 4 * q4, acc[dt], m, lsum);
     } else {
-      const int64_t rec = (int64_t(s) * p.Hq + h0 + g) * p.splits + split;
-      *reinterpret_cast<f32x4*>(p.part_o + rec * D + i) = o;
-      if (i == 0) *reinterpret_cast<f32x2*>(p.part_ml + rec * 2) = f32x2{top, l};
+      // Ranges and sequences advance together, so r + s numbers the records.
+      const int64_t rec = (int64_t(r) + s) * p.Hq + h0 + l16;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(p.part_o + rec * D + 16 * dt + 4 * q4) = acc[dt];
+      if (q4 == 0) *reinterpret_cast<f32x2*>(p.part_ml + rec * 2) = f32x2{m, lsum};
     }
   }
+  if (begin == 0 && kh == 0 && group == 0 && lane == 0) {
+    // The row's records: none, or from here to the range of its last block.
+    p.parts[2 * s] = r;
+    p.parts[2 * s + 1] = whole ? 0 : (base + nb - 1) / each - r + 1;
+  }
+  if (base + nb > f1) break;                    // the rest is the next range's
+  base += nb;
+  ++s;
+  }
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load into LDS outlives its wave
 }
 
-// Joins a row's splits: one workgroup per (query head, sequence) that has several.
-// D / 4 lanes hold a record; a wave takes 256 / D records side by side and kJoinBatch of
-// those in flight.  The first are read before the row's length is known (any record of
-// the call may be read; those that the row does not have are left out), so a row whose
-// splits fit a wave's share costs one trip to memory.  A call whose rows all fit has one
-// wave per workgroup, others four; the further waves find no record of a row that fits,
-// and adding nothing changes no bit, so a row's result does not depend on which it is.
+// Joins a row's records: one workgroup per (query head, sequence).  D / 4 lanes hold a
+// record; a wave takes 256 / D records side by side and kJoinBatch of those in flight.
+// Rows without a key get their zeros here.
 constexpr int kJoinBatch = 8;
 template <int D, int kThreads>
-__global__ __launch_bounds__(kThreads) void join_kernel(AttendParams p, int rows) {
+__global__ __launch_bounds__(kThreads) void join_kernel(AttendParams p) {
   constexpr int kLanes = D / 4, kSide = kThreads / kLanes, kWaveSide = 64 / kLanes;
   constexpr int kShare = kJoinBatch * kWaveSide, kRound = kThreads / 64 * kShare;
   const int h = blockIdx.x, s = blockIdx.y, t = threadIdx.x;
   const int side = t / kLanes, i = (t % kLanes) * 4;
   const int mine = t / 64 * kShare + side % kWaveSide;      // this lane's first record of a round
-  const int64_t rec = (int64_t(s) * p.Hq + h) * p.splits;
-  const f32x2* ml = reinterpret_cast<const f32x2*>(p.part_ml) + rec;
-  const float* po = p.part_o + rec * D + i;
-  f32x2 a[kJoinBatch];
-  f32x4 v[kJoinBatch];
-  auto read = [&](int k0) {
-#pragma unroll
-    for (int b = 0; b < kJoinBatch; ++b) {
-      const int k = min(k0 + b * kWaveSide + mine, p.splits - 1);
-      a[b] = ml[k];
-      v[b] = *reinterpret_cast<const f32x4*>(po + int64_t(k) * D);
-    }
-  };
-  read(0);
-#pragma unroll
-  for (int b = 0; b < kJoinBatch; ++b) asm volatile("" : "+v"(a[b]), "+v"(v[b]));
-  const int len = row_length(p, s), per = attend_split_keys(len, rows);
-  if (len <= per) return;
-  const int n = static_cast<int>((int64_t(len) + per - 1) / per);
+  // (Within the records whatever is read: lengths that change during a call give a wrong
+  // result, but nothing else.)
+  const int first = min(max(p.parts[2 * s], 0), p.records - 1 - s);
+  const int n = min(p.parts[2 * s + 1], p.records - s - first);
+  if (row_length(p, s) == 0) {
+    if (t < kLanes) write_row(p, s, h, i, f32x4{}, -INFINITY, 0.f);
+    return;
+  }
+  if (n <= 0) return;
+  const f32x2* ml = reinterpret_cast<const f32x2*>(p.part_ml) + (int64_t(first) + s) * p.Hq + h;
+  const float* po = p.part_o + ((int64_t(first) + s) * p.Hq + h) * D + i;
   float m = -INFINITY, l = 0.f;
   f32x4 o{};
   auto add = [&](float mk, float lk, f32x4 ok) {
@@ -460,13 +488,18 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendParams p, int rows
     o = keep * o + w * ok;
     m = top;
   };
-  for (int k0 = 0;;) {
+  for (int k0 = 0; k0 < n; k0 += kRound) {
+    f32x2 a[kJoinBatch];
+    f32x4 v[kJoinBatch];
+#pragma unroll
+    for (int b = 0; b < kJoinBatch; ++b) {
+      const int64_t k = min(k0 + b * kWaveSide + mine, n - 1);
+      a[b] = ml[k * p.Hq];
+      v[b] = *reinterpret_cast<const f32x4*>(po + k * p.Hq * D);
+    }
 #pragma unroll
     for (int b = 0; b < kJoinBatch; ++b)
       if (k0 + b * kWaveSide + mine < n) add(a[b].x, a[b].y, v[b]);
-    k0 += kRound;
-    if (k0 >= n) break;
-    read(k0);
   }
   __shared__ f32x2 mls[kSide];
   __shared__ f32x4 os[kSide][kLanes];
@@ -482,14 +515,14 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendParams p, int rows
 template <int D, CacheType T>
 hipError_t launch(const AttendParams& p, hipStream_t s) {
   const int groups = (p.Hq / p.Hkv + kAttendGroup - 1) / kAttendGroup;
-  const int rows = static_cast<int>(attend_rows(p.seqs, p.Hq, p.Hkv));
-  const int items = p.splits * p.seqs;
-  const int64_t grid = (int64_t(items) + 7) / 8 * 8 * p.Hkv * groups;
-  attend_kernel<D, T><<<static_cast<unsigned>(grid), Shape<D, T>::kWaves * 64, 0, s>>>(p, rows, items, groups);
+  const int64_t workers = int64_t(p.ranges) / 8 * p.Hkv * groups;          // on each XCD
+  const unsigned grid = static_cast<unsigned>((workers + kWaves - 1) / kWaves * 8);
+  attend_kernel<D, T><<<grid, kWaves * 64, 0, s>>>(p, groups);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   const dim3 joins(p.Hq, p.seqs);
-  if (p.splits > kJoinBatch * 256 / D) join_kernel<D, 256><<<joins, 256, 0, s>>>(p, rows);
-  else if (p.splits > 1) join_kernel<D, 64><<<joins, 64, 0, s>>>(p, rows);
+  // One wave where a row of an even batch has no more records than its share.
+  if (p.ranges / p.seqs >= kJoinBatch * 256 / D) join_kernel<D, 256><<<joins, 256, 0, s>>>(p);
+  else join_kernel<D, 64><<<joins, 64, 0, s>>>(p);
   return hipGetLastError();
 }
 

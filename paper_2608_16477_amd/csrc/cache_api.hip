@@ -87,17 +87,18 @@ int quant_call(bool store, const pallas_quant_pool* pool, int32_t layer, int32_t
   return launched(pallas::launch_quant_load(p, s), "quant load launch");
 }
 
-// Records of a call in its workspace: d + 2 floats for each of a row's query heads.
+// A call's workspace: two ints per sequence, then records of d + 2 floats per query head.
+// `ranges`: of the call, or the most of any cache type.
 struct AttendSpace {
-  size_t o_floats, bytes;
+  int records;
+  size_t o_at, ml_at, bytes;
 };
-AttendSpace attend_space(int64_t seqs, int Hq, int Hkv, int d, int max_length) {
-  const int64_t rows = pallas::attend_rows(seqs, Hq, Hkv);
-  const size_t heads = std::min(Hq / Hkv, pallas::kAttendGroup);
-  const size_t records = pallas::attend_records(max_length, rows) * heads;
-  const size_t o = (records * d + 63) / 64 * 64;
-  return {o, (o + records * 2 + 63) / 64 * 256};
+AttendSpace attend_space(int64_t seqs, int Hq, int d, int max_length, int ranges) {
+  const int64_t records = pallas::attend_records(seqs, max_length, ranges);
+  const size_t o_at = (seqs * 8 + 255) / 256 * 256, ml_at = o_at + size_t(records) * Hq * d * 4;
+  return {int(records), o_at, ml_at, (ml_at + size_t(records) * Hq * 8 + 255) / 256 * 256};
 }
+int most_ranges(int Hq, int Hkv, int d) { return pallas::attend_ranges(d, pallas::attend_heads(Hq, Hkv)); }
 
 int check_attend(int32_t num_seqs, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_length,
                  const char* what) {
@@ -110,9 +111,8 @@ int check_attend(int32_t num_seqs, int32_t n_q_heads, int32_t n_kv_heads, int32_
   if (num_seqs > 65535 || n_q_heads > 4096)
     return fail(PALLAS_ERR_UNSUPPORTED, "%s: %d sequences (at most 65535), %d query heads (at most 4096)", what, num_seqs,
                 n_q_heads);
-  const int64_t rows = pallas::attend_rows(num_seqs, n_q_heads, n_kv_heads);
-  if (rows * pallas::attend_splits(max_length, rows) > (int64_t(1) << 30))
-    return fail(PALLAS_ERR_UNSUPPORTED, "%s: %d sequences of up to %d keys make too many splits", what, num_seqs, max_length);
+  if (pallas::attend_total(num_seqs, max_length) > (int64_t(1) << 30))
+    return fail(PALLAS_ERR_UNSUPPORTED, "%s: %d sequences of up to %d keys (at most 2^35 in all)", what, num_seqs, max_length);
   return PALLAS_OK;
 }
 
@@ -137,7 +137,7 @@ int attend_call(const char* what, pallas::CacheType type, pallas::AttendParams& 
   if (!std::isfinite(scale)) return fail(PALLAS_ERR_INVALID_ARG, "%s: scale is not finite", what);
   if (!d_workspace || !aligned(d_workspace, 256))
     return fail(PALLAS_ERR_INVALID_ARG, "%s: workspace null or not 256-byte aligned", what);
-  const AttendSpace sp = attend_space(num_seqs, n_q_heads, p.Hkv, p.d, max_length);
+  const AttendSpace sp = attend_space(num_seqs, n_q_heads, p.d, max_length, most_ranges(n_q_heads, p.Hkv, p.d));
   if (ws_bytes < sp.bytes)
     return fail(PALLAS_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", what, ws_bytes, sp.bytes);
   p.Hq = n_q_heads;
@@ -152,9 +152,12 @@ int attend_call(const char* what, pallas::CacheType type, pallas::AttendParams& 
   p.out = static_cast<uint16_t*>(d_out);
   p.out_stride = out_stride;
   p.lse = d_lse;
-  p.splits = pallas::attend_splits(max_length, pallas::attend_rows(num_seqs, n_q_heads, p.Hkv));
-  p.part_o = static_cast<float*>(d_workspace);
-  p.part_ml = p.part_o + sp.o_floats;
+  p.ranges = pallas::attend_ranges(type == pallas::kCacheBf16 ? 2 * p.d : p.d, pallas::attend_heads(n_q_heads, p.Hkv));
+  p.records = sp.records;
+  char* ws = static_cast<char*>(d_workspace);
+  p.parts = reinterpret_cast<int32_t*>(ws);
+  p.part_o = reinterpret_cast<float*>(ws + sp.o_at);
+  p.part_ml = reinterpret_cast<float*>(ws + sp.ml_at);
   p.err = d_err;
   hipStream_t s = static_cast<hipStream_t>(stream);
   pallas::ProfScope ps(PALLAS_K_DECODE_ATTN, s);
@@ -320,7 +323,7 @@ int pallas_attend_quant(const pallas_quant_pool* pool, int32_t layer, int32_t nu
 size_t pallas_attend_workspace_size(int32_t num_seqs, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                                     int32_t max_length) {
   if (check_attend(num_seqs, n_q_heads, n_kv_heads, head_dim, max_length, "attend workspace") != PALLAS_OK) return 0;
-  return attend_space(num_seqs, n_q_heads, n_kv_heads, head_dim, max_length).bytes;
+  return attend_space(num_seqs, n_q_heads, head_dim, max_length, most_ranges(n_q_heads, n_kv_heads, head_dim)).bytes;
 }
 
 }  // extern "C"

@@ -405,39 +405,43 @@ struct AttendParams {
   uint16_t* out;
   int64_t out_stride;
   float* lse;              // [seqs][Hq] or null
-  int splits;              // records per row: attend_splits
-  float* part_o;           // [seqs][Hq][splits][d]
-  float* part_ml;          // [seqs][Hq][splits][2]
+  int ranges;              // attend_ranges
+  int records;             // attend_records
+  int32_t* parts;          // [seqs][2]: a row's first range and records (0: written as a whole)
+  float* part_o;           // [attend_records][Hq][d]
+  float* part_ml;          // [attend_records][Hq][2]
   int32_t* err;
 };
-// A row's keys are cut into splits of a length that follows from its own length
-// and the number of (sequence, head group) rows of the call.
-constexpr int kAttendMinSplit = 128;
-constexpr int kAttendMaxSplit = 1024;
-constexpr int kAttendTarget = 1024;      // workgroups that fill the chip
+constexpr int kAttendBlock = 32;         // keys per block
 constexpr int kAttendGroup = 16;         // query heads that share one pass over a KV head
-__host__ __device__ inline int attend_split_keys(int len, int rows) {
-  const int64_t want = (int64_t(len) * rows + kAttendTarget - 1) / kAttendTarget;
-  if (want >= kAttendMaxSplit) return kAttendMaxSplit;
-  return want <= kAttendMinSplit ? kAttendMinSplit : (int(want) + kAttendMinSplit - 1) / kAttendMinSplit * kAttendMinSplit;
+// Blocks of a wave's range: both of its ring stages at least, and at most one per pair of
+// lanes.
+constexpr int kAttendMinBlocks = 2;
+constexpr int kAttendMaxBlocks = 32;
+// Waves that a CU holds, by the bytes of a head row: each has a ring of two stages of 32
+// K and V rows, 128 KiB in all.
+constexpr int attend_waves(int row_bytes) { return 1024 / row_bytes; }
+// Ranges that run at once: a multiple of 8 (one XCD each in turn), at least 8.
+inline int attend_ranges(int row_bytes, int64_t heads) {
+  return int(std::max<int64_t>(256 * attend_waves(row_bytes) / heads / 8 * 8, 8));
 }
-inline int64_t attend_rows(int64_t seqs, int Hq, int Hkv) {
-  return seqs * Hkv * ((Hq / Hkv + kAttendGroup - 1) / kAttendGroup);
+// KV heads, times the passes over each.
+inline int64_t attend_heads(int Hq, int Hkv) { return int64_t(Hkv) * ((Hq / Hkv + kAttendGroup - 1) / kAttendGroup); }
+// Blocks per range of a call of `total` blocks: as few rounds of the ranges as the
+// largest one allows, all rounds full.
+__host__ __device__ inline int attend_blocks(int total, int ranges) {
+  const int rounds = std::max(int((int64_t(total) + int64_t(kAttendMaxBlocks) * ranges - 1) / (int64_t(kAttendMaxBlocks) * ranges)), 1);
+  const int64_t all = int64_t(rounds) * ranges;
+  return std::max(int((total + all - 1) / all), kAttendMinBlocks);
 }
-// The most splits a row of up to max_length keys has: attend_split_keys >=
-// len * rows / kAttendTarget unless it is the largest, so len / split <= target / rows.
-inline int attend_splits(int max_length, int64_t rows) {
-  const int64_t by_min = (int64_t(max_length) + kAttendMinSplit - 1) / kAttendMinSplit;
-  const int64_t by_max = (int64_t(max_length) + kAttendMaxSplit - 1) / kAttendMaxSplit;
-  const int64_t by_target = (kAttendTarget + rows - 1) / rows;
-  return int(std::min(by_min, std::max(by_max, by_target)));
+// Bound on (range, sequence) pairs of a call, which grows with seqs and max_length:
+// ranges * rounds <= ranges + total / 32, and no range is below the least length.
+inline int64_t attend_total(int64_t seqs, int max_length) {
+  return seqs * ((int64_t(max_length) + kAttendBlock - 1) / kAttendBlock);
 }
-// Records of a call, bounded by something that grows with seqs and max_length
-// (rows * attend_splits does not: ceil(target / rows) falls in steps).
-inline size_t attend_records(int max_length, int64_t rows) {
-  const int64_t by_min = (int64_t(max_length) + kAttendMinSplit - 1) / kAttendMinSplit;
-  const int64_t by_max = (int64_t(max_length) + kAttendMaxSplit - 1) / kAttendMaxSplit;
-  return size_t(std::max(rows * by_max, std::min(rows * by_min, rows + kAttendTarget)));
+inline int64_t attend_records(int64_t seqs, int max_length, int ranges) {
+  const int64_t total = attend_total(seqs, max_length);
+  return std::min((total + kAttendMinBlocks - 1) / kAttendMinBlocks, ranges + total / kAttendMaxBlocks) + seqs;
 }
 hipError_t launch_attend(const AttendParams& p, CacheType type, hipStream_t s);
 

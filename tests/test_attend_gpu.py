@@ -129,6 +129,9 @@ CASES = [
     (128, 7, 5, [1025, 12, 96]),
     (128, 8, 8, [9001]),
     (64, 4, 16, [97 * i for i in range(33)]),
+    (128, 2, 4, [0] * 70 + [33] + [0] * 64 + [1, 500] + [0] * 30),   # few keys in many rows
+    (64, 1, 2, [1 + i % 3 for i in range(300)]),                     # a block a row
+    (128, 4, 2, [0, 0, 0]),
 ]
 
 
@@ -147,6 +150,54 @@ def test_against_oracle(P, d, group, hkv, lens, fmt):
     bt = torch.full((len(lens), cache.max_pages + 300), -1, dtype=torch.int32, device=DEV)
     bt[:, :cache.max_pages] = cache.bt
     assert torch.equal(cache.attend(P, q, scale, max_length=max(lens) + 4000, bt=bt), out)
+
+
+@pytest.mark.parametrize("fmt,d,hkv,n", [("bf16", 128, 2, 400000), ("e4m3", 64, 32, 100000), ("int8", 128, 16, 100000)])
+def test_more_blocks_than_one_round(P, fmt, d, hkv, n):
+    """Ranges at their longest, several of them a wave: against torch in float64 on the GPU, head by head."""
+    lens = [n, 0, 777, n // 2]
+    pages = [(x + 15) // 16 for x in lens]
+    rng = np.random.default_rng(3)
+    spare = 50
+    bt = np.full((4, max(pages)), -1, dtype=np.int32)
+    for i, x in enumerate(pages):       # the rows share the pool's pages
+        bt[i, :x] = rng.permutation(max(pages) + spare)[:x]
+    bt = torch.from_numpy(bt).to(DEV)
+    g = torch.Generator(DEV).manual_seed(1)
+    shape = (1, 2, max(pages) + spare, 16, hkv, d)
+    q = queries(4, hkv, d, 4)
+    lengths = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    out, lse = torch.empty_like(q), torch.empty((4, hkv), dtype=torch.float32, device=DEV)
+    ws = torch.empty(P.pallas_attend_workspace_size(4, hkv, hkv, d, n), dtype=torch.uint8, device=DEV)
+    if fmt == "bf16":
+        pool = torch.randn(shape, device=DEV, generator=g).to(torch.bfloat16)
+        P.pallas_attend_kv(pool, 0, q, lengths, n, bt, 0.1, out, ws, lse=lse)
+    else:
+        codes = torch.randint(0, 120, shape, dtype=torch.uint8, device=DEV, generator=g).view(TYPES[fmt])
+        scales = torch.rand(shape[:-1], device=DEV, generator=g) * 0.01
+        P.pallas_attend_quant(codes, scales, 0, q, lengths, n, bt, 0.1, out, ws, lse=lse)
+    for i, x in enumerate(lens):
+        t = torch.arange(x, device=DEV)
+        pg, slot = bt[i].long()[t // 16], t % 16
+        for h in range(0, hkv, 5):
+            if fmt == "bf16":
+                k, v = (pool[0, kv, pg, slot, h].double() for kv in range(2))
+            else:
+                k, v = (codes.view(torch.uint8)[0, kv, pg, slot, h].view(TYPES[fmt]).double() *
+                        scales[0, kv, pg, slot, h].double()[:, None] for kv in range(2))
+            if x == 0:
+                assert not out[i, h].any() and float(lse[i, h]) == -math.inf
+                continue
+            qd = q[i, h].double()
+            z = (k * qd).sum(1) * 0.1
+            ref_lse = torch.logsumexp(z, 0)
+            p = torch.exp(z - ref_lse)
+            ref, mag = (p[:, None] * v).sum(0), (p[:, None] * v.abs()).sum(0)
+            delta = (d + 8) * 2.0 ** -24 * float(((k * qd).abs().sum(1) * 0.1).max())
+            # sums run over thousands of keys a range, and hundreds of ranges: 2^-12 in place of 2^-13
+            tol = 2.0 ** -8 * ref.abs() + (2 * delta + 2.0 ** -12) * mag
+            assert bool(((out[i, h].double() - ref).abs() <= tol).all()), (i, h)
+            assert abs(float(lse[i, h]) - float(ref_lse)) <= delta + 2.0 ** -12
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3", "int8"])
@@ -222,18 +273,19 @@ def test_lengths_outside_the_bound(P, fmt):
 
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3", "int8"])
 def test_a_row_does_not_depend_on_the_others(P, fmt):
-    """To the bit, at the same number of sequences."""
+    """Whatever the others ask and hold, at the same lengths: to the bit."""
     lens = [1300, 77, 500, 0]
     cache = Cache(fmt, 4, 128, lens, seed=10)
     q = queries(4, 16, 128, 2)
     lse = torch.empty((4, 16), dtype=torch.float32, device=DEV)
     out = cache.attend(P, q, 0.1, lse=lse)
-    q2, lengths = q.clone(), cache.lengths.clone()
+    q2 = q.clone()
     q2[1:] = 100.0
-    lengths[1:] = torch.tensor([3, 0, 0], dtype=torch.int32)
+    bt = cache.bt.clone()
+    bt[1, :5], bt[2, 3] = -1, bt[0, 7]
     lse2 = torch.empty_like(lse)
-    out2 = cache.attend(P, q2, 0.1, lse=lse2, lengths=lengths, max_length=1300)
-    assert torch.equal(out[0], out2[0]) and torch.equal(lse[0], lse2[0])
+    out2 = cache.attend(P, q2, 0.1, lse=lse2, bt=bt)
+    assert torch.equal(out[0], out2[0]) and torch.equal(lse[0], lse2[0]) and not torch.equal(out[2], out2[2])
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3", "int8"])

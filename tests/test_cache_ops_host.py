@@ -149,7 +149,7 @@ def test_attend_refusals(P, quant):
         assert "attend" in P.pallas_last_error()
     for bad in (dict(layer=2), dict(layer=-1), dict(max_length=65)):
         assert attend_rc(P, quant, **bad) == S.OUT_OF_RANGE, bad
-    for bad in (dict(seqs=65536), dict(heads=8192, qs=1 << 20, os=1 << 20)):
+    for bad in (dict(seqs=65536), dict(heads=8192, qs=1 << 20, os=1 << 20), dict(seqs=65535, max_length=(1 << 20), max_pages=1 << 16)):
         assert attend_rc(P, quant, **bad) == S.UNSUPPORTED, bad
     assert attend_rc(P, quant, pool=0) == S.INVALID_ARG
     pools = [quant_pool(head_dim=96), quant_pool(page_size=8)] if quant else [
@@ -176,15 +176,22 @@ def test_attend_workspace(P):
         b = np.array([[size(s, hq, hkv, d, n) for n in lens] for s in seqs], dtype=np.int64)
         assert (b > 0).all() and (b % 256 == 0).all()
         assert (np.diff(b, axis=0) >= 0).all() and (np.diff(b, axis=1) >= 0).all()
-    # The longest split list of any length fits a row's share (the split rule, restated).
-    for s, n in itertools.product(seqs, lens):
-        rows = s * 8
-        def splits(length):
-            per = min(1024, max(128, -(-(-(-length * rows // 1024)) // 128) * 128))
-            return -(-length // per)
-        most = max(splits(m) for m in {n, *range(max(1, n - 300), n), *range(1, min(n, 3000), 7)})
-        if most > 1:
-            assert size(s, 64, 8, 128, n) >= s * 64 * most * 130 * 4
+    # Records of any lengths fit: (range, sequence) pairs of every division (the rule, restated, with each
+    # cache type's number of ranges).
+    rng = np.random.default_rng(0)
+    for d, hq, hkv in ((128, 64, 8), (64, 8, 8), (128, 40, 1), (64, 4, 2), (128, 4096, 4096)):
+        for row_bytes in (d, 2 * d):
+            ranges = max(256 * (1024 // row_bytes) // (hkv * -(-(hq // hkv) // 16)) // 8 * 8, 8)
+            for s, n in itertools.product((1, 2, 5, 64, 200), (1, 31, 64, 1000, 40000, 1 << 20)):
+                for _ in range(3):
+                    blocks = -(-rng.integers(0, n + 1, s) // 32)
+                    blocks[rng.integers(s)] = -(-n // 32)
+                    total = int(blocks.sum())
+                    rounds = max(-(-total // (32 * ranges)), 1)
+                    each = max(-(-total // (ranges * rounds)), 2)
+                    assert each <= 32
+                    last = -(-total // each) - 1 + s - 1                # the largest range + sequence
+                    assert size(s, hq, hkv, d, n) >= 8 * s + (last + 1) * hq * (d + 2) * 4
 
 
 # ------------------------------------------------------------------ binding
