@@ -187,9 +187,15 @@ __device__ __forceinline__ int lane_length(const AttendParams& p, int at) {
 }
 __device__ __forceinline__ int blocks_of(int len) { return (len + kBlk - 1) / kBlk; }
 
-__device__ __forceinline__ int wave_total(int v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+// Inclusive prefix sums over the wave (row shifts by 1, 2, 4, 8, then the rows' last
+// lanes to the rows behind).
+__device__ __forceinline__ int wave_prefix(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);   // row_bcast:15 into rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);   // row_bcast:31 into rows 2 and 3
   return v;
 }
 
@@ -204,21 +210,28 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
   const int t = threadIdx.x, lane = t & 63;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int q4 = lane >> 4, l16 = lane & 15;
-  // Workgroups b, b + 8, .. go to one XCD and share an L2: there the heads of one range
-  // follow each other, which share its table entries and the lines of its scales.
-  const int heads = p.Hkv * groups;
-  const int worker = static_cast<int>(blockIdx.x >> 3) * kWaves + wave;
-  const int kh = worker % heads / groups, group = worker % heads % groups;
+  // A workgroup's waves take the same range of four heads: those rows are neighbours in
+  // memory (and share scale lines, table entries and address translations; 64 sequences
+  // E4M3: 62 us, 72 with four ranges of one head).  Workgroups b, b + 8, .. go to one XCD,
+  // where the range's other heads follow.
+  const int heads = p.Hkv * groups, worker = static_cast<int>(blockIdx.x >> 3) * kWaves + wave;
+  const int head = worker % heads, kh = groups == 1 ? head : head / groups, group = head - kh * groups;
   const int r0 = worker / heads * 8 + (blockIdx.x & 7);
   if (r0 >= p.ranges) return;
+  // One sequence: the pages of a range of the least length are read beside its length (a
+  // short call is a chain of loads).
+  int ahead = 0;
+  if (p.seqs == 1 && lane < 2 * kAttendMinBlocks && 2 * kAttendMinBlocks * r0 + lane < p.max_pages)
+    ahead = p.bt[2 * kAttendMinBlocks * r0 + lane];
 
   // All blocks of the call, and the ranges they make.
-  int lens = lane_length(p, 0);
-  int total = wave_total(blocks_of(lens));
-  for (int at = 64; at < p.seqs; at += 64) total += wave_total(blocks_of(lane_length(p, at)));
-  total = __builtin_amdgcn_readfirstlane(total);
+  int win = 0, lens = lane_length(p, 0);        // lens: of sequences [win, win + 64)
+  int before = wave_prefix(blocks_of(lens));    // their blocks, up to and with each
+  int total = __builtin_amdgcn_readlane(before, 63);
+  for (int at = 64; at < p.seqs; at += 64)
+    total += __builtin_amdgcn_readlane(wave_prefix(blocks_of(lane_length(p, at))), 63);
   const int each = attend_blocks(total, p.ranges);
-  if (p.err && r0 == 0 && worker == 0)
+  if (p.err && blockIdx.x == 0 && wave == 0)
     for (int s = lane; s < p.seqs; s += 64)
       if (row_length(p, s) != p.lengths[s]) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_LENGTH));
 
@@ -252,35 +265,51 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
     vb0 = static_cast<uint32_t>(key * D + v_slot<T, CH>(key) * 16 + (l16 & 1) * 8);
   }
 
-  int win = 0;                                  // lens: of sequences [win, win + 64)
+  auto window = [&](int s) {                    // makes s one of the 64
+    if (s >= win && s < win + 64) return;
+    win = s & ~63;
+    lens = lane_length(p, win);
+    before = wave_prefix(blocks_of(lens));
+  };
   auto length = [&](int s) {
-    if (s >= win + 64) lens = lane_length(p, win = s & ~63);
+    window(s);
     return __builtin_amdgcn_readlane(lens, s & 63);
   };
   int s = 0, base = 0;                          // a sequence, and the blocks before it
-  for (int r = r0; int64_t(r) * each < total; r += p.ranges) {
-  const int f0 = r * each, f1 = min(f0 + each, total);
-  // The sequence of the range's first block: whole windows, then in one.
-  while (s < p.seqs) {
-    if (s >= win + 64) lens = lane_length(p, win = s & ~63);
-    const int nb = lane >= (s & 63) ? blocks_of(lens) : 0;
-    int sum = nb;
+  // Moves them on to the sequence that block f (of the call's) is in.
+  auto seek = [&](int f) {
+    while (s < p.seqs) {
+      window(s);
+      // blocks of the window before s
+      const int skip = __builtin_amdgcn_readlane(before - blocks_of(lens), s & 63);
+      const uint64_t behind = __builtin_amdgcn_ballot_w64(lane >= (s & 63) && base + before - skip > f);
+      if (behind != 0) {
+        const int first = __builtin_ctzll(behind);
+        base += __builtin_amdgcn_readlane(before - blocks_of(lens), first) - skip;
+        s = win + first;
+        return;
+      }
+      base += __builtin_amdgcn_readlane(before, 63) - skip;
+      s = win + 64;
+    }
+  };
+  // Q: the MFMA's B operand, column l16 = a head (repeated where there are fewer).  Its
+  // dimensions follow what a lane reads of K: bf16, chunk 4 kk + q4; 8 bits, half kk % 2
+  // of chunk 4 (kk / 2) + q4.
+  u32x4 qf[D / 32];
+  auto load_q = [&](int s) {
+    const uint16_t* q = p.q + s * p.q_stride + int64_t(h0 + l16 % nh) * D;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int up = __shfl_up(sum, o, 64);
-      sum += lane >= o ? up : 0;
-    }
-    const uint64_t behind = __builtin_amdgcn_ballot_w64(base + sum > f0);
-    if (behind != 0) {
-      const int first = __builtin_ctzll(behind);
-      base += __builtin_amdgcn_readlane(sum, first) - __builtin_amdgcn_readlane(nb, first);
-      s = win + first;
-      break;
-    }
-    base += __builtin_amdgcn_readlane(sum, 63);
-    s = win + 64;
-  }
-  // Pages of its blocks.
+    for (int kk = 0; kk < D / 32; ++kk)
+      qf[kk] = *reinterpret_cast<const u32x4*>(q + (T == kCacheBf16 ? 32 * kk + 8 * q4 : 64 * (kk / 2) + 16 * q4 + 8 * (kk % 2)));
+  };
+
+  for (int r = r0; r * each < total; r += p.ranges) {
+  const int f0 = r * each, f1 = min(f0 + each, total), blocks = f1 - f0;
+  seek(f0);
+  if (s >= p.seqs) break;                       // (lengths that changed since `total`)
+  load_q(s);
+  // Pages of the range's blocks.
   src.page = 0;
   src.keys = 0;
   {
@@ -296,40 +325,27 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
       at += nb;
     }
     if (src.keys > 0) {
-      src.page = p.bt[int64_t(from) * p.max_pages + key0 / kPage];
+      src.page = p.seqs == 1 && each == kAttendMinBlocks ? ahead : p.bt[int64_t(from) * p.max_pages + key0 / kPage];
       if (src.page < 0 || src.page >= p.num_pages) {
         src.page = src.keys = 0;
-        if (p.err && kh == 0 && group == 0) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
+        if (p.err && head == 0) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
       }
     }
-    if (s < win) lens = lane_length(p, win = s & ~63);
   }
-  const int blocks = f1 - f0;
 #pragma unroll
   for (int i = 0; i < kStages; ++i) issue_block<D, T>(p, src, scales, kh, i, i < blocks, koff, voff, ring + i * S::kSlots);
-
-  int i = 0;
-  while (i < blocks && s < p.seqs) {
-  const int nb = blocks_of(length(s));
-  if (nb == 0) {
-    ++s;
-    continue;
-  }
-  const int begin = f0 + i - base, stop = min(blocks, base + nb - f0);    // its block at i; where it or the range ends
-  // Q: the MFMA's B operand, column l16 = a head (repeated where there are fewer).  Its
-  // dimensions follow what a lane reads of K: bf16, chunk 4 kk + q4; 8 bits, half kk % 2
-  // of chunk 4 (kk / 2) + q4.
-  u32x4 qf[D / 32];
-  {
-    const uint16_t* q = p.q + s * p.q_stride + int64_t(h0 + l16 % nh) * D;
+  // Waited for once, here (they are older than the K/V loads), and not inside the stream.
 #pragma unroll
-    for (int kk = 0; kk < D / 32; ++kk)
-      qf[kk] = *reinterpret_cast<const u32x4*>(q + (T == kCacheBf16 ? 32 * kk + 8 * q4 : 64 * (kk / 2) + 16 * q4 + 8 * (kk % 2)));
-  }
+  for (int kk = 0; kk < D / 32; ++kk) asm volatile("" : "+v"(qf[kk]));
+
   f32x4 acc[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) acc[dt] = f32x4{};
   float m = -INFINITY, lsum = 0.f;
+  int i = 0;
+  while (i < blocks && s < p.seqs) {
+  const int nb = blocks_of(length(s));
+  const int begin = f0 + i - base, stop = min(blocks, base + nb - f0);    // its block at i; where it or the range ends
 #pragma unroll 1
   for (; i < stop; ++i) {
     u32x4* const Kst = ring + (static_cast<unsigned>(i) % kStages) * S::kSlots;
@@ -431,7 +447,8 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
 
   // Lane: dimensions 16 dt + 4 q4 .. + 3 of head l16.
   lsum = rows_sum(lsum);
-  const bool whole = begin == 0 && base + nb <= f1;
+  const int end = base + nb;
+  const bool whole = begin == 0 && end <= f1;
   if (l16 < nh) {
     if (whole) {
 #pragma unroll
@@ -444,14 +461,19 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
       if (q4 == 0) *reinterpret_cast<f32x2*>(p.part_ml + rec * 2) = f32x2{m, lsum};
     }
   }
-  if (begin == 0 && kh == 0 && group == 0 && lane == 0) {
+  if (begin == 0 && head == 0 && lane == 0) {
     // The row's records: none, or from here to the range of its last block.
-    p.parts[2 * s] = r;
-    p.parts[2 * s + 1] = whole ? 0 : (base + nb - 1) / each - r + 1;
+    reinterpret_cast<int2*>(p.parts)[s] = int2{r, whole ? 0 : (end - 1) / each - r + 1};
   }
-  if (base + nb > f1) break;                    // the rest is the next range's
-  base += nb;
-  ++s;
+  if (i >= blocks) break;
+  // On to the next sequence that has keys.
+  seek(f0 + i);
+  if (s >= p.seqs) break;
+  load_q(s);
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) acc[dt] = f32x4{};
+  m = -INFINITY;
+  lsum = 0.f;
   }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load into LDS outlives its wave
@@ -459,6 +481,7 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
 
 // Joins a row's records: one workgroup per (query head, sequence).  D / 4 lanes hold a
 // record; a wave takes 256 / D records side by side and kJoinBatch of those in flight.
+// The records of the only sequence of a call are read before their number is known.
 // Rows without a key get their zeros here.
 constexpr int kJoinBatch = 8;
 template <int D, int kThreads>
@@ -468,17 +491,27 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendParams p) {
   const int h = blockIdx.x, s = blockIdx.y, t = threadIdx.x;
   const int side = t / kLanes, i = (t % kLanes) * 4;
   const int mine = t / 64 * kShare + side % kWaveSide;      // this lane's first record of a round
-  // (Within the records whatever is read: lengths that change during a call give a wrong
-  // result, but nothing else.)
-  const int first = min(max(p.parts[2 * s], 0), p.records - 1 - s);
-  const int n = min(p.parts[2 * s + 1], p.records - s - first);
-  if (row_length(p, s) == 0) {
+  const int2 parts = reinterpret_cast<const int2*>(p.parts)[s];
+  const int len = row_length(p, s);
+  const int first = p.seqs == 1 ? 0 : parts.x;
+  f32x2 a[kJoinBatch];
+  f32x4 v[kJoinBatch];
+  auto read = [&](int k0) {
+#pragma unroll
+    for (int b = 0; b < kJoinBatch; ++b) {
+      // (Within the records whatever is read, also where lengths change during a call.)
+      const int64_t rec = min(max(first + s + k0 + b * kWaveSide + mine, 0), p.records - 1) * int64_t(p.Hq) + h;
+      a[b] = reinterpret_cast<const f32x2*>(p.part_ml)[rec];
+      v[b] = *reinterpret_cast<const f32x4*>(p.part_o + rec * D + i);
+    }
+  };
+  if (p.seqs == 1 || (len > 0 && mine < parts.y)) read(0);
+  if (len == 0) {
     if (t < kLanes) write_row(p, s, h, i, f32x4{}, -INFINITY, 0.f);
     return;
   }
+  const int n = min(parts.y, p.records);
   if (n <= 0) return;
-  const f32x2* ml = reinterpret_cast<const f32x2*>(p.part_ml) + (int64_t(first) + s) * p.Hq + h;
-  const float* po = p.part_o + ((int64_t(first) + s) * p.Hq + h) * D + i;
   float m = -INFINITY, l = 0.f;
   f32x4 o{};
   auto add = [&](float mk, float lk, f32x4 ok) {
@@ -488,40 +521,40 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendParams p) {
     o = keep * o + w * ok;
     m = top;
   };
-  for (int k0 = 0; k0 < n; k0 += kRound) {
-    f32x2 a[kJoinBatch];
-    f32x4 v[kJoinBatch];
-#pragma unroll
-    for (int b = 0; b < kJoinBatch; ++b) {
-      const int64_t k = min(k0 + b * kWaveSide + mine, n - 1);
-      a[b] = ml[k * p.Hq];
-      v[b] = *reinterpret_cast<const f32x4*>(po + k * p.Hq * D);
-    }
+  for (int k0 = 0;;) {
 #pragma unroll
     for (int b = 0; b < kJoinBatch; ++b)
       if (k0 + b * kWaveSide + mine < n) add(a[b].x, a[b].y, v[b]);
+    k0 += kRound;
+    if (k0 + mine >= n) break;
+    read(k0);
   }
+  // The sides, as a tree.
   __shared__ f32x2 mls[kSide];
   __shared__ f32x4 os[kSide][kLanes];
-  os[side][t % kLanes] = o;
-  if (t % kLanes == 0) mls[side] = f32x2{m, l};
-  __syncthreads();
-  if (t >= kLanes) return;
 #pragma unroll
-  for (int k = 1; k < kSide; ++k) add(mls[k].x, mls[k].y, os[k][t]);
-  write_row(p, s, h, i, o, m, l);
+  for (int half = kSide / 2; half > 0; half /= 2) {
+    if (side >= half && side < 2 * half) {
+      os[side][t % kLanes] = o;
+      mls[side] = f32x2{m, l};
+    }
+    __syncthreads();
+    if (side < half) add(mls[side + half].x, mls[side + half].y, os[side + half][t % kLanes]);
+  }
+  if (side == 0) write_row(p, s, h, i, o, m, l);
 }
 
 template <int D, CacheType T>
 hipError_t launch(const AttendParams& p, hipStream_t s) {
   const int groups = (p.Hq / p.Hkv + kAttendGroup - 1) / kAttendGroup;
   const int64_t workers = int64_t(p.ranges) / 8 * p.Hkv * groups;          // on each XCD
-  const unsigned grid = static_cast<unsigned>((workers + kWaves - 1) / kWaves * 8);
-  attend_kernel<D, T><<<grid, kWaves * 64, 0, s>>>(p, groups);
+  attend_kernel<D, T><<<static_cast<unsigned>((workers + kWaves - 1) / kWaves * 8), kWaves * 64, 0, s>>>(p, groups);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  // As many waves as a row of an even batch can fill with records in one go.
   const dim3 joins(p.Hq, p.seqs);
-  // One wave where a row of an even batch has no more records than its share.
-  if (p.ranges / p.seqs >= kJoinBatch * 256 / D) join_kernel<D, 256><<<joins, 256, 0, s>>>(p);
+  constexpr int kShare = kJoinBatch * 256 / D;
+  if (p.ranges / p.seqs > 4 * kShare) join_kernel<D, 1024><<<joins, 1024, 0, s>>>(p);
+  else if (p.ranges / p.seqs >= kShare) join_kernel<D, 256><<<joins, 256, 0, s>>>(p);
   else join_kernel<D, 64><<<joins, 64, 0, s>>>(p);
   return hipGetLastError();
 }

@@ -430,8 +430,9 @@ inline int64_t attend_heads(int Hq, int Hkv) { return int64_t(Hkv) * ((Hq / Hkv 
 // Blocks per range of a call of `total` blocks: as few rounds of the ranges as the
 // largest one allows, all rounds full.
 __host__ __device__ inline int attend_blocks(int total, int ranges) {
-  const int rounds = std::max(int((int64_t(total) + int64_t(kAttendMaxBlocks) * ranges - 1) / (int64_t(kAttendMaxBlocks) * ranges)), 1);
-  const int64_t all = int64_t(rounds) * ranges;
+  if (total <= kAttendMinBlocks * ranges) return kAttendMinBlocks;
+  const uint32_t most = uint32_t(kAttendMaxBlocks) * ranges;             // total <= 2^30, most <= 2^17
+  const uint32_t rounds = std::max((total + most - 1) / most, 1u), all = rounds * ranges;
   return std::max(int((total + all - 1) / all), kAttendMinBlocks);
 }
 // Bound on (range, sequence) pairs of a call, which grows with seqs and max_length:

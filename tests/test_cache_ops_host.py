@@ -181,7 +181,8 @@ def test_attend_workspace(P):
     rng = np.random.default_rng(0)
     for d, hq, hkv in ((128, 64, 8), (64, 8, 8), (128, 40, 1), (64, 4, 2), (128, 4096, 4096)):
         for row_bytes in (d, 2 * d):
-            ranges = max(256 * (1024 // row_bytes) // (hkv * -(-(hq // hkv) // 16)) // 8 * 8, 8)
+            ranges = 256 * (1024 // row_bytes) // (hkv * -(-(hq // hkv) // 16))
+            ranges = max(ranges // 8 * 8, 8)
             for s, n in itertools.product((1, 2, 5, 64, 200), (1, 31, 64, 1000, 40000, 1 << 20)):
                 for _ in range(3):
                     blocks = -(-rng.integers(0, n + 1, s) // 32)
