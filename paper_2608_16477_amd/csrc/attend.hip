@@ -183,9 +183,10 @@ __device__ __forceinline__ void issue_block(const AttendParams& p, const Source&
 // Lengths of 64 sequences from `at` on, one per lane, in 32-key blocks (0 behind the last).
 __device__ __forceinline__ int lane_length(const AttendParams& p, int at) {
   const int s = at + static_cast<int>(threadIdx.x & 63);
-  return s < p.seqs ? row_length(p, s) : 0;
+  const int len = row_length(p, min(s, p.seqs - 1));
+  return s < p.seqs ? len : 0;
 }
-__device__ __forceinline__ int blocks_of(int len) { return (len + kBlk - 1) / kBlk; }
+__device__ __forceinline__ int blocks_of(int len) { return static_cast<int>(static_cast<uint32_t>(len + kBlk - 1) / kBlk); }
 
 // Inclusive prefix sums over the wave (row shifts by 1, 2, 4, 8, then the rows' last
 // lanes to the rows behind).
@@ -200,7 +201,7 @@ __device__ __forceinline__ int wave_prefix(int v) {
 }
 
 template <int D, CacheType T>
-__global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, int groups) {
+__global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, int groups, int head_shift) {
   using S = Shape<D, T>;
   constexpr int CH = S::kCh, DT = D / 16;
   // One array: with several, the compiler's alias scopes make LDS reads of a
@@ -210,33 +211,21 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
   const int t = threadIdx.x, lane = t & 63;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int q4 = lane >> 4, l16 = lane & 15;
-  // A workgroup's waves take the same range of four heads: those rows are neighbours in
-  // memory (and share scale lines, table entries and address translations; 64 sequences
-  // E4M3: 62 us, 72 with four ranges of one head).  Workgroups b, b + 8, .. go to one XCD,
-  // where the range's other heads follow.
-  const int heads = p.Hkv * groups, worker = static_cast<int>(blockIdx.x >> 3) * kWaves + wave;
-  const int head = worker % heads, kh = groups == 1 ? head : head / groups, group = head - kh * groups;
-  const int r0 = worker / heads * 8 + (blockIdx.x & 7);
+  // A workgroup's waves take the same range of four heads (of two or one where the heads
+  // are not a multiple): those rows are neighbours in memory, and share scale lines, table
+  // entries and address translations (64 sequences E4M3: 62 us; 65 to 72 with four ranges
+  // of one head).  Workgroups of one blockIdx.x go to one XCD.
+  const int head = (static_cast<int>(blockIdx.y) << head_shift) + (wave & ((1 << head_shift) - 1));
+  const int kh = groups == 1 ? head : head / groups, group = head - kh * groups;
+  const int r0 = static_cast<int>(blockIdx.x) * (kWaves >> head_shift) + (wave >> head_shift);
   if (r0 >= p.ranges) return;
-  // One sequence: the pages of a range of the least length are read beside its length (a
-  // short call is a chain of loads).
+  // One sequence: the pages of this range, were it of one block (lanes 0, 1) or of two
+  // (lanes 8 to 11), are read beside the length (a short call is a chain of loads).
   int ahead = 0;
-  if (p.seqs == 1 && lane < 2 * kAttendMinBlocks && 2 * kAttendMinBlocks * r0 + lane < p.max_pages)
-    ahead = p.bt[2 * kAttendMinBlocks * r0 + lane];
-
-  // All blocks of the call, and the ranges they make.
+  if (p.seqs == 1) ahead = p.bt[min(lane < 8 ? 2 * r0 + lane : 4 * r0 + lane - 8, p.max_pages - 1)];
   int win = 0, lens = lane_length(p, 0);        // lens: of sequences [win, win + 64)
-  int before = wave_prefix(blocks_of(lens));    // their blocks, up to and with each
-  int total = __builtin_amdgcn_readlane(before, 63);
-  for (int at = 64; at < p.seqs; at += 64)
-    total += __builtin_amdgcn_readlane(wave_prefix(blocks_of(lane_length(p, at))), 63);
-  const int each = attend_blocks(total, p.ranges);
-  if (p.err && blockIdx.x == 0 && wave == 0)
-    for (int s = lane; s < p.seqs; s += 64)
-      if (row_length(p, s) != p.lengths[s]) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_LENGTH));
 
-  const int G = p.Hq / p.Hkv;
-  const int h0 = kh * G + group * kAttendGroup, nh = min(kAttendGroup, G - group * kAttendGroup);
+  const int h0 = kh * p.G + group * kAttendGroup, nh = min(kAttendGroup, p.G - group * kAttendGroup);
   Source src;
   src.rs = static_cast<uint32_t>(p.Hkv) * S::kRow;
   src.page_bytes = int64_t(kPage) * src.rs;
@@ -265,6 +254,12 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
     vb0 = static_cast<uint32_t>(key * D + v_slot<T, CH>(key) * 16 + (l16 & 1) * 8);
   }
 
+  // All blocks of the call, and the ranges they make.
+  int before = wave_prefix(blocks_of(lens));    // blocks of the window's sequences, up to and with each
+  int total = __builtin_amdgcn_readlane(before, 63);
+  for (int at = 64; at < p.seqs; at += 64)
+    total += __builtin_amdgcn_readlane(wave_prefix(blocks_of(lane_length(p, at))), 63);
+  const int each = attend_blocks(total, p.ranges);
   auto window = [&](int s) {                    // makes s one of the 64
     if (s >= win && s < win + 64) return;
     win = s & ~63;
@@ -293,12 +288,12 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
       s = win + 64;
     }
   };
-  // Q: the MFMA's B operand, column l16 = a head (repeated where there are fewer).  Its
+  // Q: the MFMA's B operand, column l16 = a head (the last one again where there are fewer).  Its
   // dimensions follow what a lane reads of K: bf16, chunk 4 kk + q4; 8 bits, half kk % 2
   // of chunk 4 (kk / 2) + q4.
   u32x4 qf[D / 32];
   auto load_q = [&](int s) {
-    const uint16_t* q = p.q + s * p.q_stride + int64_t(h0 + l16 % nh) * D;
+    const uint16_t* q = p.q + s * p.q_stride + int64_t(h0 + min(l16, nh - 1)) * D;
 #pragma unroll
     for (int kk = 0; kk < D / 32; ++kk)
       qf[kk] = *reinterpret_cast<const u32x4*>(q + (T == kCacheBf16 ? 32 * kk + 8 * q4 : 64 * (kk / 2) + 16 * q4 + 8 * (kk % 2)));
@@ -324,8 +319,9 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
       }
       at += nb;
     }
+    if (each == 2) ahead = __builtin_amdgcn_mov_dpp(ahead, 0x108, 0xF, 0xF, false);   // row_shl:8
     if (src.keys > 0) {
-      src.page = p.seqs == 1 && each == kAttendMinBlocks ? ahead : p.bt[int64_t(from) * p.max_pages + key0 / kPage];
+      src.page = p.seqs == 1 && each <= 2 ? ahead : p.bt[int64_t(from) * p.max_pages + key0 / kPage];
       if (src.page < 0 || src.page >= p.num_pages) {
         src.page = src.keys = 0;
         if (p.err && head == 0) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
@@ -493,6 +489,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendParams p) {
   const int mine = t / 64 * kShare + side % kWaveSide;      // this lane's first record of a round
   const int2 parts = reinterpret_cast<const int2*>(p.parts)[s];
   const int len = row_length(p, s);
+  if (p.err && h == 0 && t == 0 && len != p.lengths[s]) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_LENGTH));
   const int first = p.seqs == 1 ? 0 : parts.x;
   f32x2 a[kJoinBatch];
   f32x4 v[kJoinBatch];
@@ -546,15 +543,19 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendParams p) {
 
 template <int D, CacheType T>
 hipError_t launch(const AttendParams& p, hipStream_t s) {
-  const int groups = (p.Hq / p.Hkv + kAttendGroup - 1) / kAttendGroup;
-  const int64_t workers = int64_t(p.ranges) / 8 * p.Hkv * groups;          // on each XCD
-  attend_kernel<D, T><<<static_cast<unsigned>((workers + kWaves - 1) / kWaves * 8), kWaves * 64, 0, s>>>(p, groups);
+  const int groups = (p.G + kAttendGroup - 1) / kAttendGroup;
+  const int heads = p.Hkv * groups, head_shift = heads % 4 == 0 ? 2 : heads % 2 == 0 ? 1 : 0;
+  const int per = kWaves >> head_shift;         // ranges of a workgroup
+  attend_kernel<D, T><<<dim3((p.ranges + per - 1) / per, heads >> head_shift), kWaves * 64, 0, s>>>(p, groups, head_shift);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  // As many waves as a row of an even batch can fill with records in one go.
+  // As many waves as a row can fill with records in one go: a wave in large batches, in
+  // others after the most records that max_length allows.  (Further waves then have
+  // nothing to add and change no bit, so a row's result does not depend on max_length.)
   const dim3 joins(p.Hq, p.seqs);
   constexpr int kShare = kJoinBatch * 256 / D;
-  if (p.ranges / p.seqs > 4 * kShare) join_kernel<D, 1024><<<joins, 1024, 0, s>>>(p);
-  else if (p.ranges / p.seqs >= kShare) join_kernel<D, 256><<<joins, 256, 0, s>>>(p);
+  const int64_t most = p.ranges / p.seqs < kShare ? 0 : attend_total(1, p.max_length);
+  if (most > 4 * kShare) join_kernel<D, 1024><<<joins, 1024, 0, s>>>(p);
+  else if (most > kShare) join_kernel<D, 256><<<joins, 256, 0, s>>>(p);
   else join_kernel<D, 64><<<joins, 64, 0, s>>>(p);
   return hipGetLastError();
 }

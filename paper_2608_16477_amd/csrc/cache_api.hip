@@ -141,6 +141,7 @@ int attend_call(const char* what, pallas::CacheType type, pallas::AttendParams& 
   if (ws_bytes < sp.bytes)
     return fail(PALLAS_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", what, ws_bytes, sp.bytes);
   p.Hq = n_q_heads;
+  p.G = n_q_heads / p.Hkv;
   p.seqs = num_seqs;
   p.max_length = max_length;
   p.max_pages = max_pages;

@@ -395,7 +395,7 @@ struct AttendParams {
   const void* k;           // [num_pages][16][Hkv][d] of the layer
   const void* v;
   const float* scales;     // 8-bit: [2][num_pages][16][Hkv], K and V of the layer, below 4 GiB
-  int num_pages, Hkv, Hq, d;
+  int num_pages, Hkv, Hq, G, d;   // G = Hq / Hkv
   int seqs, max_length, max_pages;
   const uint16_t* q;
   int64_t q_stride;
@@ -414,9 +414,7 @@ struct AttendParams {
 };
 constexpr int kAttendBlock = 32;         // keys per block
 constexpr int kAttendGroup = 16;         // query heads that share one pass over a KV head
-// Blocks of a wave's range: both of its ring stages at least, and at most one per pair of
-// lanes.
-constexpr int kAttendMinBlocks = 2;
+// Blocks of a wave's range: at most one per pair of lanes.
 constexpr int kAttendMaxBlocks = 32;
 // Waves that a CU holds, by the bytes of a head row: each has a ring of two stages of 32
 // K and V rows, 128 KiB in all.
@@ -428,21 +426,25 @@ inline int attend_ranges(int row_bytes, int64_t heads) {
 // KV heads, times the passes over each.
 inline int64_t attend_heads(int Hq, int Hkv) { return int64_t(Hkv) * ((Hq / Hkv + kAttendGroup - 1) / kAttendGroup); }
 // Blocks per range of a call of `total` blocks: as few rounds of the ranges as the
-// largest one allows, all rounds full.
+// largest one allows, all rounds full.  Calls that leave half of the waves without a block
+// give one to each; others at least two, one per ring stage (one and two, us: 1 row of 500
+// keys bf16 8.4, 8.6; 27 rows of 30 to 2000 keys 8.4, 9.2; 1 row of 4000 keys 13.7, 12.4: more
+// records to join).
 __host__ __device__ inline int attend_blocks(int total, int ranges) {
-  if (total <= kAttendMinBlocks * ranges) return kAttendMinBlocks;
+  if (2 * int64_t(total) <= ranges) return 1;
+  if (total <= 2 * ranges) return 2;
   const uint32_t most = uint32_t(kAttendMaxBlocks) * ranges;             // total <= 2^30, most <= 2^17
   const uint32_t rounds = std::max((total + most - 1) / most, 1u), all = rounds * ranges;
-  return std::max(int((total + all - 1) / all), kAttendMinBlocks);
+  return int((total + all - 1) / all);
 }
 // Bound on (range, sequence) pairs of a call, which grows with seqs and max_length:
-// ranges * rounds <= ranges + total / 32, and no range is below the least length.
+// ranges * rounds <= ranges + total / 32, and no range is empty.
 inline int64_t attend_total(int64_t seqs, int max_length) {
   return seqs * ((int64_t(max_length) + kAttendBlock - 1) / kAttendBlock);
 }
 inline int64_t attend_records(int64_t seqs, int max_length, int ranges) {
   const int64_t total = attend_total(seqs, max_length);
-  return std::min((total + kAttendMinBlocks - 1) / kAttendMinBlocks, ranges + total / kAttendMaxBlocks) + seqs;
+  return std::min(total, ranges + total / kAttendMaxBlocks) + seqs;
 }
 hipError_t launch_attend(const AttendParams& p, CacheType type, hipStream_t s);
 

@@ -189,7 +189,7 @@ def test_attend_workspace(P):
                     blocks[rng.integers(s)] = -(-n // 32)
                     total = int(blocks.sum())
                     rounds = max(-(-total // (32 * ranges)), 1)
-                    each = max(-(-total // (ranges * rounds)), 2)
+                    each = 1 if 2 * total <= ranges else 2 if total <= 2 * ranges else -(-total // (ranges * rounds))
                     assert each <= 32
                     last = -(-total // each) - 1 + s - 1                # the largest range + sequence
                     assert size(s, hq, hkv, d, n) >= 8 * s + (last + 1) * hq * (d + 2) * 4
