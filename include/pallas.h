@@ -440,7 +440,7 @@ typedef struct {
  * [0, num_seqs), a position beyond the table, or an entry outside [0, num_pages)
  * is skipped too and raises PALLAS_DEVERR_PAGE in *d_err (nullable).  Nothing
  * else of the pool is written.  What a slot gets that two tokens of one call
- * name is undefined. */
+ * name is undefined.  num_tokens * 2 * n_kv_heads below 2^31 (UNSUPPORTED). */
 int pallas_quant_store(const pallas_quant_pool* pool, int32_t layer, int32_t num_tokens,
                        const int32_t* d_seq_ids, const int32_t* d_positions, const void* d_k,
                        int64_t k_stride, const void* d_v, int64_t v_stride, int32_t num_seqs,

@@ -259,7 +259,7 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
   int total = __builtin_amdgcn_readlane(before, 63);
   for (int at = 64; at < p.seqs; at += 64)
     total += __builtin_amdgcn_readlane(wave_prefix(blocks_of(lane_length(p, at))), 63);
-  const int each = attend_blocks(total, p.ranges);
+  const int each = attend_blocks(total, p.seqs, p.ranges);
   auto window = [&](int s) {                    // makes s one of the 64
     if (s >= win && s < win + 64) return;
     win = s & ~63;
@@ -553,7 +553,7 @@ hipError_t launch(const AttendParams& p, hipStream_t s) {
   // nothing to add and change no bit, so a row's result does not depend on max_length.)
   const dim3 joins(p.Hq, p.seqs);
   constexpr int kShare = kJoinBatch * 256 / D;
-  const int64_t most = p.ranges / p.seqs < kShare ? 0 : attend_total(1, p.max_length);
+  const int64_t most = p.ranges / p.seqs < kShare ? 0 : attend_row_records(attend_total(1, p.max_length), p.seqs, p.ranges);
   if (most > 4 * kShare) join_kernel<D, 1024><<<joins, 1024, 0, s>>>(p);
   else if (most > kShare) join_kernel<D, 256><<<joins, 256, 0, s>>>(p);
   else join_kernel<D, 64><<<joins, 64, 0, s>>>(p);

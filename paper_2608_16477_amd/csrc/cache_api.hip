@@ -55,9 +55,9 @@ int quant_call(bool store, const pallas_quant_pool* pool, int32_t layer, int32_t
     return fail(PALLAS_ERR_INVALID_ARG, "%s: rows not 16-byte aligned", what);
   if (k_stride < row || v_stride < row)
     return fail(PALLAS_ERR_INVALID_ARG, "%s: row stride below the %lld elements of a row", what, (long long)row);
-  // Workgroups of 32 (or 64) rows: fewer than 2^31 of them.
-  if (int64_t(num_tokens) * 2 * pool->n_kv_heads > (int64_t(1) << 35))
-    return fail(PALLAS_ERR_UNSUPPORTED, "%s: too many rows", what);
+  if (int64_t(num_tokens) * 2 * pool->n_kv_heads >= (int64_t(1) << 31))
+    return fail(PALLAS_ERR_UNSUPPORTED, "%s: %d tokens of %d K and V rows (below 2^31 rows in all)", what, num_tokens,
+                2 * pool->n_kv_heads);
   pallas::QuantParams p{};
   p.codes = static_cast<uint8_t*>(pool->codes) + 2 * layer * plane_rows(pool) * pool->head_dim;
   p.scales = pool->scales + 2 * layer * plane_rows(pool);

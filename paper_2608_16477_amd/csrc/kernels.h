@@ -426,16 +426,22 @@ inline int attend_ranges(int row_bytes, int64_t heads) {
 // KV heads, times the passes over each.
 inline int64_t attend_heads(int Hq, int Hkv) { return int64_t(Hkv) * ((Hq / Hkv + kAttendGroup - 1) / kAttendGroup); }
 // Blocks per range of a call of `total` blocks: as few rounds of the ranges as the
-// largest one allows, all rounds full.  Calls that leave half of the waves without a block
-// give one to each; others at least two, one per ring stage (one and two, us: 1 row of 500
-// keys bf16 8.4, 8.6; 27 rows of 30 to 2000 keys 8.4, 9.2; 1 row of 4000 keys 13.7, 12.4: more
-// records to join).
-__host__ __device__ inline int attend_blocks(int total, int ranges) {
-  if (2 * int64_t(total) <= ranges) return 1;
+// largest one allows, all rounds full.  Calls of short rows that leave half of the waves
+// without a block give one to each, others at least two, one per ring stage (one and two,
+// us: 1 row of 500 keys bf16 8.4, 8.6; 27 rows of 30 to 2000 keys 8.4, 9.2; 1 row of 4000
+// keys 13.7, 12.4: more records to join).
+constexpr int kAttendShort = 32;         // blocks of a row
+__host__ __device__ inline int attend_blocks(int total, int seqs, int ranges) {
+  if (2 * int64_t(total) <= ranges && total <= int64_t(kAttendShort) * seqs) return 1;
   if (total <= 2 * ranges) return 2;
   const uint32_t most = uint32_t(kAttendMaxBlocks) * ranges;             // total <= 2^30, most <= 2^17
   const uint32_t rounds = std::max((total + most - 1) / most, 1u), all = rounds * ranges;
   return int((total + all - 1) / all);
+}
+// The most records of a row of `blocks`: all its blocks where each is a range (as above),
+// else those of ranges of two and a part at either end.
+inline int64_t attend_row_records(int64_t blocks, int64_t seqs, int ranges) {
+  return std::min(blocks, std::max(std::min(kAttendShort * seqs, int64_t(ranges) / 2), blocks / 2 + 2));
 }
 // Bound on (range, sequence) pairs of a call, which grows with seqs and max_length:
 // ranges * rounds <= ranges + total / 32, and no range is empty.

@@ -18,32 +18,41 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kPage = 16;
+// Rows read back are stored non-temporally from this many bytes on (35,000 tokens of 8
+// heads of 128: XX us, YY with plain stores; 3000: XX, YY); fewer stay in the caches for
+// what reads them next.
+constexpr int64_t kNtStoreBytes = int64_t(4) << 20;
 constexpr uint32_t kInfBits = 0x7F80;
 constexpr uint32_t kNanScale = 0x7FC00000;
 
-// Where row `row` of the call (token-major, K heads then V heads) sits in the pool
-// (its index among the K plane's rows, then the V plane's) and in the caller's rows.
-struct Place {
-  int64_t slot;
-  int64_t at;     // element offset in the K (or V) rows
+// Row `row` of the call (token-major, K heads then V heads): a token, its plane and head.
+struct Row {
+  int t, h, h2;
   bool v;
 };
-__device__ __forceinline__ bool place(const QuantParams& p, int64_t row, bool flag, Place& out) {
-  const int t = static_cast<int>(row / (2 * p.Hkv)), h2 = static_cast<int>(row - int64_t(t) * (2 * p.Hkv));
-  out.v = h2 >= p.Hkv;
-  const int h = out.v ? h2 - p.Hkv : h2;
-  out.at = t * (out.v ? p.v_stride : p.k_stride) + int64_t(h) * p.d;
-  const int pos = p.pos[t];
-  if (pos < 0) return false;
-  const int s = p.seq ? p.seq[t] : t;
+__device__ __forceinline__ Row row_of(const QuantParams& p, uint32_t row) {
+  Row r;
+  r.t = static_cast<int>(row / static_cast<uint32_t>(2 * p.Hkv));
+  r.h2 = static_cast<int>(row) - r.t * (2 * p.Hkv);
+  r.v = r.h2 >= p.Hkv;
+  r.h = r.v ? r.h2 - p.Hkv : r.h2;
+  return r;
+}
+// Its element offset in the caller's K (or V) rows.
+__device__ __forceinline__ int64_t at_of(const QuantParams& p, const Row& r) {
+  return r.t * (r.v ? p.v_stride : p.k_stride) + static_cast<int64_t>(r.h) * p.d;
+}
+// Its place in the pool, among the rows of both planes; negative: skipped.
+__device__ __forceinline__ int64_t slot_of(const QuantParams& p, const Row& r, bool flag) {
+  const int pos = p.pos[r.t], s = p.seq ? p.seq[r.t] : r.t;
+  if (pos < 0) return -1;
   int pg = -1;
-  if (s >= 0 && s < p.seqs && pos / kPage < p.max_pages) pg = p.bt[int64_t(s) * p.max_pages + pos / kPage];
+  if (s >= 0 && s < p.seqs && pos / kPage < p.max_pages) pg = p.bt[static_cast<int64_t>(s) * p.max_pages + pos / kPage];
   if (pg < 0 || pg >= p.num_pages) {
-    if (flag && h2 == 0 && p.err) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
-    return false;
+    if (flag && r.h2 == 0 && p.err) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
+    return -1;
   }
-  out.slot = ((int64_t(out.v ? p.num_pages : 0) + pg) * kPage + pos % kPage) * p.Hkv + h;
-  return true;
+  return ((static_cast<int64_t>(r.v ? p.num_pages : 0) + pg) * kPage + pos % kPage) * p.Hkv + r.h;
 }
 
 // Larger magnitude of each half of two packed pairs of bf16 (signs cleared).
@@ -56,16 +65,16 @@ __device__ __forceinline__ uint32_t dpp_xor2(uint32_t v) { return __builtin_amdg
 constexpr int kDppHalfMirror = 0x141;   // lane i of 8 reads lane 7 - i: the other quad
 
 template <int D, bool kInt8>
-__global__ __launch_bounds__(kThreads) void quant_store_kernel(QuantParams p, int64_t rows) {
+__global__ __launch_bounds__(kThreads) void quant_store_kernel(QuantParams p, uint32_t rows) {
   constexpr int kLanes = D / 16;
-  const int64_t row = (int64_t(blockIdx.x) * kThreads + threadIdx.x) / kLanes;
+  const uint32_t row = blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes;
   const int part = threadIdx.x % kLanes;
   // Every lane stays for the row's reduction: rows past the end repeat the last one.
-  Place at;
   const bool in = row < rows;
-  const bool ok = place(p, in ? row : rows - 1, in && part == 0, at) && in;
-  const u32x4* src = reinterpret_cast<const u32x4*>((at.v ? p.v : p.k) + at.at + part * 16);
+  const Row r = row_of(p, in ? row : rows - 1);
+  const u32x4* src = reinterpret_cast<const u32x4*>((r.v ? p.v : p.k) + at_of(p, r) + part * 16);
   const u32x4 x0 = src[0], x1 = src[1];
+  const int64_t slot = slot_of(p, r, in && part == 0);
   const uint32_t w[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
   uint32_t top = 0;   // bf16 magnitudes order as their bit patterns
 #pragma unroll
@@ -107,20 +116,22 @@ __global__ __launch_bounds__(kThreads) void quant_store_kernel(QuantParams p, in
       }
     }
   }
-  if (!ok) return;
-  *reinterpret_cast<u32x4*>(p.codes + at.slot * D + part * 16) = codes;
-  if (part == 0) p.scales[at.slot] = scale;
+  if (!in || slot < 0) return;
+  *reinterpret_cast<u32x4*>(p.codes + slot * D + part * 16) = codes;
+  if (part == 0) p.scales[slot] = scale;
 }
 
-template <int D, bool kInt8>
-__global__ __launch_bounds__(kThreads) void quant_load_kernel(QuantParams p, int64_t rows) {
+template <int D, bool kInt8, bool kNt>
+__global__ __launch_bounds__(kThreads) void quant_load_kernel(QuantParams p, uint32_t rows) {
   constexpr int kLanes = D / 16;
-  const int64_t row = (int64_t(blockIdx.x) * kThreads + threadIdx.x) / kLanes;
+  const uint32_t row = blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes;
   const int part = threadIdx.x % kLanes;
-  Place at;
-  if (row >= rows || !place(p, row, part == 0, at)) return;
-  const u32x4 codes = *reinterpret_cast<const u32x4*>(p.codes + at.slot * D + part * 16);
-  const float scale = p.scales[at.slot];
+  if (row >= rows) return;
+  const Row r = row_of(p, row);
+  const int64_t slot = slot_of(p, r, part == 0);
+  if (slot < 0) return;
+  const u32x4 codes = *reinterpret_cast<const u32x4*>(p.codes + slot * D + part * 16);
+  const float scale = p.scales[slot];
   uint32_t w[8];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -136,21 +147,28 @@ __global__ __launch_bounds__(kThreads) void quant_load_kernel(QuantParams p, int
     w[2 * e] = pack_bf2(f[0] * scale, f[1] * scale);
     w[2 * e + 1] = pack_bf2(f[2] * scale, f[3] * scale);
   }
-  u32x4* dst = reinterpret_cast<u32x4*>((at.v ? p.v_out : p.k_out) + at.at + part * 16);
-  dst[0] = u32x4{w[0], w[1], w[2], w[3]};
-  dst[1] = u32x4{w[4], w[5], w[6], w[7]};
+  u32x4* dst = reinterpret_cast<u32x4*>((r.v ? p.v_out : p.k_out) + at_of(p, r) + part * 16);
+  const u32x4 lo = {w[0], w[1], w[2], w[3]}, hi = {w[4], w[5], w[6], w[7]};
+  if constexpr (kNt) {
+    __builtin_nontemporal_store(lo, dst);
+    __builtin_nontemporal_store(hi, dst + 1);
+  } else {
+    dst[0] = lo;
+    dst[1] = hi;
+  }
 }
 
-int64_t row_count(const QuantParams& p) { return int64_t(p.tokens) * 2 * p.Hkv; }
+uint32_t row_count(const QuantParams& p) { return static_cast<uint32_t>(p.tokens) * 2 * p.Hkv; }
 unsigned groups(const QuantParams& p) {
-  return static_cast<unsigned>((row_count(p) * (p.d / 16) + kThreads - 1) / kThreads);
+  const uint32_t per = kThreads / (p.d / 16);
+  return (row_count(p) + per - 1) / per;
 }
 
 }  // namespace
 
 hipError_t launch_quant_store(const QuantParams& p, hipStream_t s) {
   if (p.tokens == 0) return hipSuccess;
-  const int64_t rows = row_count(p);
+  const uint32_t rows = row_count(p);
   const unsigned grid = groups(p);
   if (p.d == 128 && p.int8) quant_store_kernel<128, true><<<grid, kThreads, 0, s>>>(p, rows);
   else if (p.d == 128) quant_store_kernel<128, false><<<grid, kThreads, 0, s>>>(p, rows);
@@ -160,14 +178,23 @@ hipError_t launch_quant_store(const QuantParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
+namespace {
+
+template <int D, bool kInt8>
+void load(const QuantParams& p, hipStream_t s) {
+  const uint32_t rows = row_count(p);
+  if (int64_t(rows) * D * 2 >= kNtStoreBytes) quant_load_kernel<D, kInt8, true><<<groups(p), kThreads, 0, s>>>(p, rows);
+  else quant_load_kernel<D, kInt8, false><<<groups(p), kThreads, 0, s>>>(p, rows);
+}
+
+}  // namespace
+
 hipError_t launch_quant_load(const QuantParams& p, hipStream_t s) {
   if (p.tokens == 0) return hipSuccess;
-  const int64_t rows = row_count(p);
-  const unsigned grid = groups(p);
-  if (p.d == 128 && p.int8) quant_load_kernel<128, true><<<grid, kThreads, 0, s>>>(p, rows);
-  else if (p.d == 128) quant_load_kernel<128, false><<<grid, kThreads, 0, s>>>(p, rows);
-  else if (p.d == 64 && p.int8) quant_load_kernel<64, true><<<grid, kThreads, 0, s>>>(p, rows);
-  else if (p.d == 64) quant_load_kernel<64, false><<<grid, kThreads, 0, s>>>(p, rows);
+  if (p.d == 128 && p.int8) load<128, true>(p, s);
+  else if (p.d == 128) load<128, false>(p, s);
+  else if (p.d == 64 && p.int8) load<64, true>(p, s);
+  else if (p.d == 64) load<64, false>(p, s);
   else return hipErrorInvalidValue;
   return hipGetLastError();
 }

@@ -16,8 +16,19 @@ namespace pallas {
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kPasses = 5;   // units of a thread whose loads are in flight together
+constexpr int kThreads = 256;   // at most
+constexpr int kPasses = 3;      // units of a thread whose loads are in flight together
+
+// Outputs from this many bytes on are stored non-temporally (111 MB read and written: 21.1
+// us, 26.8 with plain stores; 164 MB: 34.1, 38.4); smaller ones stay in the caches for what
+// reads them next.
+constexpr int64_t kNtStoreBytes = int64_t(4) << 20;
+
+template <bool kNt, class V>
+__device__ __forceinline__ void put(V v, void* at) {
+  if constexpr (kNt) __builtin_nontemporal_store(v, static_cast<V*>(at));
+  else *static_cast<V*>(at) = v;
+}
 
 // (cos, sin) of an angle of `a` 2^-64 turns, times m.  |rest| <= pi / 4: the first
 // terms left out are below 2^-29 (sine, x^11 / 11!) and 2^-32 (cosine, x^12 / 12!)
@@ -51,7 +62,9 @@ __device__ __forceinline__ uint64_t turned(const RopeParams& p, int pos, int i) 
 // 8 elements behind the rotated ones.  `units` of a head are worked on (the
 // copied ones only where y is not x).  A thread keeps its unit, and so its four
 // angles, for all the heads that it takes: `slots` heads of a token go side by
-// side (several tokens where a token has fewer), kPasses times.
+// side (several tokens where a token has fewer), kPasses times.  The first loads are
+// issued before the angles are worked out.
+template <bool kNt>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeParams p, int units, int slots, int tokens_per, int heads_per) {
   const int j = threadIdx.x % units, slot = threadIdx.x / units;
   const int t = blockIdx.x * tokens_per + (tokens_per > 1 ? slot / p.heads : 0);
@@ -63,14 +76,8 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeParams p, int units,
   const int lo = half ? 4 * j : 8 * j, hi = half ? p.r / 2 + 4 * j : 8 * j + 4;
   const uint16_t* x = p.x + t * p.x_token;
   uint16_t* y = p.y + t * p.y_token;
-  float c[4], s[4];
-  if (turn) {
-    const int pos = p.pos[t];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) turn_cos_sin(turned(p, pos, 4 * j + e), p.magnitude, c[e], s[e]);
-  }
-  for (; h < h1; h += kPasses * slots) {
-    u32x2 a[kPasses], b[kPasses];
+  u32x2 a[kPasses], b[kPasses];
+  auto read = [&] {
 #pragma unroll
     for (int k = 0; k < kPasses; ++k) {
       if (h + k * slots >= h1) continue;
@@ -78,6 +85,15 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeParams p, int units,
       a[k] = *reinterpret_cast<const u32x2*>(src + lo);
       b[k] = *reinterpret_cast<const u32x2*>(src + hi);
     }
+  };
+  read();
+  float c[4], s[4];
+  if (turn) {
+    const int pos = p.pos[t];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) turn_cos_sin(turned(p, pos, 4 * j + e), p.magnitude, c[e], s[e]);
+  }
+  for (;;) {
 #pragma unroll
     for (int k = 0; k < kPasses; ++k) {
       if (h + k * slots >= h1) continue;
@@ -102,33 +118,33 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeParams p, int units,
         b[k] = u32x2{pack_bf2(w[4], w[5]), pack_bf2(w[6], w[7])};
       }
       uint16_t* dst = y + (h + k * slots) * p.y_head;
-      *reinterpret_cast<u32x2*>(dst + lo) = a[k];
-      *reinterpret_cast<u32x2*>(dst + hi) = b[k];
+      put<kNt>(a[k], dst + lo);
+      put<kNt>(b[k], dst + hi);
     }
+    h += kPasses * slots;
+    if (h >= h1) return;
+    read();
   }
 }
 
-// The same a pair (or two copied elements, the last alone in an odd head) at a
-// time, for any alignment.
-__global__ __launch_bounds__(kThreads) void rope_any_kernel(RopeParams p) {
-  const int t = blockIdx.x;
-  const bool copy = p.x != p.y;
-  const int units = p.r / 2 + (copy ? (p.d - p.r + 1) / 2 : 0);
+// The same with units of a pair (or of two copied elements, the last alone in an odd
+// head), for any alignment; heads of more units than threads take them in turns.
+__global__ __launch_bounds__(kThreads) void rope_any_kernel(RopeParams p, int units, int slots, int heads_per) {
+  const int t = blockIdx.x, slot = threadIdx.x / units;
+  const int h0 = blockIdx.y * heads_per, h1 = min(p.heads, h0 + heads_per);
+  if (slot >= slots) return;
   const int pos = p.pos[t];
-  for (int e = blockIdx.y * kThreads + threadIdx.x; e < units * p.heads; e += gridDim.y * kThreads) {
-    const int h = e / units, i = e - h * units;
-    const uint16_t* x = p.x + t * p.x_token + h * p.x_head;
-    uint16_t* y = p.y + t * p.y_token + h * p.y_head;
-    if (2 * i < p.r) {
-      const int lo = p.interleaved ? 2 * i : i, hi = p.interleaved ? 2 * i + 1 : i + p.r / 2;
-      float c, s;
-      turn_cos_sin(turned(p, pos, i), p.magnitude, c, s);
-      const float x0 = bf2f(x[lo]), x1 = bf2f(x[hi]);
-      y[lo] = f2bf(x0 * c - x1 * s);
-      y[hi] = f2bf(x1 * c + x0 * s);
-    } else {
-      y[2 * i] = x[2 * i];
-      if (2 * i + 1 < p.d) y[2 * i + 1] = x[2 * i + 1];
+  for (int i = threadIdx.x % units; i < units; i += kThreads) {
+    const bool turn = 2 * i < p.r;
+    const int lo = !turn || p.interleaved ? 2 * i : i, hi = !turn || p.interleaved ? 2 * i + 1 : i + p.r / 2;
+    float c = 1.f, s = 0.f;
+    if (turn) turn_cos_sin(turned(p, pos, i), p.magnitude, c, s);
+    for (int h = h0 + slot; h < h1; h += slots) {
+      const uint16_t* x = p.x + t * p.x_token + h * p.x_head;
+      uint16_t* y = p.y + t * p.y_token + h * p.y_head;
+      const uint16_t a = x[lo], b = hi < p.d ? x[hi] : 0;
+      y[lo] = turn ? f2bf(bf2f(a) * c - bf2f(b) * s) : a;
+      if (hi < p.d) y[hi] = turn ? f2bf(bf2f(b) * c + bf2f(a) * s) : b;
     }
   }
 }
@@ -140,20 +156,28 @@ hipError_t launch_rope(const RopeParams& p, hipStream_t s) {
   auto by = [](const void* q, int64_t a, int64_t b) {
     return (reinterpret_cast<uintptr_t>(q) & 15) == 0 && a % 8 == 0 && b % 8 == 0;
   };
+  const bool copy = p.x != p.y;
   if (p.r % 8 != 0 || p.d % 8 != 0 || p.d > 8 * kThreads || !by(p.x, p.x_token, p.x_head) ||
       !by(p.y, p.y_token, p.y_head)) {
-    const int64_t units = (int64_t(p.d) + 1) / 2 * p.heads;
-    const dim3 grid(p.tokens, static_cast<unsigned>(std::min<int64_t>((units + kThreads - 1) / kThreads, 64)));
-    rope_any_kernel<<<grid, kThreads, 0, s>>>(p);
+    const int units = p.r / 2 + (copy ? (p.d - p.r + 1) / 2 : 0);
+    const int slots = std::max(kThreads / units, 1);
+    const int heads_per = p.tokens < 512 ? slots : p.heads;
+    rope_any_kernel<<<dim3(p.tokens, (p.heads + heads_per - 1) / heads_per), kThreads, 0, s>>>(p, units, slots, heads_per);
     return hipGetLastError();
   }
-  const int units = p.x == p.y ? p.r / 8 : p.d / 8;
-  const int slots = kThreads / units;
-  const int tokens_per = std::max(1, slots / p.heads);
+  // Workgroups as wide as a token's heads fill evenly.
+  const int units = copy ? p.d / 8 : p.r / 8;
+  const int most = kThreads / units, passes = (p.heads + most - 1) / most;
+  const int tokens_per = std::max(most / p.heads, 1);
+  const int slots = tokens_per > 1 ? tokens_per * p.heads : (p.heads + passes - 1) / passes;
   // Few tokens: a token's heads over several workgroups.
   const int heads_per = p.tokens < 512 ? slots : p.heads;
   const dim3 grid((p.tokens + tokens_per - 1) / tokens_per, tokens_per > 1 ? 1 : (p.heads + heads_per - 1) / heads_per);
-  rope_kernel<<<grid, kThreads, 0, s>>>(p, units, slots, tokens_per, heads_per);
+  const int threads = (units * slots + 63) / 64 * 64;
+  if (int64_t(p.tokens) * p.heads * units * 16 >= kNtStoreBytes)
+    rope_kernel<true><<<grid, threads, 0, s>>>(p, units, slots, tokens_per, heads_per);
+  else
+    rope_kernel<false><<<grid, threads, 0, s>>>(p, units, slots, tokens_per, heads_per);
   return hipGetLastError();
 }
 

@@ -120,6 +120,7 @@ def test_quant_refusals(P, name):
     for bad in (dict(head_dim=96), dict(head_dim=256), dict(page_size=32), dict(n_kv_heads=4097)):
         assert quant_rc(P, name, quant_pool(**bad)) == S.UNSUPPORTED, bad
     assert quant_rc(P, name, pool=0) == S.INVALID_ARG
+    assert quant_rc(P, name, tokens=1 << 28) == S.UNSUPPORTED          # 2^31 rows
     assert quant_rc(P, name, tokens=0) == S.OK           # nothing to do
 
 
@@ -189,7 +190,7 @@ def test_attend_workspace(P):
                     blocks[rng.integers(s)] = -(-n // 32)
                     total = int(blocks.sum())
                     rounds = max(-(-total // (32 * ranges)), 1)
-                    each = 1 if 2 * total <= ranges else 2 if total <= 2 * ranges else -(-total // (ranges * rounds))
+                    each = 1 if 2 * total <= ranges and total <= 32 * s else 2 if total <= 2 * ranges else -(-total // (ranges * rounds))
                     assert each <= 32
                     last = -(-total // each) - 1 + s - 1                # the largest range + sequence
                     assert size(s, hq, hkv, d, n) >= 8 * s + (last + 1) * hq * (d + 2) * 4
