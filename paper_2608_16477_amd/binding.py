@@ -358,11 +358,12 @@ def _packed_rows(t, what: str, dev: int, shape):
 def _launch(dev: int, stream, call, *args):
     """``call(*args, stream)`` with the tensors' GPU current, on its current stream unless one is given."""
     cuda = _torch.cuda
+    handle = cuda.current_stream(dev).cuda_stream if stream is None else _stream(stream)
     if cuda.current_device() == dev:
-        _check(call(*args, _stream(stream)))
+        _check(call(*args, handle))
     else:
         with cuda.device(dev):
-            _check(call(*args, _stream(stream)))
+            _check(call(*args, handle))
 
 
 def pallas_rope_init(rotary_dim: int, theta: float, layout: str = "half", scaling: str = "none", factor: float = 1.0,
