@@ -254,11 +254,21 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
     vb0 = static_cast<uint32_t>(key * D + v_slot<T, CH>(key) * 16 + (l16 & 1) * 8);
   }
 
-  // All blocks of the call, and the ranges they make.
+  // All blocks of the call, and the ranges they make.  coarse: blocks of the first (lane +
+  // 1) 64ths of the sequences.
   int before = wave_prefix(blocks_of(lens));    // blocks of the window's sequences, up to and with each
-  int total = __builtin_amdgcn_readlane(before, 63);
-  for (int at = 64; at < p.seqs; at += 64)
-    total += __builtin_amdgcn_readlane(wave_prefix(blocks_of(lane_length(p, at))), 63);
+  int coarse = before;
+  const int share = static_cast<int>(static_cast<uint32_t>(p.seqs + 63) / 64);
+  if (share > 1) {
+    int sum = 0;
+#pragma unroll 8
+    for (int n = 0; n < share; ++n) {
+      const int q = lane * share + n, len = row_length(p, min(q, p.seqs - 1));
+      sum += q < p.seqs ? blocks_of(len) : 0;
+    }
+    coarse = wave_prefix(sum);
+  }
+  const int total = __builtin_amdgcn_readlane(coarse, 63);
   const int each = attend_blocks(total, p.seqs, p.ranges);
   auto window = [&](int s) {                    // makes s one of the 64
     if (s >= win && s < win + 64) return;
@@ -273,6 +283,14 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
   int s = 0, base = 0;                          // a sequence, and the blocks before it
   // Moves them on to the sequence that block f (of the call's) is in.
   auto seek = [&](int f) {
+    if (share > 1) {
+      const uint64_t behind = __builtin_amdgcn_ballot_w64(coarse > f);
+      const int n = behind != 0 ? __builtin_ctzll(behind) : 0;
+      if (n * share > s) {
+        s = n * share;
+        base = __builtin_amdgcn_readlane(coarse, n - 1);
+      }
+    }
     while (s < p.seqs) {
       window(s);
       // blocks of the window before s
