@@ -393,11 +393,12 @@ int pallas_rope_init(const pallas_rope_config* cfg, pallas_rope_plan* plan);
  * (elements, >= 0) and goes to the same place of d_y and its strides.  d_y may be
  * d_x with the same strides (in place); otherwise heads read and heads written
  * must not overlap.  d_positions (int32, device, [num_tokens]) may hold any
- * int32; angles are exact to 2^-32 turn at every one.  inverse = 1 takes a
+ * int32; angles are exact to 2^-31 turn at every one.  inverse = 1 takes a
  * rotation by the same plan and position back (angle -p f_i, factor 1 / m), so
  * it also moves a cached K row: back from p, then on to q.  Rounded once, from
  * float32.  2-byte alignment suffices; pointers 16-byte aligned, strides and
- * head_dim multiples of 8 and rotary_dim a multiple of 8 are faster. */
+ * head_dim multiples of 8 and rotary_dim a multiple of 8 are faster.  num_tokens
+ * below 2^24, n_heads * head_dim at most 2^20 (UNSUPPORTED). */
 int pallas_rope_apply(const pallas_rope_plan* plan, int32_t inverse, int32_t num_tokens,
                       int32_t n_heads, int32_t head_dim, const int32_t* d_positions,
                       const void* d_x, int64_t x_token_stride, int64_t x_head_stride, void* d_y,
@@ -440,7 +441,8 @@ typedef struct {
  * [0, num_seqs), a position beyond the table, or an entry outside [0, num_pages)
  * is skipped too and raises PALLAS_DEVERR_PAGE in *d_err (nullable).  Nothing
  * else of the pool is written.  What a slot gets that two tokens of one call
- * name is undefined.  num_tokens * 2 * n_kv_heads below 2^31 (UNSUPPORTED). */
+ * name is undefined.  num_tokens * 2 * n_kv_heads * head_dim below
+ * 2^35 (UNSUPPORTED). */
 int pallas_quant_store(const pallas_quant_pool* pool, int32_t layer, int32_t num_tokens,
                        const int32_t* d_seq_ids, const int32_t* d_positions, const void* d_k,
                        int64_t k_stride, const void* d_v, int64_t v_stride, int32_t num_seqs,

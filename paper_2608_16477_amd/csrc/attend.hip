@@ -2,17 +2,21 @@
 // INT8 rows).
 //
 // The kernel is bound by the K/V stream, so the stream is what is divided: the 32-key
-// blocks of all sequences, one behind the other, are cut into ranges of equal length,
-// as many as waves are resident at once (attend_plan), and a wave takes a range of one
-// KV head and up to 16 query heads that share it.  It streams its blocks without a
-// pause, also where one sequence ends and the next begins, as an online softmax per
-// sequence, in registers; no wave waits for another.  What it has of a sequence that
-// lies in its range as a whole is the result, anything else a record, which a second
-// launch joins in order.  Ranges follow from the lengths alone and nothing is counted
-// or accumulated across waves.
-//   Against a workgroup per (split of a sequence, KV head), with splits sized by a row's
-// own length (the first form), us: 64 sequences of 500 to 8000 keys, E4M3, 64 / 8 heads,
-// 87 -> XX; 131,071 keys INT8 65 -> XX; 8 sequences bf16 32 -> XX.
+// blocks of all sequences, one behind the other, are cut into ranges of equal length
+// (attend_blocks), as many as waves are resident at once (attend_ranges), and a wave
+// takes a range of one KV head and up to 16 query heads that share it.  Its loads go on
+// where one sequence ends and the next begins; each sequence is an online softmax in
+// registers, and no wave waits for another.  What a wave has of a sequence that lies in
+// its range as a whole is the result, anything else a record, which a second launch
+// joins in order.  Ranges follow from the lengths alone and nothing is counted or
+// accumulated across waves, so results are the same in every run.
+//   us of a call, against a workgroup per KV head and split of a sequence, of a length
+// that followed from the sequence's own (the first form): 64 sequences of 500 to 8000
+// keys, E4M3, 64 / 8 heads of 128 (344 MB), 87 -> 68; 131,071 keys INT8 (277 MB) 65 -> 57; 60,001
+// and 33,333 keys bf16, 32 / 8 heads (383 MB), 79 -> 69; 8 sequences of 1000 to 8000 keys
+// bf16 (106 MB) 32 -> 28; one of 4000 keys bf16 11.2 -> 12.6; one of 500 keys 8.0, both.  The
+// first launch of the first four reads what it has to and no more, at 5.6, 5.7, 5.9 and 4.8
+// TB/s; the join takes 4 to 5.  LDS has no bank conflict.
 //
 // Each wave moves its blocks from memory straight into a private two-stage LDS ring,
 // with the rows' scales.  Scores are S^T = K Q^T with v_mfma_f32_16x16x32_bf16 (the
@@ -50,7 +54,7 @@ struct Shape {
   static constexpr int kSlots = 2 * kBlk * kCh + kScaleSlots;    // 16-byte slots of a stage
   static constexpr int kLoads = 4 * kPerPage + (T == kCacheBf16 ? 0 : 1);   // instructions per block
   static constexpr int kRing = kStages * kSlots;                 // of a wave
-  // attend_plan counts on the waves that a CU's 160 KiB of LDS hold.
+  // attend_ranges counts on the waves that a CU's 160 KiB of LDS hold.
   static_assert(160 * 1024 / (4 * kRing * 16) * 4 >= attend_waves(kRow), "resident waves");
 };
 
@@ -212,9 +216,9 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int q4 = lane >> 4, l16 = lane & 15;
   // A workgroup's waves take the same range of four heads (of two or one where the heads
-  // are not a multiple): those rows are neighbours in memory, and share scale lines, table
-  // entries and address translations (64 sequences E4M3: 62 us; 65 to 72 with four ranges
-  // of one head).  Workgroups of one blockIdx.x go to one XCD.
+  // are not a multiple), whose rows are neighbours in memory and share scale lines and table
+  // entries; workgroups of one blockIdx.x, the range's other heads, go to one XCD.  (64
+  // sequences E4M3, first launch: 62 us; 65 to 72 with four ranges of one head.)
   const int head = (static_cast<int>(blockIdx.y) << head_shift) + (wave & ((1 << head_shift) - 1));
   const int kh = groups == 1 ? head : head / groups, group = head - kh * groups;
   const int r0 = static_cast<int>(blockIdx.x) * (kWaves >> head_shift) + (wave >> head_shift);

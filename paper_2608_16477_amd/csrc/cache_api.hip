@@ -55,9 +55,12 @@ int quant_call(bool store, const pallas_quant_pool* pool, int32_t layer, int32_t
     return fail(PALLAS_ERR_INVALID_ARG, "%s: rows not 16-byte aligned", what);
   if (k_stride < row || v_stride < row)
     return fail(PALLAS_ERR_INVALID_ARG, "%s: row stride below the %lld elements of a row", what, (long long)row);
-  if (int64_t(num_tokens) * 2 * pool->n_kv_heads >= (int64_t(1) << 31))
-    return fail(PALLAS_ERR_UNSUPPORTED, "%s: %d tokens of %d K and V rows (below 2^31 rows in all)", what, num_tokens,
-                2 * pool->n_kv_heads);
+  if (!aligned(d_seq_ids, 4) || !aligned(d_positions, 4) || !aligned(d_block_tables, 4) || !aligned(d_err, 4))
+    return fail(PALLAS_ERR_INVALID_ARG, "%s: sequence ids, positions, tables or d_err not 4-byte aligned", what);
+  // A launch has fewer than 2^32 threads, 16 elements each.
+  if (int64_t(num_tokens) * 2 * row >= (int64_t(1) << 35))
+    return fail(PALLAS_ERR_UNSUPPORTED, "%s: %d tokens of %lld K and V elements (below 2^35 in all)", what, num_tokens,
+                (long long)(2 * row));
   pallas::QuantParams p{};
   p.codes = static_cast<uint8_t*>(pool->codes) + 2 * layer * plane_rows(pool) * pool->head_dim;
   p.scales = pool->scales + 2 * layer * plane_rows(pool);
@@ -134,7 +137,8 @@ int attend_call(const char* what, pallas::CacheType type, pallas::AttendParams& 
   if (max_length > int64_t(max_pages) * page_size)
     return fail(PALLAS_ERR_OUT_OF_RANGE, "%s: max_length %d outside the table (%lld)", what, max_length,
                 (long long)(int64_t(max_pages) * page_size));
-  if (!std::isfinite(scale)) return fail(PALLAS_ERR_INVALID_ARG, "%s: scale is not finite", what);
+  p.scale_log2 = static_cast<float>(double(scale) * 1.4426950408889634);
+  if (!std::isfinite(p.scale_log2)) return fail(PALLAS_ERR_INVALID_ARG, "%s: scale is not finite", what);
   if (!d_workspace || !aligned(d_workspace, 256))
     return fail(PALLAS_ERR_INVALID_ARG, "%s: workspace null or not 256-byte aligned", what);
   const AttendSpace sp = attend_space(num_seqs, n_q_heads, p.d, max_length, most_ranges(n_q_heads, p.Hkv, p.d));
@@ -149,7 +153,6 @@ int attend_call(const char* what, pallas::CacheType type, pallas::AttendParams& 
   p.q_stride = q_stride;
   p.lengths = d_lengths;
   p.bt = d_block_tables;
-  p.scale_log2 = static_cast<float>(double(scale) * 1.4426950408889634);
   p.out = static_cast<uint16_t*>(d_out);
   p.out_stride = out_stride;
   p.lse = d_lse;
@@ -238,8 +241,9 @@ int pallas_rope_apply(const pallas_rope_plan* plan, int32_t inverse, int32_t num
     return fail(PALLAS_ERR_INVALID_ARG, "rope: output strides below a head of %d", head_dim);
   if (d_x == d_y && (x_token_stride != y_token_stride || x_head_stride != y_head_stride))
     return fail(PALLAS_ERR_INVALID_ARG, "rope: in place with other strides");
-  if (int64_t(n_heads) * head_dim > (int64_t(1) << 30))
-    return fail(PALLAS_ERR_UNSUPPORTED, "rope: %d heads of %d", n_heads, head_dim);
+  if (int64_t(n_heads) * head_dim > (int64_t(1) << 20) || num_tokens >= (1 << 24))
+    return fail(PALLAS_ERR_UNSUPPORTED, "rope: %d tokens (below 2^24) of %d heads of %d (at most 2^20 elements)", num_tokens,
+                n_heads, head_dim);
   pallas::RopeParams p;
   p.x = static_cast<const uint16_t*>(d_x);
   p.y = static_cast<uint16_t*>(d_y);

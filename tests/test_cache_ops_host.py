@@ -83,7 +83,8 @@ def test_rope_refusals(P, bad):
 
 
 def test_rope_limits(P):
-    assert rope_rc(P, heads=1 << 25) == P.Status.UNSUPPORTED
+    assert rope_rc(P, heads=(1 << 14) + 1) == P.Status.UNSUPPORTED
+    assert rope_rc(P, tokens=1 << 24) == P.Status.UNSUPPORTED
     assert rope_rc(P, tokens=0) == P.Status.OK           # nothing to do: nothing is touched
 
 
@@ -120,7 +121,9 @@ def test_quant_refusals(P, name):
     for bad in (dict(head_dim=96), dict(head_dim=256), dict(page_size=32), dict(n_kv_heads=4097)):
         assert quant_rc(P, name, quant_pool(**bad)) == S.UNSUPPORTED, bad
     assert quant_rc(P, name, pool=0) == S.INVALID_ARG
-    assert quant_rc(P, name, tokens=1 << 28) == S.UNSUPPORTED          # 2^31 rows
+    assert quant_rc(P, name, tokens=1 << 26) == S.UNSUPPORTED          # 2^35 elements
+    for bad in (dict(seq=FAKE + 2), dict(pos=FAKE + 1), dict(bt=FAKE + 2)):
+        assert quant_rc(P, name, **bad) == S.INVALID_ARG, bad
     assert quant_rc(P, name, tokens=0) == S.OK           # nothing to do
 
 
@@ -144,7 +147,7 @@ def test_attend_refusals(P, quant):
     S = P.Status
     for bad in (dict(seqs=0), dict(heads=0), dict(heads=6), dict(max_length=0), dict(q=None), dict(lens=None),
                 dict(bt=None), dict(out=None), dict(max_pages=0), dict(q=FAKE + 8), dict(out=FAKE + 4), dict(qs=516),
-                dict(os=508), dict(qs=504), dict(os=0), dict(scale=math.inf), dict(scale=math.nan), dict(ws=None),
+                dict(os=508), dict(qs=504), dict(os=0), dict(scale=math.inf), dict(scale=math.nan), dict(scale=3e38), dict(ws=None),
                 dict(ws=FAKE + 16), dict(lens=FAKE + 2), dict(lse=FAKE + 1)):
         assert attend_rc(P, quant, **bad) == S.INVALID_ARG, bad
         assert "attend" in P.pallas_last_error()
