@@ -138,51 +138,213 @@ __device__ __forceinline__ float join_weight(float m, float l, float top) {
   return m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m - top);
 }
 
-// A wave's range: what it takes to load its blocks.  Lane 2 i + h: half h (a page) of
-// block i of the range.
-struct Source {
-  const char* k;        // layer planes, at this KV head
-  const char* v;
-  uint32_t rs;          // bytes between tokens of a page
-  int64_t page_bytes;
-  int page;             // its page
-  int keys;             // keys in it, 0 for a page outside the pool
-};
-
-// Loads of block `i` of the range into a stage: rows that exist; everything else reads
-// zeros, as do blocks that are not `in` the range.  Every step issues its loads, so that
-// those in flight can be counted.
-template <int D, CacheType T>
-__device__ __forceinline__ void issue_block(const AttendParams& p, const Source& src, __amdgpu_buffer_rsrc_t scales, int kh,
-                                            int i, bool in, const uint32_t* koff, const uint32_t* voff, u32x4* st) {
+// What a wave works with: where the blocks that it takes are, what each lane loads and
+// reads of a block, and the softmax of the sequence that it is in.  (kOf: a type for each
+// kernel.  Of kernels that share one, the compiler's host pass emits the stub of the first
+// alone.)
+template <int D, CacheType T, int kOf>
+struct Wave {
   using S = Shape<D, T>;
-  int pg[2], nv[2];
+  static constexpr int CH = S::kCh, DT = D / 16;
+  const char* k;          // layer planes, at this KV head
+  const char* v;
+  uint32_t rs;            // bytes between tokens of a page
+  int kh;
+  int page, keys;         // lane 2 i + h: page of half h of block i, and the keys in it (0: none, or no page of the pool)
+  uint32_t koff[S::kPerPage], voff[2 * S::kPerPage];   // byte offset in a page of what this lane loads in an instruction
+  uint32_t kb0, vb0;      // where this lane reads: a K block at (row l16, chunk q4), a V block transposed
+  u32x4* ring;
+  u32x4 qf[D / 32];
+  f32x4 acc[DT];          // lane: dimensions 16 dt + 4 q4 .. + 3 of head l16
+  float m, lsum;          // (lsum: of this lane's keys)
+
+  __device__ __forceinline__ void init(const AttendParams& p, int head, u32x4* at) {
+    const int lane = threadIdx.x & 63, q4 = lane >> 4, l16 = lane & 15;
+    kh = head;
+    rs = static_cast<uint32_t>(p.Hkv) * S::kRow;
+    k = static_cast<const char*>(p.k) + int64_t(kh) * S::kRow;
+    v = static_cast<const char*>(p.v) + int64_t(kh) * S::kRow;
+    ring = at;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    pg[h] = __builtin_amdgcn_readlane(src.page, (i * 2 + h) & 63);
-    nv[h] = in ? __builtin_amdgcn_readlane(src.keys, (i * 2 + h) & 63) : 0;
-    const uint32_t range = nv[h] > 0 ? static_cast<uint32_t>(nv[h] - 1) * src.rs + S::kRow : 0;
-    const int64_t base = nv[h] > 0 ? pg[h] * src.page_bytes : 0;
-    const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc((void*)(src.k + base), 0, range, kRsrcFlags);
-    const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void*)(src.v + base), 0, range, kRsrcFlags);
-#pragma unroll
-    for (int v = 0; v < S::kPerPage; ++v)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void*)(st + (h * S::kPerPage + v) * 64), 16, koff[v], 0, 0, kAuxStream);
-#pragma unroll
-    for (int v = 0; v < S::kPerPage; ++v)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void*)(st + kBlk * S::kCh + (h * S::kPerPage + v) * 64), 16,
-                                               voff[h * S::kPerPage + v], 0, 0, kAuxStream);
+    for (int n = 0; n < S::kPerPage; ++n) {
+      const int r = n * S::kRowsPerLoad + lane / CH, c = lane % CH;
+      koff[n] = r * rs + static_cast<uint32_t>((c ^ k_slot<T, CH>(r)) * 16);
+      voff[n] = r * rs + static_cast<uint32_t>((c ^ v_slot<T, CH>(r)) * 16);
+      voff[S::kPerPage + n] = r * rs + static_cast<uint32_t>((c ^ v_slot<T, CH>(kPage + r)) * 16);
+    }
+    kb0 = static_cast<uint32_t>(l16 * CH + (q4 ^ k_slot<T, CH>(l16)));
+    if constexpr (T == kCacheBf16) {
+      const int key = 4 * q4 + (l16 >> 2);
+      vb0 = static_cast<uint32_t>(key * D * 2 + ((v_slot<T, CH>(key) | ((l16 & 3) >> 1)) * 16) + (l16 & 1) * 8);
+    } else {
+      const int key = (l16 >> 3) * kPage + 4 * q4 + ((l16 >> 1) & 3);
+      vb0 = static_cast<uint32_t>(key * D + v_slot<T, CH>(key) * 16 + (l16 & 1) * 8);
+    }
   }
-  if constexpr (T != kCacheBf16) {
-    // Lane l: the K (below 32) or V scale of key l % 32.
-    const int lane = threadIdx.x & 63, key = lane % kPage;
-    const bool second = lane & kPage;
-    const uint32_t page = second ? pg[1] : pg[0];
-    const uint32_t row = ((lane < 32 ? page : page + p.num_pages) * kPage + key) * p.Hkv + kh;
-    const bool live = key < (second ? nv[1] : nv[0]);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(scales, (lds_void*)(st + 2 * kBlk * S::kCh), 4, live ? row * 4 : kOutside, 0, 0, 0);
+
+  // Q: the MFMA's B operand, column l16 = head h0 + l16 of nh (the last one again where
+  // there are fewer).  Its dimensions follow what a lane reads of K: bf16, chunk 4 kk + q4;
+  // 8 bits, half kk % 2 of chunk 4 (kk / 2) + q4.
+  __device__ __forceinline__ void load_q(const AttendParams& p, int s, int h0, int nh) {
+    const int lane = threadIdx.x & 63, q4 = lane >> 4, l16 = lane & 15;
+    const uint16_t* q = p.q + s * p.q_stride + int64_t(h0 + min(l16, nh - 1)) * D;
+#pragma unroll
+    for (int kk = 0; kk < D / 32; ++kk)
+      qf[kk] = *reinterpret_cast<const u32x4*>(q + (T == kCacheBf16 ? 32 * kk + 8 * q4 : 64 * (kk / 2) + 16 * q4 + 8 * (kk % 2)));
   }
-}
+  // Waited for once, where this stands, and not inside the stream.
+  __device__ __forceinline__ void await_q() {
+#pragma unroll
+    for (int kk = 0; kk < D / 32; ++kk) asm volatile("" : "+v"(qf[kk]));
+  }
+
+  __device__ __forceinline__ void begin() {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) acc[dt] = f32x4{};
+    m = -INFINITY;
+    lsum = 0.f;
+  }
+
+  // Loads of block `i` into a stage: rows that exist; everything else reads zeros, as do
+  // blocks that are not `in`.  Every step issues its loads, so that those in flight can be
+  // counted.
+  __device__ __forceinline__ void issue(const AttendParams& p, int i, bool in, int stage) const {
+    u32x4* const st = ring + stage * S::kSlots;
+    int pg[2], nv[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      pg[h] = __builtin_amdgcn_readlane(page, (i * 2 + h) & 63);
+      nv[h] = in ? __builtin_amdgcn_readlane(keys, (i * 2 + h) & 63) : 0;
+      const uint32_t range = nv[h] > 0 ? static_cast<uint32_t>(nv[h] - 1) * rs + S::kRow : 0;
+      const int64_t base = nv[h] > 0 ? pg[h] * (int64_t(kPage) * rs) : 0;
+      const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc((void*)(k + base), 0, range, kRsrcFlags);
+      const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void*)(v + base), 0, range, kRsrcFlags);
+#pragma unroll
+      for (int n = 0; n < S::kPerPage; ++n)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void*)(st + (h * S::kPerPage + n) * 64), 16, koff[n], 0, 0, kAuxStream);
+#pragma unroll
+      for (int n = 0; n < S::kPerPage; ++n)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void*)(st + kBlk * CH + (h * S::kPerPage + n) * 64), 16,
+                                                 voff[h * S::kPerPage + n], 0, 0, kAuxStream);
+    }
+    if constexpr (T != kCacheBf16) {
+      // Lane l: the K (below 32) or V scale of key l % 32.
+      const int lane = threadIdx.x & 63, key = lane % kPage;
+      const bool second = lane & kPage;
+      const uint32_t pgl = second ? pg[1] : pg[0];
+      const uint32_t row = ((lane < 32 ? pgl : pgl + p.num_pages) * kPage + key) * p.Hkv + kh;
+      const bool live = key < (second ? nv[1] : nv[0]);
+      const __amdgpu_buffer_rsrc_t scales = __builtin_amdgcn_make_buffer_rsrc(
+          (void*)p.scales, 0, static_cast<uint32_t>(p.num_pages) * (2 * kPage * 4) * p.Hkv, kRsrcFlags);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(scales, (lds_void*)(st + 2 * kBlk * CH), 4, live ? row * 4 : kOutside, 0, 0, 0);
+    }
+  }
+
+  // Blocks [i, stop), block n in stage n % kStages, the loads of the next kStages - 1 in
+  // flight; `blocks`: all that the wave takes.
+  __device__ __forceinline__ void stream(const AttendParams& p, int& i, int stop, int blocks) {
+    const int lane = threadIdx.x & 63, q4 = lane >> 4;
+#pragma unroll 1
+    for (; i < stop; ++i) {
+      const int stage = static_cast<int>(static_cast<unsigned>(i) % kStages);
+      const u32x4* const Kst = ring + stage * S::kSlots;
+      const u32x4* const Vst = Kst + kBlk * CH;
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kStages - 1) * S::kLoads) : "memory");   // this block is here
+      f32x4 sc[2] = {f32x4{}, f32x4{}};
+      if constexpr (T == kCacheBf16) {
+#pragma unroll
+        for (int kk = 0; kk < D / 32; ++kk)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const bf16x8 a = __builtin_bit_cast(bf16x8, Kst[(kb0 ^ (kk * 4u)) + h * (kPage * CH)]);
+            sc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, qf[kk]), sc[h], 0, 0, 0);
+          }
+      } else {
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const u32x4 a = Kst[(kb0 ^ (j * 4u)) + h * (kPage * CH)];
+            sc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_bf16<T>(a.x, a.y), __builtin_bit_cast(bf16x8, qf[2 * j]), sc[h], 0, 0, 0);
+            sc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_bf16<T>(a.z, a.w), __builtin_bit_cast(bf16x8, qf[2 * j + 1]), sc[h], 0, 0, 0);
+          }
+      }
+      float pr[8], vs[8];
+      if constexpr (T == kCacheBf16) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pr[e] = sc[e / 4][e % 4] * p.scale_log2;
+      } else {
+        const f32x4* f = reinterpret_cast<const f32x4*>(Kst + 2 * kBlk * CH);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const f32x4 ks = f[4 * h + q4], w = f[8 + 4 * h + q4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            pr[4 * h + r] = sc[h][r] * (ks[r] * p.scale_log2);
+            vs[4 * h + r] = w[r];
+          }
+        }
+      }
+      const int nv0 = __builtin_amdgcn_readlane(keys, i * 2), nv1 = __builtin_amdgcn_readlane(keys, i * 2 + 1);
+      if (nv0 < kPage || nv1 < kPage) {
+        // Keys past the end, and keys on a page outside the pool.
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (4 * q4 + e >= (h ? nv1 : nv0)) pr[h * 4 + e] = -INFINITY;
+      }
+      float mx = fmaxf(fmaxf(fmaxf(pr[0], pr[1]), fmaxf(pr[2], pr[3])), fmaxf(fmaxf(pr[4], pr[5]), fmaxf(pr[6], pr[7])));
+      mx = rows_max(mx);
+      if (__builtin_amdgcn_ballot_w64(mx > m) != 0) {
+        const float m_new = fmaxf(m, mx);
+        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+        m = m_new;
+        lsum *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) acc[dt] *= alpha;
+      }
+      const float mc = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        pr[e] = __builtin_amdgcn_exp2f(pr[e] - mc);
+        lsum += pr[e];
+        if constexpr (T != kCacheBf16) pr[e] *= vs[e];
+      }
+      bf16x8 pb[2];
+#pragma unroll
+      for (int part = 0; part < 2; ++part) {
+        u32x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = take_bf2(pr[2 * e], pr[2 * e + 1]);
+        pb[part] = __builtin_bit_cast(bf16x8, w);
+      }
+      const uint32_t vst = vb0 + static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)Vst));
+      if constexpr (T == kCacheBf16) {
+        u32x4 va[DT];
+#pragma unroll
+        for (int dt = 0; dt < DT; dt += 4) read_pv4<kPage * D * 2>(vst, dt, va + dt);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int part = 1; part >= 0; --part)
+            acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va[dt]), pb[part], acc[dt], 0, 0, 0);
+      } else {
+        u32x2 vc[DT];
+#pragma unroll
+        for (int dt = 0; dt < DT; dt += 4) read_pv8(vst, dt, vc + dt);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          const bf16x8 a = codes_bf16<T>(vc[dt].x, vc[dt].y);
+#pragma unroll
+          for (int part = 1; part >= 0; --part) acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pb[part], acc[dt], 0, 0, 0);
+        }
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this block's LDS reads are done
+      issue(p, i + kStages, i + kStages < blocks, stage);
+    }
+  }
+};
 
 // Lengths of 64 sequences from `at` on, one per lane, in 32-key blocks (0 behind the last).
 __device__ __forceinline__ int lane_length(const AttendParams& p, int at) {
@@ -207,13 +369,13 @@ __device__ __forceinline__ int wave_prefix(int v) {
 template <int D, CacheType T>
 __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, int groups, int head_shift) {
   using S = Shape<D, T>;
-  constexpr int CH = S::kCh, DT = D / 16;
+  constexpr int DT = D / 16;
   // One array: with several, the compiler's alias scopes make LDS reads of a
   // stage wait for the loads in flight into the other.
   __shared__ __attribute__((aligned(256))) u32x4 lds[kWaves * S::kRing];
 
-  const int t = threadIdx.x, lane = t & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int q4 = lane >> 4, l16 = lane & 15;
   // A workgroup's waves take the same range of four heads (of two or one where the heads
   // are not a multiple), whose rows are neighbours in memory and share scale lines and table
@@ -230,33 +392,8 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
   int win = 0, lens = lane_length(p, 0);        // lens: of sequences [win, win + 64)
 
   const int h0 = kh * p.G + group * kAttendGroup, nh = min(kAttendGroup, p.G - group * kAttendGroup);
-  Source src;
-  src.rs = static_cast<uint32_t>(p.Hkv) * S::kRow;
-  src.page_bytes = int64_t(kPage) * src.rs;
-  src.k = static_cast<const char*>(p.k) + int64_t(kh) * S::kRow;
-  src.v = static_cast<const char*>(p.v) + int64_t(kh) * S::kRow;
-  u32x4* const ring = lds + wave * S::kRing;
-  const __amdgpu_buffer_rsrc_t scales = __builtin_amdgcn_make_buffer_rsrc(
-      (void*)p.scales, 0, static_cast<uint32_t>(p.num_pages) * (2 * kPage * 4) * p.Hkv, kRsrcFlags);
-  // Byte offset in a page of what this lane loads in instruction v of it.
-  uint32_t koff[S::kPerPage], voff[2 * S::kPerPage];
-#pragma unroll
-  for (int v = 0; v < S::kPerPage; ++v) {
-    const int r = v * S::kRowsPerLoad + lane / CH, c = lane % CH;
-    koff[v] = r * src.rs + static_cast<uint32_t>((c ^ k_slot<T, CH>(r)) * 16);
-    voff[v] = r * src.rs + static_cast<uint32_t>((c ^ v_slot<T, CH>(r)) * 16);
-    voff[S::kPerPage + v] = r * src.rs + static_cast<uint32_t>((c ^ v_slot<T, CH>(kPage + r)) * 16);
-  }
-  // Where this lane reads: a K block at (row l16, chunk q4), a V block transposed.
-  const uint32_t kb0 = static_cast<uint32_t>(l16 * CH + (q4 ^ k_slot<T, CH>(l16)));
-  uint32_t vb0;
-  if constexpr (T == kCacheBf16) {
-    const int key = 4 * q4 + (l16 >> 2);
-    vb0 = static_cast<uint32_t>(key * D * 2 + ((v_slot<T, CH>(key) | ((l16 & 3) >> 1)) * 16) + (l16 & 1) * 8);
-  } else {
-    const int key = (l16 >> 3) * kPage + 4 * q4 + ((l16 >> 1) & 3);
-    vb0 = static_cast<uint32_t>(key * D + v_slot<T, CH>(key) * 16 + (l16 & 1) * 8);
-  }
+  Wave<D, T, 0> w;
+  w.init(p, kh, lds + wave * S::kRing);
 
   // All blocks of the call, and the ranges they make.  coarse: blocks of the first (lane +
   // 1) 64ths of the sequences.
@@ -310,26 +447,14 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
       s = win + 64;
     }
   };
-  // Q: the MFMA's B operand, column l16 = a head (the last one again where there are fewer).  Its
-  // dimensions follow what a lane reads of K: bf16, chunk 4 kk + q4; 8 bits, half kk % 2
-  // of chunk 4 (kk / 2) + q4.
-  u32x4 qf[D / 32];
-  auto load_q = [&](int s) {
-    const uint16_t* q = p.q + s * p.q_stride + int64_t(h0 + min(l16, nh - 1)) * D;
-#pragma unroll
-    for (int kk = 0; kk < D / 32; ++kk)
-      qf[kk] = *reinterpret_cast<const u32x4*>(q + (T == kCacheBf16 ? 32 * kk + 8 * q4 : 64 * (kk / 2) + 16 * q4 + 8 * (kk % 2)));
-  };
 
   for (int r = r0; r * each < total; r += p.ranges) {
-  const int f0 = r * each, f1 = min(f0 + each, total), blocks = f1 - f0;
-  seek(f0);
-  if (s >= p.seqs) break;                       // (lengths that changed since `total`)
-  load_q(s);
-  // Pages of the range's blocks.
-  src.page = 0;
-  src.keys = 0;
-  {
+    const int f0 = r * each, f1 = min(f0 + each, total), blocks = f1 - f0;
+    seek(f0);
+    if (s >= p.seqs) break;                     // (lengths that changed since `total`)
+    w.load_q(p, s, h0, nh);
+    // Pages of the range's blocks.
+    w.page = w.keys = 0;
     const int f = f0 + lane / 2;
     int from = 0, key0 = -1;
     for (int n = s, at = base; at < f1 && n < p.seqs; ++n) {
@@ -337,164 +462,132 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
       if (f >= at && f < at + nb && f < f1) {
         from = n;
         key0 = ((f - at) * 2 + lane % 2) * kPage;
-        src.keys = min(max(len - key0, 0), kPage);
+        w.keys = min(max(len - key0, 0), kPage);
       }
       at += nb;
     }
     if (each == 2) ahead = __builtin_amdgcn_mov_dpp(ahead, 0x108, 0xF, 0xF, false);   // row_shl:8
-    if (src.keys > 0) {
-      src.page = p.seqs == 1 && each <= 2 ? ahead : p.bt[int64_t(from) * p.max_pages + key0 / kPage];
-      if (src.page < 0 || src.page >= p.num_pages) {
-        src.page = src.keys = 0;
+    if (w.keys > 0) {
+      w.page = p.seqs == 1 && each <= 2 ? ahead : p.bt[int64_t(from) * p.max_pages + key0 / kPage];
+      if (w.page < 0 || w.page >= p.num_pages) {
+        w.page = w.keys = 0;
         if (p.err && head == 0) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
       }
     }
-  }
 #pragma unroll
-  for (int i = 0; i < kStages; ++i) issue_block<D, T>(p, src, scales, kh, i, i < blocks, koff, voff, ring + i * S::kSlots);
-  // Waited for once, here (they are older than the K/V loads), and not inside the stream.
+    for (int i = 0; i < kStages; ++i) w.issue(p, i, i < blocks, i);
+    w.await_q();
+    w.begin();
+    for (int i = 0; s < p.seqs;) {
+      const int nb = blocks_of(length(s));
+      const int begin = f0 + i - base;          // the sequence's block at i
+      w.stream(p, i, min(blocks, base + nb - f0), blocks);
+      const float l = rows_sum(w.lsum);
+      const int end = base + nb;
+      const bool whole = begin == 0 && end <= f1;
+      if (l16 < nh) {
+        if (whole) {
 #pragma unroll
-  for (int kk = 0; kk < D / 32; ++kk) asm volatile("" : "+v"(qf[kk]));
-
-  f32x4 acc[DT];
+          for (int dt = 0; dt < DT; ++dt) write_row(p, s, h0 + l16, 16 * dt + 4 * q4, w.acc[dt], w.m, l);
+        } else {
+          // Ranges and sequences advance together, so r + s numbers the records.
+          const int64_t rec = (int64_t(r) + s) * p.Hq + h0 + l16;
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt) acc[dt] = f32x4{};
-  float m = -INFINITY, lsum = 0.f;
-  int i = 0;
-  while (i < blocks && s < p.seqs) {
-  const int nb = blocks_of(length(s));
-  const int begin = f0 + i - base, stop = min(blocks, base + nb - f0);    // its block at i; where it or the range ends
-#pragma unroll 1
-  for (; i < stop; ++i) {
-    u32x4* const Kst = ring + (static_cast<unsigned>(i) % kStages) * S::kSlots;
-    u32x4* const Vst = Kst + kBlk * CH;
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kStages - 1) * S::kLoads) : "memory");   // this block is here
-    f32x4 sc[2] = {f32x4{}, f32x4{}};
-    if constexpr (T == kCacheBf16) {
-#pragma unroll
-      for (int kk = 0; kk < D / 32; ++kk)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const bf16x8 a = __builtin_bit_cast(bf16x8, Kst[(kb0 ^ (kk * 4u)) + h * (kPage * CH)]);
-          sc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, qf[kk]), sc[h], 0, 0, 0);
-        }
-    } else {
-#pragma unroll
-      for (int j = 0; j < D / 64; ++j)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const u32x4 a = Kst[(kb0 ^ (j * 4u)) + h * (kPage * CH)];
-          sc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_bf16<T>(a.x, a.y), __builtin_bit_cast(bf16x8, qf[2 * j]), sc[h], 0, 0, 0);
-          sc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_bf16<T>(a.z, a.w), __builtin_bit_cast(bf16x8, qf[2 * j + 1]), sc[h], 0, 0, 0);
-        }
-    }
-    float pr[8], vs[8];
-    if constexpr (T == kCacheBf16) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) pr[e] = sc[e / 4][e % 4] * p.scale_log2;
-    } else {
-      const f32x4* f = reinterpret_cast<const f32x4*>(Kst + 2 * kBlk * CH);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const f32x4 ks = f[4 * h + q4], w = f[8 + 4 * h + q4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          pr[4 * h + r] = sc[h][r] * (ks[r] * p.scale_log2);
-          vs[4 * h + r] = w[r];
+          for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(p.part_o + rec * D + 16 * dt + 4 * q4) = w.acc[dt];
+          if (q4 == 0) *reinterpret_cast<f32x2*>(p.part_ml + rec * 2) = f32x2{w.m, l};
         }
       }
-    }
-    const int nv0 = __builtin_amdgcn_readlane(src.keys, i * 2), nv1 = __builtin_amdgcn_readlane(src.keys, i * 2 + 1);
-    if (nv0 < kPage || nv1 < kPage) {
-      // Keys past the end, and keys on a page outside the pool.
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (4 * q4 + e >= (h ? nv1 : nv0)) pr[h * 4 + e] = -INFINITY;
-    }
-    float mx = fmaxf(fmaxf(fmaxf(pr[0], pr[1]), fmaxf(pr[2], pr[3])), fmaxf(fmaxf(pr[4], pr[5]), fmaxf(pr[6], pr[7])));
-    mx = rows_max(mx);
-    if (__builtin_amdgcn_ballot_w64(mx > m) != 0) {
-      const float m_new = fmaxf(m, mx);
-      const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
-      m = m_new;
-      lsum *= alpha;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) acc[dt] *= alpha;
-    }
-    const float mc = m == -INFINITY ? 0.f : m;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      pr[e] = __builtin_amdgcn_exp2f(pr[e] - mc);
-      lsum += pr[e];
-      if constexpr (T != kCacheBf16) pr[e] *= vs[e];
-    }
-    bf16x8 pb[2];
-#pragma unroll
-    for (int part = 0; part < 2; ++part) {
-      u32x4 w;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = take_bf2(pr[2 * e], pr[2 * e + 1]);
-      pb[part] = __builtin_bit_cast(bf16x8, w);
-    }
-    const uint32_t vst = vb0 + static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)Vst));
-    if constexpr (T == kCacheBf16) {
-      u32x4 va[DT];
-#pragma unroll
-      for (int dt = 0; dt < DT; dt += 4) read_pv4<kPage * D * 2>(vst, dt, va + dt);
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int part = 1; part >= 0; --part)
-          acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va[dt]), pb[part], acc[dt], 0, 0, 0);
-    } else {
-      u32x2 vc[DT];
-#pragma unroll
-      for (int dt = 0; dt < DT; dt += 4) read_pv8(vst, dt, vc + dt);
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const bf16x8 a = codes_bf16<T>(vc[dt].x, vc[dt].y);
-#pragma unroll
-        for (int part = 1; part >= 0; --part) acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pb[part], acc[dt], 0, 0, 0);
+      if (begin == 0 && head == 0 && lane == 0) {
+        // The row's records: none, or from here to the range of its last block.
+        reinterpret_cast<int2*>(p.parts)[s] = int2{r, whole ? 0 : (end - 1) / each - r + 1};
       }
+      if (i >= blocks) break;
+      // On to the next sequence that has keys.
+      seek(f0 + i);
+      if (s >= p.seqs) break;
+      w.load_q(p, s, h0, nh);
+      w.begin();
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this block's LDS reads are done
-    issue_block<D, T>(p, src, scales, kh, i + kStages, i + kStages < blocks, koff, voff, Kst);
-  }
-
-  // Lane: dimensions 16 dt + 4 q4 .. + 3 of head l16.
-  lsum = rows_sum(lsum);
-  const int end = base + nb;
-  const bool whole = begin == 0 && end <= f1;
-  if (l16 < nh) {
-    if (whole) {
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) write_row(p, s, h0 + l16, 16 * dt + 4 * q4, acc[dt], m, lsum);
-    } else {
-      // Ranges and sequences advance together, so r + s numbers the records.
-      const int64_t rec = (int64_t(r) + s) * p.Hq + h0 + l16;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(p.part_o + rec * D + 16 * dt + 4 * q4) = acc[dt];
-      if (q4 == 0) *reinterpret_cast<f32x2*>(p.part_ml + rec * 2) = f32x2{m, lsum};
-    }
-  }
-  if (begin == 0 && head == 0 && lane == 0) {
-    // The row's records: none, or from here to the range of its last block.
-    reinterpret_cast<int2*>(p.parts)[s] = int2{r, whole ? 0 : (end - 1) / each - r + 1};
-  }
-  if (i >= blocks) break;
-  // On to the next sequence that has keys.
-  seek(f0 + i);
-  if (s >= p.seqs) break;
-  load_q(s);
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt) acc[dt] = f32x4{};
-  m = -INFINITY;
-  lsum = 0.f;
-  }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load into LDS outlives its wave
+}
+
+// The same for short rows: a workgroup per sequence, KV head and group of query heads,
+// whose waves take equal runs of its blocks and merge them through LDS: one launch and no
+// record.
+template <int D, CacheType T, int kWaves>
+__global__ __launch_bounds__(kBoundThreads) void attend_short_kernel(AttendParams p, int groups) {
+  using S = Shape<D, T>;
+  constexpr int DT = D / 16;
+  __shared__ __attribute__((aligned(256))) u32x4 lds[kWaves * S::kRing];
+  const int lane = threadIdx.x & 63, q4 = lane >> 4, l16 = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // Heads of a sequence on one XCD, where there are sequences for all of them.
+  const int heads = p.Hkv * groups;
+  int s, head;
+  if (p.seqs < 8) {
+    s = static_cast<int>(blockIdx.x) / heads;
+    head = static_cast<int>(blockIdx.x) - s * heads;
+  } else {
+    const int y = static_cast<int>(blockIdx.x >> 3);
+    s = y / heads * 8 + (blockIdx.x & 7);
+    head = y % heads;
+    if (s >= p.seqs) return;
+  }
+  const int kh = groups == 1 ? head : head / groups, group = head - kh * groups;
+  const int h0 = kh * p.G + group * kAttendGroup, nh = min(kAttendGroup, p.G - group * kAttendGroup);
+  // The row's first 64 pages beside its length.
+  int page = p.bt[int64_t(s) * p.max_pages + min(lane, p.max_pages - 1)];
+  Wave<D, T, kWaves> w;
+  w.load_q(p, s, h0, nh);
+  const int len = row_length(p, s);
+  w.init(p, kh, lds + wave * S::kRing);
+  const int all = blocks_of(len), each = (all + kWaves - 1) / kWaves;
+  const int b0 = min(wave * each, all), blocks = min(each, all - b0);
+  const bool bad = page < 0 || page >= p.num_pages;
+  if (p.err && wave == 0 && head == 0) {
+    if (bad && lane * kPage < len) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
+    if (lane == 0 && len != p.lengths[s]) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_LENGTH));
+  }
+  // (Lane 2 i + h: of the wave's block i.)
+  const int key0 = lane * kPage;
+  w.keys = __shfl(bad ? 0 : min(max(len - key0, 0), kPage), 2 * b0 + lane, 64);
+  w.page = __shfl(page, 2 * b0 + lane, 64);
+#pragma unroll
+  for (int i = 0; i < kStages; ++i) w.issue(p, i, i < blocks, i);
+  w.await_q();
+  w.begin();
+  int i = 0;
+  w.stream(p, i, blocks, blocks);
+  // The waves' parts, each in its own ring once nothing is in flight there: [head][dim],
+  // then (maximum, sum) per head.
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  const float l = rows_sum(w.lsum);
+  if (l16 < nh) {
+    float* dst = reinterpret_cast<float*>(w.ring) + l16 * D + 4 * q4;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(dst + dt * 16) = w.acc[dt];
+    if (q4 == 0) reinterpret_cast<f32x2*>(w.ring + kAttendGroup * D / 4)[l16] = f32x2{w.m, l};
+  }
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  for (int e = threadIdx.x; e < nh * D / 4; e += kWaves * 64) {
+    const int g = e / (D / 4), d = (e % (D / 4)) * 4;
+    f32x2 ml[kWaves];
+    float top = -INFINITY, sum = 0.f;
+    f32x4 o{};
+#pragma unroll
+    for (int n = 0; n < kWaves; ++n) {
+      ml[n] = reinterpret_cast<const f32x2*>(lds + n * S::kRing + kAttendGroup * D / 4)[g];
+      top = fmaxf(top, ml[n].x);
+    }
+#pragma unroll
+    for (int n = 0; n < kWaves; ++n) {
+      const float f = join_weight(ml[n].x, ml[n].y, top);
+      sum += f * ml[n].y;
+      o += f * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(lds + n * S::kRing) + g * D + d);
+    }
+    write_row(p, s, h0 + g, d, o, top, sum);
+  }
 }
 
 // Joins a row's records: one workgroup per (query head, sequence).  D / 4 lanes hold a
@@ -563,9 +656,28 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendParams p) {
   if (side == 0) write_row(p, s, h, i, o, m, l);
 }
 
+constexpr int kShortKeys = 512;          // (a lane per page: at most 1024)
+constexpr int kShortGroups = 1536;
+
+template <int D, CacheType T, int kWaves>
+hipError_t launch_short(const AttendParams& p, int groups, hipStream_t s) {
+  const int64_t seqs = p.seqs < 8 ? p.seqs : (int64_t(p.seqs) + 7) / 8 * 8;
+  attend_short_kernel<D, T, kWaves><<<static_cast<unsigned>(seqs * p.Hkv * groups), kWaves * 64, 0, s>>>(p, groups);
+  return hipGetLastError();
+}
+
 template <int D, CacheType T>
 hipError_t launch(const AttendParams& p, hipStream_t s) {
   const int groups = (p.G + kAttendGroup - 1) / kAttendGroup;
+  // Short rows, in as many workgroups as a CU holds a few of: eight waves (bf16 rows of
+  // 128: four, their rings fill a CU's LDS), or half of them where there are several rows
+  // to a CU.  us, and as ranges with a join: 4 rows of 60 keys 4.4, 8.3; 1 of 500 7.1, 8.1; 128
+  // of 300 (8 KV heads, E4M3) 21.3, 26.4; beyond the limits, 1 row of 1000 11.5, 9.4, and 256
+  // of 300 38.5, 36.4.
+  constexpr int kFill = std::min(attend_waves(Shape<D, T>::kRow), 8);
+  const int64_t wgs = int64_t(p.seqs) * p.Hkv * groups;
+  if (p.max_length <= kShortKeys && wgs <= kShortGroups)
+    return wgs <= 256 ? launch_short<D, T, kFill>(p, groups, s) : launch_short<D, T, kFill / 2>(p, groups, s);
   const int heads = p.Hkv * groups, head_shift = heads % 4 == 0 ? 2 : heads % 2 == 0 ? 1 : 0;
   const int per = kWaves >> head_shift;         // ranges of a workgroup
   attend_kernel<D, T><<<dim3((p.ranges + per - 1) / per, heads >> head_shift), kWaves * 64, 0, s>>>(p, groups, head_shift);

@@ -132,6 +132,12 @@ CASES = [
     (128, 2, 4, [0] * 70 + [33] + [0] * 64 + [1, 500] + [0] * 30),   # few keys in many rows
     (64, 1, 2, [1 + i % 3 for i in range(300)]),                     # a block a row
     (128, 4, 2, [0, 0, 0]),
+    (128, 8, 8, [7 * i for i in range(73)]),                         # short rows, several to a CU
+    (64, 4, 4, [14 * i for i in range(36)]),
+    (64, 2, 8, [i % 40 for i in range(200)]),                        # too many of them for a workgroup each
+    (128, 20, 8, [512, 511, 1]),                                     # the longest short rows
+    (64, 1, 1, [512, 0, 33]),
+    (64, 1, 1, [513, 0, 33]),
 ]
 
 
@@ -146,10 +152,15 @@ def test_against_oracle(P, d, group, hkv, lens, fmt):
     out = cache.attend(P, q, scale, lse=lse, err=err)
     assert int(err.item()) == 0
     check(cache, q, scale, out, lse)
-    # Without lse, with a larger bound on the lengths and a table wider than they need: the same bits.
+    # Without lse: the same bits.
+    assert torch.equal(cache.attend(P, q, scale), out)
+    # With a larger bound on the lengths (short rows are then divided as long ones are) and a table wider than
+    # they need.
     bt = torch.full((len(lens), cache.max_pages + 300), -1, dtype=torch.int32, device=DEV)
     bt[:, :cache.max_pages] = cache.bt
-    assert torch.equal(cache.attend(P, q, scale, max_length=max(lens) + 4000, bt=bt), out)
+    lse.fill_(9.0)
+    check(cache, q, scale, cache.attend(P, q, scale, max_length=max(lens) + 4000, bt=bt, lse=lse, err=err), lse)
+    assert int(err.item()) == 0
 
 
 @pytest.mark.parametrize("fmt,d,hkv,n", [("bf16", 128, 2, 400000), ("e4m3", 64, 32, 100000), ("int8", 128, 16, 100000)])
@@ -254,6 +265,14 @@ def test_pages_outside_the_pool(P, fmt):
     out = cache.attend(P, q, 0.09, lse=lse, err=err, bt=torch.from_numpy(bt).to(DEV))
     assert int(err.item()) == 1
     check(cache, q, 0.09, out, lse, gone)
+    # short rows alone
+    cache.lens[-1] = 17
+    cache.k[-1], cache.v[-1] = cache.k[-1][:17], cache.v[-1][:17]
+    lengths = torch.tensor(cache.lens, dtype=torch.int32, device=DEV)
+    err.zero_()
+    out = cache.attend(P, q, 0.09, lse=lse, err=err, bt=torch.from_numpy(bt).to(DEV), lengths=lengths)
+    assert int(err.item()) == 1
+    check(cache, q, 0.09, out, lse, gone)
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "int8"])
@@ -268,6 +287,13 @@ def test_lengths_outside_the_bound(P, fmt):
     cache.lens = [150, 0, 50]
     for i, n in enumerate(cache.lens):
         cache.k[i], cache.v[i] = cache.k[i][:n], cache.v[i][:n]
+    check(cache, q, 0.1, out, lse)
+    # the same where long rows are possible
+    bt = torch.nn.functional.pad(cache.bt, (0, 200), value=-1).contiguous()
+    lengths[0] = 150
+    err.zero_()
+    out = cache.attend(P, q, 0.1, lse=lse, max_length=3000, err=err, lengths=lengths, bt=bt)
+    assert int(err.item()) == 4
     check(cache, q, 0.1, out, lse)
 
 
