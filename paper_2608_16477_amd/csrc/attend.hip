@@ -14,9 +14,9 @@
 // that followed from the sequence's own (the first form): 64 sequences of 500 to 8000
 // keys, E4M3, 64 / 8 heads of 128 (344 MB), 87 -> 68; 131,071 keys INT8 (277 MB) 65 -> 57; 60,001
 // and 33,333 keys bf16, 32 / 8 heads (383 MB), 79 -> 69; 8 sequences of 1000 to 8000 keys
-// bf16 (106 MB) 32 -> 28; one of 4000 keys bf16 11.2 -> 12.6; one of 500 keys 8.0, both.  The
-// first launch of the first four reads what it has to and no more, at 5.6, 5.7, 5.9 and 4.8
-// TB/s; the join takes 4 to 5.  LDS has no bank conflict.
+// bf16 (106 MB) 32 -> 28; one of 4000 keys bf16 11.2 -> 12.7.  The first launch of the first
+// four reads what it has to and no more, at 5.7, 5.7, 6.3 and 4.7 TB/s; the join takes 4 to
+// 5.  LDS has no bank conflict.  (Short rows: attend_short_kernel.)
 //
 // Each wave moves its blocks from memory straight into a private two-stage LDS ring,
 // with the rows' scales.  Scores are S^T = K Q^T with v_mfma_f32_16x16x32_bf16 (the
