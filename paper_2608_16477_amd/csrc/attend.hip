@@ -14,9 +14,10 @@
 // that followed from the sequence's own (the first form): 64 sequences of 500 to 8000
 // keys, E4M3, 64 / 8 heads of 128 (344 MB), 87 -> 68; 131,071 keys INT8 (277 MB) 65 -> 57; 60,001
 // and 33,333 keys bf16, 32 / 8 heads (383 MB), 79 -> 69; 8 sequences of 1000 to 8000 keys
-// bf16 (106 MB) 32 -> 28; one of 4000 keys bf16 11.2 -> 12.7.  The first launch of the first
-// four reads what it has to and no more, at 5.7, 5.7, 6.3 and 4.7 TB/s; the join takes 4 to
-// 5.  LDS has no bank conflict.  (Short rows: attend_short_kernel.)
+// bf16 (106 MB) 32 -> 28.  The first launch of these four reads what it has to and no more, at
+// 5.7, 5.7, 6.3 and 4.7 TB/s; the join takes 4 to 5.  LDS has no bank conflict.  Calls that
+// do not fill the chip are a chain of loads, which the way to a range is longer than: they
+// keep a workgroup per split (attend_split_kernel).
 //
 // Each wave moves its blocks from memory straight into a private two-stage LDS ring,
 // with the rows' scales.  Scores are S^T = K Q^T with v_mfma_f32_16x16x32_bf16 (the
@@ -512,45 +513,48 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load into LDS outlives its wave
 }
 
-// The same for short rows: a workgroup per sequence, KV head and group of query heads,
-// whose waves take equal runs of its blocks and merge them through LDS: one launch and no
-// record.
+// The same for calls of little work: a workgroup per split of `per` blocks of a sequence,
+// KV head and group of query heads, whose waves take equal runs of its blocks and merge
+// them through LDS.  A row of one split is written as it is (short rows: one launch).
 template <int D, CacheType T, int kWaves>
-__global__ __launch_bounds__(kBoundThreads) void attend_short_kernel(AttendParams p, int groups) {
+__global__ __launch_bounds__(kBoundThreads) void attend_split_kernel(AttendParams p, int groups, int splits, int per) {
   using S = Shape<D, T>;
   constexpr int DT = D / 16;
   __shared__ __attribute__((aligned(256))) u32x4 lds[kWaves * S::kRing];
   const int lane = threadIdx.x & 63, q4 = lane >> 4, l16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // Heads of a sequence on one XCD, where there are sequences for all of them.
-  const int heads = p.Hkv * groups;
-  int s, head;
-  if (p.seqs < 8) {
-    s = static_cast<int>(blockIdx.x) / heads;
-    head = static_cast<int>(blockIdx.x) - s * heads;
+  // Heads of a split on one XCD, where there are splits for all of them.
+  const int heads = p.Hkv * groups, items = p.seqs * splits;
+  int item, head;
+  if (items < 8) {
+    item = static_cast<int>(blockIdx.x) / heads;
+    head = static_cast<int>(blockIdx.x) - item * heads;
   } else {
     const int y = static_cast<int>(blockIdx.x >> 3);
-    s = y / heads * 8 + (blockIdx.x & 7);
+    item = y / heads * 8 + (blockIdx.x & 7);
     head = y % heads;
-    if (s >= p.seqs) return;
+    if (item >= items) return;
   }
+  const int s = item / splits, split = item - s * splits, f0 = split * per;
   const int kh = groups == 1 ? head : head / groups, group = head - kh * groups;
   const int h0 = kh * p.G + group * kAttendGroup, nh = min(kAttendGroup, p.G - group * kAttendGroup);
-  // The row's first 64 pages beside its length.
-  int page = p.bt[int64_t(s) * p.max_pages + min(lane, p.max_pages - 1)];
+  // The split's pages (at most 64) beside the row's length.
+  int page = p.bt[int64_t(s) * p.max_pages + min(2 * f0 + lane, p.max_pages - 1)];
   Wave<D, T, kWaves> w;
   w.load_q(p, s, h0, nh);
   const int len = row_length(p, s);
   w.init(p, kh, lds + wave * S::kRing);
-  const int all = blocks_of(len), each = (all + kWaves - 1) / kWaves;
+  const int blocks_all = blocks_of(len), all = min(max(blocks_all - f0, 0), per);
+  if (split > 0 && all == 0) return;
+  const int each = (all + kWaves - 1) / kWaves;
   const int b0 = min(wave * each, all), blocks = min(each, all - b0);
   const bool bad = page < 0 || page >= p.num_pages;
+  const int key0 = (2 * f0 + lane) * kPage;
   if (p.err && wave == 0 && head == 0) {
-    if (bad && lane * kPage < len) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
-    if (lane == 0 && len != p.lengths[s]) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_LENGTH));
+    if (bad && key0 < len) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
+    if (split == 0 && lane == 0 && len != p.lengths[s]) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_LENGTH));
   }
   // (Lane 2 i + h: of the wave's block i.)
-  const int key0 = lane * kPage;
   w.keys = __shfl(bad ? 0 : min(max(len - key0, 0), kPage), 2 * b0 + lane, 64);
   w.page = __shfl(page, 2 * b0 + lane, 64);
 #pragma unroll
@@ -570,6 +574,9 @@ __global__ __launch_bounds__(kBoundThreads) void attend_short_kernel(AttendParam
     if (q4 == 0) reinterpret_cast<f32x2*>(w.ring + kAttendGroup * D / 4)[l16] = f32x2{w.m, l};
   }
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  const bool whole = blocks_all <= per;
+  if (splits > 1 && split == 0 && head == 0 && threadIdx.x == 0)      // records s * splits on (join_kernel adds s)
+    reinterpret_cast<int2*>(p.parts)[s] = int2{s * splits - s, whole ? 0 : (blocks_all + per - 1) / per};
   for (int e = threadIdx.x; e < nh * D / 4; e += kWaves * 64) {
     const int g = e / (D / 4), d = (e % (D / 4)) * 4;
     f32x2 ml[kWaves];
@@ -586,7 +593,13 @@ __global__ __launch_bounds__(kBoundThreads) void attend_short_kernel(AttendParam
       sum += f * ml[n].y;
       o += f * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(lds + n * S::kRing) + g * D + d);
     }
-    write_row(p, s, h0 + g, d, o, top, sum);
+    if (whole) {
+      write_row(p, s, h0 + g, d, o, top, sum);
+    } else {
+      const int64_t rec = int64_t(item) * p.Hq + h0 + g;
+      *reinterpret_cast<f32x4*>(p.part_o + rec * D + d) = o;
+      if (d == 0) *reinterpret_cast<f32x2*>(p.part_ml + rec * 2) = f32x2{top, sum};
+    }
   }
 }
 
@@ -656,42 +669,58 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendParams p) {
   if (side == 0) write_row(p, s, h, i, o, m, l);
 }
 
-constexpr int kShortKeys = 512;          // (a lane per page: at most 1024)
-constexpr int kShortGroups = 1536;
-
-template <int D, CacheType T, int kWaves>
-hipError_t launch_short(const AttendParams& p, int groups, hipStream_t s) {
-  const int64_t seqs = p.seqs < 8 ? p.seqs : (int64_t(p.seqs) + 7) / 8 * 8;
-  attend_short_kernel<D, T, kWaves><<<static_cast<unsigned>(seqs * p.Hkv * groups), kWaves * 64, 0, s>>>(p, groups);
-  return hipGetLastError();
-}
-
-template <int D, CacheType T>
-hipError_t launch(const AttendParams& p, hipStream_t s) {
-  const int groups = (p.G + kAttendGroup - 1) / kAttendGroup;
-  // Short rows, in as many workgroups as a CU holds a few of: eight waves (bf16 rows of
-  // 128: four, their rings fill a CU's LDS), or half of them where there are several rows
-  // to a CU.  us, and as ranges with a join: 4 rows of 60 keys 4.4, 8.3; 1 of 500 7.1, 8.1; 128
-  // of 300 (8 KV heads, E4M3) 21.3, 26.4; beyond the limits, 1 row of 1000 11.5, 9.4, and 256
-  // of 300 38.5, 36.4.
-  constexpr int kFill = std::min(attend_waves(Shape<D, T>::kRow), 8);
-  const int64_t wgs = int64_t(p.seqs) * p.Hkv * groups;
-  if (p.max_length <= kShortKeys && wgs <= kShortGroups)
-    return wgs <= 256 ? launch_short<D, T, kFill>(p, groups, s) : launch_short<D, T, kFill / 2>(p, groups, s);
-  const int heads = p.Hkv * groups, head_shift = heads % 4 == 0 ? 2 : heads % 2 == 0 ? 1 : 0;
-  const int per = kWaves >> head_shift;         // ranges of a workgroup
-  attend_kernel<D, T><<<dim3((p.ranges + per - 1) / per, heads >> head_shift), kWaves * 64, 0, s>>>(p, groups, head_shift);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  // As many waves as a row can fill with records in one go: a wave in large batches, in
-  // others after the most records that max_length allows.  (Further waves then have
-  // nothing to add and change no bit, so a row's result does not depend on max_length.)
+// Waves per row of the join: as many as it can fill with records (at most `most`) in one go.
+// Further waves have nothing to add and change no bit.
+template <int D>
+hipError_t launch_join(const AttendParams& p, int64_t most, hipStream_t s) {
   const dim3 joins(p.Hq, p.seqs);
   constexpr int kShare = kJoinBatch * 256 / D;
-  const int64_t most = p.ranges / p.seqs < kShare ? 0 : attend_row_records(attend_total(1, p.max_length), p.seqs, p.ranges);
   if (most > 4 * kShare) join_kernel<D, 1024><<<joins, 1024, 0, s>>>(p);
   else if (most > kShare) join_kernel<D, 256><<<joins, 256, 0, s>>>(p);
   else join_kernel<D, 64><<<joins, 64, 0, s>>>(p);
   return hipGetLastError();
+}
+
+template <int D, CacheType T, int kWaves>
+hipError_t launch_split(const AttendParams& p, int groups, int splits, int per, hipStream_t s) {
+  const int64_t items = int64_t(p.seqs) * splits, all = items < 8 ? items : (items + 7) / 8 * 8;
+  attend_split_kernel<D, T, kWaves><<<static_cast<unsigned>(all * p.Hkv * groups), kWaves * 64, 0, s>>>(p, groups, splits, per);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess || splits == 1) return e;
+  return launch_join<D>(p, splits, s);
+}
+
+// How a call is run (us on the GPU; 8 KV heads of 128).
+//   Rows of up to kShortKeys keys, up to kShortGroups (sequence, head) pairs: a workgroup each
+// and one launch.  Its waves' rings fill a CU's LDS, or half of it where there are several
+// rows to a CU.  As ranges in parentheses: 4 rows of 60 keys bf16 4.4 (8.3), 128 of 300 E4M3
+// 21.3 (26.4); beyond the limits, 1 of 1000 11.5 (9.4), 256 of 300 38.5 (36.4).
+//   Else splits of one or two blocks a wave, if those are at most a workgroup per CU: 1 row of
+// 4000 keys bf16 10.4 (12.3), 16,000 E4M3 15.7 (19.2), 8 of 1000 INT8 10.0 (14.1).  Four blocks
+// a wave gain nothing on equal rows and lose on others (27 of 30 to 2000 keys, 4 heads of
+// 64, 11.5 (8.5)), as do two workgroups per CU (16,000 keys 19.1).
+//   Else ranges.
+constexpr int kShortKeys = 512;
+constexpr int kShortGroups = 1536;
+constexpr int kSplitBlocks = 2;
+
+template <int D, CacheType T>
+hipError_t launch(const AttendParams& p, hipStream_t s) {
+  const int groups = (p.G + kAttendGroup - 1) / kAttendGroup, heads = p.Hkv * groups;
+  constexpr int kFill = std::min(attend_waves(Shape<D, T>::kRow), 8);     // waves whose rings fill a CU's LDS
+  const int64_t rows = int64_t(p.seqs) * heads;
+  const int most = static_cast<int>(attend_total(1, p.max_length));       // blocks of a row
+  if (p.max_length <= kShortKeys && rows <= kShortGroups)
+    return rows <= 256 ? launch_split<D, T, kFill>(p, groups, 1, most, s) : launch_split<D, T, kFill / 2>(p, groups, 1, most, s);
+  for (int each = 1; each <= kSplitBlocks; each *= 2) {
+    // (Records, seqs * splits <= 256 / heads: fewer than attend_ranges, so there is room.)
+    const int per = kFill * each, splits = (most + per - 1) / per;
+    if (rows * splits <= 256) return launch_split<D, T, kFill>(p, groups, splits, per, s);
+  }
+  const int head_shift = heads % 4 == 0 ? 2 : heads % 2 == 0 ? 1 : 0;
+  const int per = kWaves >> head_shift;         // ranges of a workgroup
+  attend_kernel<D, T><<<dim3((p.ranges + per - 1) / per, heads >> head_shift), kWaves * 64, 0, s>>>(p, groups, head_shift);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  return launch_join<D>(p, p.ranges / p.seqs < kJoinBatch * 256 / D ? 0 : attend_row_records(most, p.seqs, p.ranges), s);
 }
 
 template <int D>

@@ -428,8 +428,8 @@ inline int64_t attend_heads(int Hq, int Hkv) { return int64_t(Hkv) * ((Hq / Hkv 
 // Blocks per range of a call of `total` blocks: as few rounds of the ranges as the
 // largest one allows, all rounds full.  Calls of short rows that leave half of the waves
 // without a block give one to each, others at least two, one per ring stage (one and two,
-// us: 1 row of 500 keys bf16 8.4, 8.6; 27 rows of 30 to 2000 keys 8.4, 9.2; 1 row of 4000
-// keys 13.7, 12.4: more records to join).
+// us: 27 rows of 30 to 2000 keys 8.4, 9.2; 1 row of 4000 keys, in ranges, 13.7, 12.4: more
+// records to join).
 constexpr int kAttendShort = 32;         // blocks of a row
 __host__ __device__ inline int attend_blocks(int total, int seqs, int ranges) {
   if (2 * int64_t(total) <= ranges && total <= int64_t(kAttendShort) * seqs) return 1;

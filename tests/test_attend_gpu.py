@@ -138,6 +138,11 @@ CASES = [
     (128, 20, 8, [512, 511, 1]),                                     # the longest short rows
     (64, 1, 1, [512, 0, 33]),
     (64, 1, 1, [513, 0, 33]),
+    (128, 8, 8, [4001]),                                             # splits of one block a wave (bf16: of two)
+    (128, 4, 4, [3000, 1, 0, 257]),
+    (128, 8, 1, [7000, 5000]),
+    (64, 4, 2, [9000]),
+    (128, 5, 3, [2500, 600, 2047]),
 ]
 
 

@@ -197,6 +197,11 @@ def test_attend_workspace(P):
                     assert each <= 32
                     last = -(-total // each) - 1 + s - 1                # the largest range + sequence
                     assert size(s, hq, hkv, d, n) >= 8 * s + (last + 1) * hq * (d + 2) * 4
+                heads, waves = hkv * -(-(hq // hkv) // 16), min(1024 // row_bytes, 8)
+                for each in (1, 2):                                     # splits of one or two blocks a wave
+                    splits = -(-(-(-n // 32)) // (waves * each))
+                    if s * heads * splits <= 256:
+                        assert size(s, hq, hkv, d, n) >= 8 * s + s * splits * hq * (d + 2) * 4
 
 
 # ------------------------------------------------------------------ binding
