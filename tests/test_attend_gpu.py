@@ -226,6 +226,45 @@ def test_many_sequences_and_long_ones(P, fmt):
     check(cache, q, 0.09, cache.attend(P, q, 0.09, lse=lse), lse)
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+def test_thousands_of_rows(P, fmt):
+    """More rows than 64 partial sums of 64 lengths, most of them short or empty: a sample against the oracle."""
+    rng = np.random.default_rng(4)
+    lens = [int(n) for n in rng.choice([0, 1, 5, 31, 32, 33, 70], size=4500)]
+    lens[2222] = 3000
+    cache = Cache(fmt, 1, 64, lens, seed=14)
+    q = queries(len(lens), 2, 64, 7)
+    lse = torch.empty((len(lens), 2), dtype=torch.float32, device=DEV)
+    out = cache.attend(P, q, 0.125, lse=lse)
+    some = sorted({0, 1, 63, 64, 65, 2221, 2222, 2223, 4498, 4499, *rng.integers(0, 4500, 150).tolist()})
+    cache.lens, cache.k, cache.v = [lens[i] for i in some], [cache.k[i] for i in some], [cache.v[i] for i in some]
+    check(cache, q[some], 0.125, out[some], lse[some])
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3", "int8"])
+def test_pages_beyond_4_gib(P, fmt):
+    """Pages at the end of planes of more than 4 GiB; nothing else of the pool is read."""
+    hkv, d, lens = 8, 128, [600, 33, 1100]
+    cache = Cache(fmt, hkv, d, lens, seed=15)
+    page_bytes = 16 * hkv * d * (2 if fmt == "bf16" else 1)
+    pages = (1 << 32) // page_bytes + 500
+    small = cache.pool if fmt == "bf16" else cache.codes.view(torch.uint8)
+    held = small.shape[2]
+    big = torch.empty((1, 2, pages, 16, hkv, d), dtype=small.dtype, device=DEV)
+    big[0, :, pages - held:] = small[1]
+    bt = torch.where(cache.bt >= 0, cache.bt + (pages - held), cache.bt)
+    q = queries(3, 16, d, 9)
+    out, lse = torch.empty_like(q), torch.empty((3, 16), dtype=torch.float32, device=DEV)
+    ws = torch.empty(P.pallas_attend_workspace_size(3, 16, hkv, d, 1100), dtype=torch.uint8, device=DEV)
+    if fmt == "bf16":
+        P.pallas_attend_kv(big, 0, q, cache.lengths, 1100, bt, 0.09, out, ws, lse=lse)
+    else:
+        scales = torch.empty((1, 2, pages, 16, hkv), dtype=torch.float32, device=DEV)
+        scales[0, :, pages - held:] = cache.scales[1]
+        P.pallas_attend_quant(big.view(TYPES[fmt]), scales, 0, q, cache.lengths, 1100, bt, 0.09, out, ws, lse=lse)
+    check(cache, q, 0.09, out, lse)
+
+
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3", "int8"])
 def test_steep_scores(P, fmt):
     """Scores of hundreds: the running maximum moves by more than the exponent's range."""

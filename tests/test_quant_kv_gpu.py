@@ -163,3 +163,28 @@ def test_one_token_per_sequence(P):
     P.pallas_quant_store(*a, 0, k, v, pos, table)
     P.pallas_quant_store(*b, 0, k, v, pos, table, seq_ids=torch.tensor([0, 1], dtype=torch.int32, device=DEV))
     assert torch.equal(a[0].view(torch.uint8), b[0].view(torch.uint8)) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_pages_beyond_4_gib(P, fmt):
+    """Slots at the end of a plane of more than 4 GiB, of the second layer."""
+    hkv, d = 16, 128
+    pages = (1 << 32) // (16 * hkv * d) + 9
+    codes = torch.empty((2, 2, pages, 16, hkv, d), dtype=torch.uint8, device=DEV).view(TYPES[fmt])
+    scales = torch.empty((2, 2, pages, 16, hkv), device=DEV)
+    table = torch.tensor([[pages - 1, 3, pages - 7]], dtype=torch.int32, device=DEV)
+    pos = torch.tensor([0, 15, 16, 47, 33], dtype=torch.int32, device=DEV)
+    x = special_rows(5, hkv, d, 6).to(DEV)
+    seq = torch.zeros_like(pos)
+    P.pallas_quant_store(codes, scales, 1, x, x, pos, table, seq_ids=seq)
+    c, s = co.quantise(to_np64(x), fmt)
+    pg, slot = table[0, (pos // 16).long()].long(), (pos % 16).long()
+    for kv in range(2):
+        assert np.array_equal(scales[1, kv, pg, slot].cpu().numpy(), s, equal_nan=True)
+        assert np.array_equal(codes.view(torch.uint8)[1, kv, pg, slot].cpu().numpy(), c)
+    bk, bv = torch.empty_like(x), torch.empty_like(x)
+    P.pallas_quant_load(codes, scales, 1, bk, bv, pos, table, seq_ids=seq)
+    val = co.dequantise(c, np.ones_like(s), fmt).astype(np.float32) * s[..., None]
+    fine = np.isfinite(val)
+    for got in (bk, bv):
+        assert np.array_equal(bits(got)[fine], bf16_bits(bf16_round(val.astype(np.float64)))[fine])
