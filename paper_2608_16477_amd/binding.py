@@ -420,8 +420,8 @@ def _quant_call(what, call, codes, scales, layer, k, v, positions, block_tables,
     seqs, pages = _whole(block_tables, what + ": block tables", i32, 2, dev)
     if seq_ids is not None and _whole(seq_ids, what + ": sequence ids", i32, 1, dev) != n:
         _bad(f"{what}: {seq_ids.shape[0]} sequence ids of {T} tokens")
-    if err is not None:
-        _whole(err, what + ": err", i32, 1, dev)
+    if err is not None and not _whole(err, what + ": err", i32, 1, dev)[0]:
+        _bad(f"{what}: an empty err")
     if T:
         _launch(dev, stream, call, C.byref(ps), layer, T, _ptr(seq_ids), positions.data_ptr(), k.data_ptr(), ks,
                 v.data_ptr(), vs, seqs, block_tables.data_ptr(), pages, _ptr(err))
@@ -452,8 +452,8 @@ def _attend_call(call, ps, dev, layer, q, lengths, max_length, block_tables, sca
         _bad(f"attend: {tuple(shape)} queries, {lengths.shape[0]} lengths, {seqs} tables, a pool of head_dim {ps.head_dim}")
     if lse is not None and _whole(lse, "attend: lse", _torch.float32, 2, dev) != shape[:2]:
         _bad(f"attend: lse {tuple(lse.shape)}")
-    if err is not None:
-        _whole(err, "attend: err", i32, 1, dev)
+    if err is not None and not _whole(err, "attend: err", i32, 1, dev)[0]:
+        _bad("attend: an empty err")
     if workspace.get_device() != dev or not workspace.is_contiguous():
         _bad("attend: workspace on another device, or not contiguous")
     _launch(dev, stream, call, C.byref(ps), layer, S, H, q.data_ptr(), qs, lengths.data_ptr(), max_length,

@@ -188,3 +188,19 @@ def test_pages_beyond_4_gib(P, fmt):
     fine = np.isfinite(val)
     for got in (bk, bv):
         assert np.array_equal(bits(got)[fine], bf16_bits(bf16_round(val.astype(np.float64)))[fine])
+
+
+def test_an_empty_err_is_refused(P):
+    """An empty slice has an address that is another tensor's."""
+    codes, scales = torch.zeros((1, 2, 3, 16, 2, 64), dtype=torch.int8, device=DEV), torch.zeros((1, 2, 3, 16, 2), device=DEV)
+    x, ints = torch.ones((1, 2, 64), dtype=torch.bfloat16, device=DEV), torch.zeros(8, dtype=torch.int32, device=DEV)
+    bt = torch.full((1, 3), 99, dtype=torch.int32, device=DEV)
+    ws = torch.empty(P.pallas_attend_workspace_size(1, 2, 2, 64, 5), dtype=torch.uint8, device=DEV)
+    err, pos, lens = ints[2:2], ints[4:5], ints[5:6].fill_(5)
+    for call in (lambda: P.pallas_quant_store(codes, scales, 0, x, x, pos, bt, err=err),
+                 lambda: P.pallas_quant_load(codes, scales, 0, x, x, pos, bt, err=err),
+                 lambda: P.pallas_attend_quant(codes, scales, 0, x, lens, 5, bt, 1.0, x.clone(), ws, err=err)):
+        with pytest.raises(P.PallasError) as e:
+            call()
+        assert e.value.status == P.Status.INVALID_ARG
+    assert ints.tolist() == [0, 0, 0, 0, 0, 5, 0, 0]
