@@ -373,7 +373,7 @@ typedef struct {
   double theta;        /* > 1 */
   double factor;       /* s >= 1 (all but UNSCALED) */
   double fast, slow;   /* turns over L, fast > slow > 0 (YARN, BANDS) */
-  double magnitude;    /* m > 0, or 0: as above */
+  double magnitude;    /* m, 2^-126 .. 2^126, or 0: as above */
 } pallas_rope_config;
 
 /* Filled by pallas_rope_init, owned by the caller, read during a call. */
@@ -392,7 +392,8 @@ int pallas_rope_init(const pallas_rope_config* cfg, pallas_rope_plan* plan);
  * elements: head h of token t is at d_x + t * x_token_stride + h * x_head_stride
  * (elements, >= 0) and goes to the same place of d_y and its strides.  d_y may be
  * d_x with the same strides (in place); otherwise heads read and heads written
- * must not overlap.  d_positions (int32, device, [num_tokens]) may hold any
+ * must not overlap.  Of d_y's two dimensions one must step over all of the other
+ * (INVALID_ARG: heads written would overlap).  d_positions (int32, device, [num_tokens]) may hold any
  * int32; angles are exact to 2^-31 turn at every one.  inverse = 1 takes a
  * rotation by the same plan and position back (angle -p f_i, factor 1 / m), so
  * it also moves a cached K row: back from p, then on to q.  Rounded once, from
@@ -467,7 +468,9 @@ int pallas_quant_load(const pallas_quant_pool* pool, int32_t layer, int32_t num_
  * out_stride elements apart (multiples of 8, 16-byte aligned pointers; d_out may
  * not overlap d_q).  d_lse (nullable): float32 [num_seqs][n_q_heads], the natural
  * logarithm of sum_j exp(scale q . k_j), with which results over parts of a
- * cache are joined.  A row without keys gives zeros and -infinity.
+ * cache are joined.  A row without keys, or of scores that are all -infinity, gives
+ * zeros and -infinity.  An infinity or a NaN in a query or in a K or V row that is
+ * attended to may make the results of the heads that read it NaN, of no other.
  *   head_dim 64 or 128 (UNSUPPORTED otherwise), page_size 16, any number of
  * query heads per KV head, num_seqs up to 65535, max_length (the longest length
  * the call can meet) at least 1 and at most max_pages * page_size; num_seqs *
@@ -479,7 +482,7 @@ int pallas_quant_load(const pallas_quant_pool* pool, int32_t layer, int32_t num_
  * lengths of the call and max_length, so a row's last bits follow them, not the
  * other rows' queries or keys.  d_lengths may not change during the call.
  * The workspace (device, 256-byte aligned, pallas_attend_workspace_size bytes)
- * holds nothing between calls. */
+ * holds nothing between calls; calls that may run at once need one each. */
 int pallas_attend_kv(const pallas_kv_pool* pool, int32_t layer, int32_t num_seqs, int32_t n_q_heads,
                      const void* d_q, int64_t q_stride, const int32_t* d_lengths,
                      int32_t max_length, const int32_t* d_block_tables, int32_t max_pages,

@@ -353,7 +353,7 @@ __device__ __forceinline__ int lane_length(const AttendParams& p, int at) {
   const int len = row_length(p, min(s, p.seqs - 1));
   return s < p.seqs ? len : 0;
 }
-__device__ __forceinline__ int blocks_of(int len) { return static_cast<int>(static_cast<uint32_t>(len + kBlk - 1) / kBlk); }
+__device__ __forceinline__ int blocks_of(int len) { return static_cast<int>((static_cast<uint32_t>(len) + kBlk - 1) / kBlk); }
 
 // Inclusive prefix sums over the wave (row shifts by 1, 2, 4, 8, then the rows' last
 // lanes to the rows behind).

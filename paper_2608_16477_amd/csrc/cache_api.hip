@@ -207,6 +207,8 @@ int pallas_rope_init(const pallas_rope_config* cfg, pallas_rope_plan* plan) {
   out.layout = c.layout;
   double m = c.magnitude;
   if (m == 0.0) m = c.scaling == PALLAS_ROPE_YARN ? 0.1 * std::log(c.factor) + 1.0 : 1.0;
+  if (!(m >= 0x1p-126 && m <= 0x1p126))
+    return fail(PALLAS_ERR_INVALID_ARG, "rope: magnitude %g (2^-126 to 2^126)", m);
   out.magnitude = static_cast<float>(m);
   for (int i = 0; i < r / 2; ++i) {
     real f = std::pow(theta, real(-2 * i) / r);
@@ -236,14 +238,18 @@ int pallas_rope_apply(const pallas_rope_plan* plan, int32_t inverse, int32_t num
     return fail(PALLAS_ERR_INVALID_ARG, "rope: rows not 2-byte, or positions not 4-byte aligned");
   if (x_token_stride < 0 || x_head_stride < 0 || y_token_stride < 0 || y_head_stride < 0)
     return fail(PALLAS_ERR_INVALID_ARG, "rope: negative stride");
-  // Rows written may not fall on each other (rows read may: a stride of 0 repeats them).
-  if ((n_heads > 1 && y_head_stride < head_dim) || (num_tokens > 1 && y_token_stride < head_dim))
-    return fail(PALLAS_ERR_INVALID_ARG, "rope: output strides below a head of %d", head_dim);
-  if (d_x == d_y && (x_token_stride != y_token_stride || x_head_stride != y_head_stride))
-    return fail(PALLAS_ERR_INVALID_ARG, "rope: in place with other strides");
   if (int64_t(n_heads) * head_dim > (int64_t(1) << 20) || num_tokens >= (1 << 24))
     return fail(PALLAS_ERR_UNSUPPORTED, "rope: %d tokens (below 2^24) of %d heads of %d (at most 2^20 elements)", num_tokens,
                 n_heads, head_dim);
+  // Heads written may not fall on each other (heads read may: a stride of 0 repeats them):
+  // of the two dimensions, one steps over all of the other.
+  auto apart = [&](int64_t inner, int64_t n, int64_t outer, int64_t m) {
+    return (n <= 1 || inner >= head_dim) && (m <= 1 || (outer >= head_dim && (n <= 1 || (outer - head_dim) / (n - 1) >= inner)));
+  };
+  if (!apart(y_head_stride, n_heads, y_token_stride, num_tokens) && !apart(y_token_stride, num_tokens, y_head_stride, n_heads))
+    return fail(PALLAS_ERR_INVALID_ARG, "rope: output strides at which heads of %d overlap", head_dim);
+  if (d_x == d_y && ((num_tokens > 1 && x_token_stride != y_token_stride) || (n_heads > 1 && x_head_stride != y_head_stride)))
+    return fail(PALLAS_ERR_INVALID_ARG, "rope: in place with other strides");
   pallas::RopeParams p;
   p.x = static_cast<const uint16_t*>(d_x);
   p.y = static_cast<uint16_t*>(d_y);

@@ -88,6 +88,27 @@ def test_rope_limits(P):
     assert rope_rc(P, tokens=0) == P.Status.OK           # nothing to do: nothing is touched
 
 
+@pytest.mark.parametrize("tokens,heads,yt,yh,ok", [
+    (4, 2, 128, 64, True), (4, 2, 64, 256, True),            # heads of a token side by side, tokens of a head
+    (4, 2, 127, 64, False), (4, 2, 64, 255, False), (4, 2, 64, 64, False), (4, 3, 96, 64, False),
+    (1, 2, 0, 64, True), (4, 1, 64, 0, True), (1, 2, 0, 63, False), (2, 1, 63, 0, False),
+    (2, 2, 1 << 62, 1 << 61, True), (4, 1 << 14, 1 << 20, 64, True), (4, 1 << 14, (1 << 20) - 1, 64, False)])
+def test_rope_output_heads_do_not_overlap(P, tokens, heads, yt, yh, ok):
+    """Strides that pass are refused by the next check (in place with other strides), so that nothing is enqueued."""
+    at = sorted(t * yt + h * yh for t in range(tokens) for h in range(heads))
+    assert all(b - a >= 64 for a, b in zip(at, at[1:])) == ok
+    assert rope_rc(P, tokens=tokens, heads=heads, x=FAKE, y=FAKE, yt=yt, yh=yh, xt=yt + 8, xh=yh + 8) == P.Status.INVALID_ARG
+    assert ("in place" if ok else "overlap") in P.pallas_last_error()
+
+
+@pytest.mark.parametrize("m", [1e-300, 2.0 ** -127, 2.0 ** 127, 1e300])
+def test_plan_magnitude_has_a_reciprocal(P, m):
+    cfg, plan = RopeConfigC(**{**GOOD, "magnitude": m}), RopePlan()
+    assert P.lib().pallas_rope_init(C.byref(cfg), C.byref(plan)) == P.Status.INVALID_ARG
+    for fine in (2.0 ** -126, 2.0 ** 126):
+        assert P.pallas_rope_init(64, 1e4, magnitude=fine).magnitude == fine
+
+
 # ------------------------------------------------------------------ 8-bit pool
 def quant_pool(**kw):
     a = dict(codes=FAKE, scales=FAKE, num_pages=8, page_size=16, n_layers=2, n_kv_heads=4, head_dim=64, format=1)
