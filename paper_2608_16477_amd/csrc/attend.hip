@@ -13,9 +13,9 @@
 //   us of a call, against a workgroup per KV head and split of a sequence, of a length
 // that followed from the sequence's own (the first form): 64 sequences of 500 to 8000
 // keys, E4M3, 64 / 8 heads of 128 (344 MB), 87 -> 68; 131,071 keys INT8 (277 MB) 65 -> 57; 60,001
-// and 33,333 keys bf16, 32 / 8 heads (383 MB), 79 -> 69; 8 sequences of 1000 to 8000 keys
-// bf16 (106 MB) 32 -> 28.  The first launch of these four reads what it has to and no more, at
-// 5.7, 5.7, 6.3 and 4.7 TB/s; the join takes 4 to 5.  LDS has no bank conflict.  Calls that
+// and 33,333 keys bf16, 32 / 8 heads (383 MB), 79 -> 68; 8 sequences of 1000 to 8000 keys
+// bf16 (106 MB) 32 -> 27.  The first launch of these four reads what it has to and no more, at
+// 5.6, 5.7, 6.4 and 5.1 TB/s; the join takes 4 to 5.  LDS has no bank conflict.  Calls that
 // do not fill the chip are a chain of loads, which the way to a range is longer than: they
 // keep a workgroup per split (attend_split_kernel).
 //
@@ -156,6 +156,7 @@ struct Wave {
   uint32_t kb0, vb0;      // where this lane reads: a K block at (row l16, chunk q4), a V block transposed
   u32x4* ring;
   u32x4 qf[D / 32];
+  u32x4 qn[D / 32];       // of the sequence that comes next
   f32x4 acc[DT];          // lane: dimensions 16 dt + 4 q4 .. + 3 of head l16
   float m, lsum;          // (lsum: of this lane's keys)
 
@@ -186,12 +187,12 @@ struct Wave {
   // Q: the MFMA's B operand, column l16 = head h0 + l16 of nh (the last one again where
   // there are fewer).  Its dimensions follow what a lane reads of K: bf16, chunk 4 kk + q4;
   // 8 bits, half kk % 2 of chunk 4 (kk / 2) + q4.
-  __device__ __forceinline__ void load_q(const AttendParams& p, int s, int h0, int nh) {
+  __device__ __forceinline__ void load_q(const AttendParams& p, int s, int h0, int nh, u32x4* to) const {
     const int lane = threadIdx.x & 63, q4 = lane >> 4, l16 = lane & 15;
     const uint16_t* q = p.q + s * p.q_stride + int64_t(h0 + min(l16, nh - 1)) * D;
 #pragma unroll
     for (int kk = 0; kk < D / 32; ++kk)
-      qf[kk] = *reinterpret_cast<const u32x4*>(q + (T == kCacheBf16 ? 32 * kk + 8 * q4 : 64 * (kk / 2) + 16 * q4 + 8 * (kk % 2)));
+      to[kk] = *reinterpret_cast<const u32x4*>(q + (T == kCacheBf16 ? 32 * kk + 8 * q4 : 64 * (kk / 2) + 16 * q4 + 8 * (kk % 2)));
   }
   // Waited for once, where this stands, and not inside the stream.
   __device__ __forceinline__ void await_q() {
@@ -241,16 +242,22 @@ struct Wave {
     }
   }
 
-  // Blocks [i, stop), block n in stage n % kStages, the loads of the next kStages - 1 in
-  // flight; `blocks`: all that the wave takes.
+  // The oldest of the kStages blocks whose loads were issued is here.
+  __device__ __forceinline__ void await_block() const {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kStages - 1) * S::kLoads) : "memory");
+  }
+
+  // Blocks [i, stop), i below it, block n in stage n % kStages, the loads of the next kStages
+  // - 1 in flight; `blocks`: all that the wave takes.  Block i is here, and block `stop` at
+  // the end: what the wave stores and loads between two calls is behind the ring's loads, and
+  // a wait at the head of a block would empty the ring to get past it.
   __device__ __forceinline__ void stream(const AttendParams& p, int& i, int stop, int blocks) {
     const int lane = threadIdx.x & 63, q4 = lane >> 4;
 #pragma unroll 1
-    for (; i < stop; ++i) {
+    do {
       const int stage = static_cast<int>(static_cast<unsigned>(i) % kStages);
       const u32x4* const Kst = ring + stage * S::kSlots;
       const u32x4* const Vst = Kst + kBlk * CH;
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kStages - 1) * S::kLoads) : "memory");   // this block is here
       f32x4 sc[2] = {f32x4{}, f32x4{}};
       if constexpr (T == kCacheBf16) {
 #pragma unroll
@@ -343,7 +350,8 @@ struct Wave {
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this block's LDS reads are done
       issue(p, i + kStages, i + kStages < blocks, stage);
-    }
+      await_block();
+    } while (++i < stop);
   }
 };
 
@@ -453,7 +461,7 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
     const int f0 = r * each, f1 = min(f0 + each, total), blocks = f1 - f0;
     seek(f0);
     if (s >= p.seqs) break;                     // (lengths that changed since `total`)
-    w.load_q(p, s, h0, nh);
+    w.load_q(p, s, h0, nh, w.qf);
     // Pages of the range's blocks.
     w.page = w.keys = 0;
     const int f = f0 + lane / 2;
@@ -478,35 +486,43 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
 #pragma unroll
     for (int i = 0; i < kStages; ++i) w.issue(p, i, i < blocks, i);
     w.await_q();
+    w.await_block();
     w.begin();
-    for (int i = 0; s < p.seqs;) {
-      const int nb = blocks_of(length(s));
-      const int begin = f0 + i - base;          // the sequence's block at i
-      w.stream(p, i, min(blocks, base + nb - f0), blocks);
+    for (int i = 0;;) {
+      const int cur = s, at = f0 + i - base, end = base + blocks_of(length(s));     // at: the sequence's block at i
+      const int stop = min(blocks, end - f0);
+      // The next sequence that has keys, and its query, are there when this one ends (us;
+      // found and read after it, 1000 rows of 100 keys E4M3 57 (60), 200 of 700 bf16 34.1
+      // (35.4), 8 of 1000 to 8000 26.8 (27.8); on equal long rows within 1%).
+      bool more = false;
+      if (stop < blocks) {
+        seek(f0 + stop);
+        more = s < p.seqs;
+      }
+      w.load_q(p, more ? s : cur, h0, nh, w.qn);
+      w.stream(p, i, stop, blocks);
+#pragma unroll
+      for (int kk = 0; kk < D / 32; ++kk) w.qf[kk] = w.qn[kk];
+      w.await_q();
       const float l = rows_sum(w.lsum);
-      const int end = base + nb;
-      const bool whole = begin == 0 && end <= f1;
+      const bool whole = at == 0 && end <= f1;
       if (l16 < nh) {
         if (whole) {
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt) write_row(p, s, h0 + l16, 16 * dt + 4 * q4, w.acc[dt], w.m, l);
+          for (int dt = 0; dt < DT; ++dt) write_row(p, cur, h0 + l16, 16 * dt + 4 * q4, w.acc[dt], w.m, l);
         } else {
           // Ranges and sequences advance together, so r + s numbers the records.
-          const int64_t rec = (int64_t(r) + s) * p.Hq + h0 + l16;
+          const int64_t rec = (int64_t(r) + cur) * p.Hq + h0 + l16;
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(p.part_o + rec * D + 16 * dt + 4 * q4) = w.acc[dt];
           if (q4 == 0) *reinterpret_cast<f32x2*>(p.part_ml + rec * 2) = f32x2{w.m, l};
         }
       }
-      if (begin == 0 && head == 0 && lane == 0) {
+      if (at == 0 && head == 0 && lane == 0) {
         // The row's records: none, or from here to the range of its last block.
-        reinterpret_cast<int2*>(p.parts)[s] = int2{r, whole ? 0 : (end - 1) / each - r + 1};
+        reinterpret_cast<int2*>(p.parts)[cur] = int2{r, whole ? 0 : (end - 1) / each - r + 1};
       }
-      if (i >= blocks) break;
-      // On to the next sequence that has keys.
-      seek(f0 + i);
-      if (s >= p.seqs) break;
-      w.load_q(p, s, h0, nh);
+      if (!more) break;
       w.begin();
     }
   }
@@ -541,7 +557,7 @@ __global__ __launch_bounds__(kBoundThreads) void attend_split_kernel(AttendParam
   // The split's pages (at most 64) beside the row's length.
   int page = p.bt[int64_t(s) * p.max_pages + min(2 * f0 + lane, p.max_pages - 1)];
   Wave<D, T, kWaves> w;
-  w.load_q(p, s, h0, nh);
+  w.load_q(p, s, h0, nh, w.qf);
   const int len = row_length(p, s);
   w.init(p, kh, lds + wave * S::kRing);
   const int blocks_all = blocks_of(len), all = min(max(blocks_all - f0, 0), per);
@@ -560,9 +576,10 @@ __global__ __launch_bounds__(kBoundThreads) void attend_split_kernel(AttendParam
 #pragma unroll
   for (int i = 0; i < kStages; ++i) w.issue(p, i, i < blocks, i);
   w.await_q();
+  w.await_block();
   w.begin();
   int i = 0;
-  w.stream(p, i, blocks, blocks);
+  if (blocks > 0) w.stream(p, i, blocks, blocks);
   // The waves' parts, each in its own ring once nothing is in flight there: [head][dim],
   // then (maximum, sum) per head.
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
