@@ -478,7 +478,7 @@ int pallas_quant_load(const pallas_quant_pool* pool, int32_t layer, int32_t num_
  * outside [0, max_length] is cut to it and raises PALLAS_DEVERR_LENGTH; keys on
  * pages outside [0, num_pages) are masked and raise PALLAS_DEVERR_PAGE, in *d_err
  * (nullable).  What is in slots behind a length has no effect.
- *   Scores, softmax statistics and sums are float32.  The work is divided by the
+ *   Scores, softmax statistics, weights and sums are float32.  The work is divided by the
  * lengths of the call and max_length, so a row's last bits follow them, not the
  * other rows' queries or keys.  d_lengths may not change during the call.
  * The workspace (device, 256-byte aligned, pallas_attend_workspace_size bytes)
