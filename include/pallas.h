@@ -394,10 +394,10 @@ int pallas_rope_init(const pallas_rope_config* cfg, pallas_rope_plan* plan);
  * d_x with the same strides (in place); otherwise heads read and heads written
  * must not overlap.  Of d_y's two dimensions one must step over all of the other
  * (INVALID_ARG: heads written would overlap).  d_positions (int32, device, [num_tokens]) may hold any
- * int32; angles are exact to 2^-31 turn at every one.  inverse = 1 takes a
- * rotation by the same plan and position back (angle -p f_i, factor 1 / m), so
- * it also moves a cached K row: back from p, then on to q.  Rounded once, from
- * float32.  2-byte alignment suffices; pointers 16-byte aligned, strides and
+ * int32: whole turns are dropped exactly, and sine and cosine are within 2^-23 at
+ * every one.  inverse = 1 takes a rotation by the same plan and position back
+ * (angle -p f_i, factor 1 / m), so it also moves a cached K row: back from p, then
+ * on to q.  Rounded once, from float32.  2-byte alignment suffices; pointers 16-byte aligned, strides and
  * head_dim multiples of 8 and rotary_dim a multiple of 8 are faster.  num_tokens
  * below 2^24, n_heads * head_dim at most 2^20 (UNSUPPORTED). */
 int pallas_rope_apply(const pallas_rope_plan* plan, int32_t inverse, int32_t num_tokens,

@@ -6,7 +6,8 @@
 // 2^64 is the angle without its whole turns, exactly, at any position, so far
 // positions lose nothing and nothing needs 64-bit floating point.  The two top bits
 // (rounded) are the quarter, and what is left, within an eighth of a turn,
-// goes through the Taylor polynomials of sine and cosine.
+// goes through the Taylor polynomials of sine and cosine in float32: both are within 2^-23
+// of the exact angle's (2^-23.2 at worst, most of it the 24 bits of what is left).
 //
 // The floor is one read and one write of the rows: 3000 tokens of 72 heads of 128 (111 MB)
 // 22 us, 16,000 (590 MB) 115 us, 5.0 and 5.1 TB/s with the launch; one token 2.8 us.
