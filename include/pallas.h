@@ -412,9 +412,12 @@ int pallas_rope_apply(const pallas_rope_plan* plan, int32_t inverse, int32_t num
  * (device, 16-byte aligned).  With a = the row's largest magnitude:
  *   E4M3  scale = 2^e, the least power of two (at least 2^-126) with a / scale <=
  *         448; code = x / scale rounded to nearest even (OCP 8-bit float, 4
- *         exponent and 3 mantissa bits): reading back rounds nothing more
+ *         exponent and 3 mantissa bits): reading back rounds nothing more, but
+ *         values from 248 * 2^120 on become 2^128, which is no bf16 value: it
+ *         reads back, and can attend, as an infinity
  *   INT8  scale = a / 127; code = x * (127 / a) rounded to nearest even in
- *         [-127, 127] (float32 arithmetic); rows with a < 2^-100 count as zero
+ *         [-127, 127] (float32 arithmetic: a nearest code, either one where
+ *         127 x / a is halfway); rows with a < 2^-100 count as zero
  * A row of zeros has scale 0.  A row with an infinity or a NaN has scale NaN and
  * codes 0: it reads back, and attends, as NaN.
  *   Codes and scales are moved by pallas_pack_suffix_blocks and

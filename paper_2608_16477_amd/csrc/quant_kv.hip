@@ -3,7 +3,8 @@
 //
 //   E4M3  scale = 2^e, the least with a <= 448 * 2^e (a: the row's largest
 //         magnitude).  A power of two costs a floating-point code no precision and
-//         makes both directions exact but for the code's own rounding.
+//         makes both directions exact but for the code's own rounding (and for 2^128,
+//         which the last 8 of bf16's magnitudes round to).
 //   INT8  scale = a / 127: a power of two would cost up to one of seven bits.
 //
 // Both are bound by memory: 2 d bytes and d + 4 bytes per row (34,708 tokens of 8 heads of
