@@ -467,14 +467,22 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
     w.page = w.keys = 0;
     const int f = f0 + lane / 2;
     int from = 0, key0 = -1;
-    for (int n = s, at = base; at < f1 && n < p.seqs; ++n) {
-      const int len = length(n), nb = blocks_of(len);
-      if (f >= at && f < at + nb && f < f1) {
-        from = n;
-        key0 = ((f - at) * 2 + lane % 2) * kPage;
+    for (const int s0 = s, base0 = base;;) {
+      const int len = length(s), nb = blocks_of(len);
+      if (f >= base && f < base + nb && f < f1) {
+        from = s;
+        key0 = ((f - base) * 2 + lane % 2) * kPage;
         w.keys = min(max(len - key0, 0), kPage);
       }
-      at += nb;
+      base += nb;
+      ++s;
+      // Rows without keys are jumped over (250 between two of 4000 keys bf16, 32 / 8 heads: 19
+      // us, 42 one by one; 60,000 of them 510, 6270).
+      if (base < f1 && s < p.seqs && length(s) == 0) seek(base);
+      if (base < f1 && s < p.seqs) continue;
+      s = s0;
+      base = base0;
+      break;
     }
     if (each == 2) ahead = __builtin_amdgcn_mov_dpp(ahead, 0x108, 0xF, 0xF, false);   // row_shl:8
     if (w.keys > 0) {
