@@ -475,7 +475,7 @@ int pallas_quant_load(const pallas_quant_pool* pool, int32_t layer, int32_t num_
  * zeros and -infinity.  An infinity or a NaN in a query or in a K or V row that is
  * attended to may make the results of the heads that read it NaN, of no other.
  *   head_dim 64 or 128 (UNSUPPORTED otherwise), page_size 16, any number of
- * query heads per KV head, num_seqs up to 65535, max_length (the longest length
+ * query heads per KV head, num_seqs 1 to 65535, max_length (the longest length
  * the call can meet) at least 1 and at most max_pages * page_size; num_seqs *
  * max_length up to 2^35 (UNSUPPORTED beyond).  A length
  * outside [0, max_length] is cut to it and raises PALLAS_DEVERR_LENGTH; keys on

@@ -456,14 +456,16 @@ def _attend_call(call, ps, dev, layer, q, lengths, max_length, block_tables, sca
         _bad("attend: an empty err")
     if workspace.get_device() != dev or not workspace.is_contiguous():
         _bad("attend: workspace on another device, or not contiguous")
-    _launch(dev, stream, call, C.byref(ps), layer, S, H, q.data_ptr(), qs, lengths.data_ptr(), max_length,
-            block_tables.data_ptr(), pages, scale, out.data_ptr(), os_, _ptr(lse), workspace.data_ptr(), workspace.nbytes,
-            _ptr(err))
+    if S:
+        _launch(dev, stream, call, C.byref(ps), layer, S, H, q.data_ptr(), qs, lengths.data_ptr(), max_length,
+                block_tables.data_ptr(), pages, scale, out.data_ptr(), os_, _ptr(lse), workspace.data_ptr(), workspace.nbytes,
+                _ptr(err))
 
 
 def pallas_attend_kv(pool, layer: int, q, lengths, max_length: int, block_tables, scale: float, out, workspace, lse=None,
                      err=None, stream=None):
-    """One new token per sequence: ``q``, ``out`` bf16 [num_seqs, Hq, d] (any row stride) over a bf16 pool."""
+    """One new token per sequence: ``q``, ``out`` bf16 [num_seqs, Hq, d] (any row stride) over a bf16 pool.  As with
+    the other operators nothing is enqueued for an empty batch."""
     dev = pool.get_device()
     _whole(pool, "attend: pool", (_torch or _load_torch()).bfloat16, 6, dev)
     _attend_call(lib().pallas_attend_kv, kv_pool_struct(pool), dev, layer, q, lengths, max_length, block_tables, scale, out,
