@@ -1,7 +1,7 @@
 // Attention of one new token per sequence over a paged KV cache (bf16, E4M3 or
 // INT8 rows).
 //
-// The kernel is bound by the K/V stream, so the stream is what is divided: the 32-key
+// Calls that fill the chip live off the K/V stream, so the stream is what is divided: the 32-key
 // blocks of all sequences, one behind the other, are cut into ranges of equal length
 // (attend_blocks), as many as waves are resident at once (attend_ranges), and a wave
 // takes a range of one KV head and up to 16 query heads that share it.  Its loads go on
@@ -12,12 +12,15 @@
 // accumulated across waves, so results are the same in every run.
 //   us of a call, against a workgroup per KV head and split of a sequence, of a length
 // that followed from the sequence's own (the first form): 64 sequences of 500 to 8000
-// keys, E4M3, 64 / 8 heads of 128 (344 MB), 87 -> 68; 131,071 keys INT8 (277 MB) 65 -> 57; 60,001
+// keys, E4M3, 64 / 8 heads of 128 (344 MB), 87 -> 69; 131,071 keys INT8 (277 MB) 65 -> 57; 60,001
 // and 33,333 keys bf16, 32 / 8 heads (383 MB), 79 -> 68; 8 sequences of 1000 to 8000 keys
 // bf16 (106 MB) 32 -> 27.  The first launch of these four reads what it has to and no more, at
-// 5.6, 5.7, 6.4 and 5.1 TB/s; the join takes 4 to 5.  LDS has no bank conflict.  Calls that
-// do not fill the chip are a chain of loads, which the way to a range is longer than: they
-// keep a workgroup per split (attend_split_kernel).
+// 5.6, 5.6, 6.4 and 5.0 TB/s; the join takes 4 to 5.  The long bf16 call is bound by the stream
+// (a kernel that only reads such a buffer reaches 6.1); 8-bit rows are held back by what a
+// block costs beside it as well: vector instructions take 0.36 (E4M3) and 0.54 (INT8) of the
+// issue slots, bf16 0.13, and the matrix pipes are busy for 0.16, bf16 0.09.  LDS has no bank
+// conflict.  Calls that do not fill the chip are a chain of loads, which the way to a range is
+// longer than: they keep a workgroup per split (attend_split_kernel).
 //
 // Each wave moves its blocks from memory straight into a private two-stage LDS ring,
 // with the rows' scales.  Scores are S^T = K Q^T with v_mfma_f32_16x16x32_bf16 (the
@@ -718,13 +721,17 @@ hipError_t launch_split(const AttendParams& p, int groups, int splits, int per, 
 // How a call is run (us on the GPU; 8 KV heads of 128).
 //   Rows of up to kShortKeys keys, up to kShortGroups (sequence, head) pairs: a workgroup each
 // and one launch.  Its waves' rings fill a CU's LDS, or half of it where there are several
-// rows to a CU.  As ranges in parentheses: 4 rows of 60 keys bf16 4.4 (8.3), 128 of 300 E4M3
-// 21.3 (26.4); beyond the limits, 1 of 1000 11.5 (9.4), 256 of 300 38.5 (36.4).
+// rows to a CU.  As ranges in parentheses: 4 rows of 60 keys bf16 4.7 (8.3), 128 of 300 E4M3
+// 22.4 (25.9), bf16 31.9 (31.6), 128 of 500 bf16 50.4 (48.2), 180 of them 66.8 (70.1); beyond the
+// limits, 1 of 1000 E4M3 11.7 (9.6), 256 of 300 40.3 (36.1).
 //   Else splits of one or two blocks a wave, if those are at most a workgroup per CU: 1 row of
-// 4000 keys bf16 10.4 (12.3), 16,000 E4M3 15.7 (19.2), 8 of 1000 INT8 10.0 (14.1).  Four blocks
+// 4000 keys bf16 10.5 (12.5), 16,000 E4M3 15.8 (18.7), 8 of 1000 INT8 10.4 (14.3).  Four blocks
 // a wave gain nothing on equal rows and lose on others (27 of 30 to 2000 keys, 4 heads of
-// 64, 11.5 (8.5)), as do two workgroups per CU (16,000 keys 19.1).
+// 64, 11.7 (8.7)), as do two workgroups per CU (16,000 keys 19.3).
 //   Else ranges.
+//   The host knows max_length alone, so the bound that a call states chooses.  With room
+// for 4096 and for 32,768 keys: 4 rows of 60 bf16 9.1, 9.0 (4.7 with 60), 1 of 500 8.4, 10.7 (7.6),
+// 1 of 4000 10.5, 14.1; 8 of 1000 to 8000 and 64 E4M3 level.
 constexpr int kShortKeys = 512;
 constexpr int kShortGroups = 1536;
 constexpr int kSplitBlocks = 2;
