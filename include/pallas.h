@@ -18,10 +18,10 @@
  *   pallas_assemble_kv         scatter chunks into the target block table
  *   pallas_decode_step         one decode step over an assembled cache
  *   pallas_rope_*              rotary positions of Q and K rows
- *   pallas_quant_store, _load  an 8-bit cache: rows quantised as they are
+ *   pallas_quant_store, _load  an 8- or 4-bit cache: rows quantised as they are
  *                              written, and read back
  *   pallas_attend_*            attention of one new token per sequence over a
- *                              paged cache, bf16 or 8-bit
+ *                              paged cache, bf16, 8- or 4-bit
  *   pallas_check_coverage      host-only [0, n) coverage check
  *   pallas_window_*, pallas_ewma_update, pallas_admit, pallas_waste_bound
  *                              host-only Scheduler Engine (when to migrate)
@@ -329,7 +329,7 @@ int pallas_decode_step_static(pallas_model* m, int32_t num_seqs, const int32_t* 
 
 /* ------------------------------------------------------------------------
  * Operators on the cache, for callers that run a decoder's layers themselves
- * (another architecture, a long-context rotary, an 8-bit cache).  A new token
+ * (another architecture, a long-context rotary, an 8- or 4-bit cache).  A new token
  * of each sequence takes pallas_rope_apply on its Q and K heads, the store
  * (pallas_quant_store, or the caller's own into a bf16 pool) and
  * pallas_attend_*; a prompt's rows take the first two.  Per-row arguments
@@ -405,11 +405,15 @@ int pallas_rope_apply(const pallas_rope_plan* plan, int32_t inverse, int32_t num
                       const void* d_x, int64_t x_token_stride, int64_t x_head_stride, void* d_y,
                       int64_t y_token_stride, int64_t y_head_stride, void* stream);
 
-/* An 8-bit paged KV pool.  A row (one token's K or V of one KV head) is head_dim
- * codes and one float32 scale, and stands for code * scale:
+/* An 8- or 4-bit paged KV pool.  A row (one token's K or V of one KV head) is head_dim
+ * codes with one float32 scale, or with a scale for each quarter of it, and stands for
+ * code * scale:
  *   codes  [n_layers][2 (K, V)][num_pages][page_size][n_kv_heads][head_dim] bytes
+ *          (E2M1: [head_dim / 2], element 2 i in the low half of byte i)
  *   scales [n_layers][2][num_pages][page_size][n_kv_heads] float32
- * (device, 16-byte aligned).  With a = the row's largest magnitude:
+ *          (E2M1: four bytes in place of each, one per quarter of the row)
+ * (device, 16-byte aligned).  With a = the largest magnitude of the row (E2M1: of the
+ * quarter):
  *   E4M3  scale = 2^e, the least power of two (at least 2^-126) with a / scale <=
  *         448; code = x / scale rounded to nearest even (OCP 8-bit float, 4
  *         exponent and 3 mantissa bits): reading back rounds nothing more, but
@@ -418,12 +422,16 @@ int pallas_rope_apply(const pallas_rope_plan* plan, int32_t inverse, int32_t num
  *   INT8  scale = a / 127; code = x * (127 / a) rounded to nearest even in
  *         [-127, 127] (float32 arithmetic: a nearest code, either one where
  *         127 x / a is halfway); rows with a < 2^-100 count as zero
- * A row of zeros has scale 0.  A row with an infinity or a NaN has scale NaN and
- * codes 0: it reads back, and attends, as NaN.
+ *   E2M1  scale = 2^(b - 127) of a byte b (OCP E8M0), the least power of two, at most
+ *         2^125, with a / scale <= 6; code = x / scale rounded to nearest even, at most
+ *         6 (OCP 4-bit float, 2 exponent bits and 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3,
+ *         4, 6): reading back rounds nothing more; quarters with a < 2^-100 count as zero
+ * A row (quarter) of zeros has scale 0 (b 0, codes 0).  A row (quarter) with an infinity
+ * or a NaN has scale NaN (b 255) and codes 0: it reads back, and attends, as NaN.
  *   Codes and scales are moved by pallas_pack_suffix_blocks and
  * pallas_assemble_kv, which copy bits: the codes as a pallas_kv_pool of head_dim
- * / 2, the scales as one of head_dim 2 (n_kv_heads a multiple of 4). */
-typedef enum { PALLAS_QUANT_E4M3 = 1, PALLAS_QUANT_INT8 = 2 } pallas_quant_format;
+ * / 2 (E2M1: / 4), the scales as one of head_dim 2 (n_kv_heads a multiple of 4). */
+typedef enum { PALLAS_QUANT_E4M3 = 1, PALLAS_QUANT_INT8 = 2, PALLAS_QUANT_E2M1 = 4 } pallas_quant_format;
 typedef struct {
   void* codes;
   float* scales;
@@ -492,7 +500,7 @@ int pallas_attend_kv(const pallas_kv_pool* pool, int32_t layer, int32_t num_seqs
                      float scale, void* d_out, int64_t out_stride, float* d_lse, void* d_workspace,
                      size_t ws_bytes, int32_t* d_err, void* stream);
 
-/* The same over an 8-bit pool.  One layer's scales must stay below 4 GiB
+/* The same over an 8- or 4-bit pool.  One layer's scales must stay below 4 GiB
  * (UNSUPPORTED). */
 int pallas_attend_quant(const pallas_quant_pool* pool, int32_t layer, int32_t num_seqs,
                         int32_t n_q_heads, const void* d_q, int64_t q_stride,

@@ -1,5 +1,5 @@
 """Operators on the cache, in float64: rotary positions (layouts, partial heads,
-long-context scaling), the 8-bit row formats, attention of one new token.
+long-context scaling), the 8- and 4-bit row formats, attention of one new token.
 
 Written from the formulas that ``include/pallas.h`` states.
 """
@@ -92,6 +92,44 @@ def quantise(x, fmt):
 def dequantise(codes, scales, fmt):
     v = codes.view(np.int8).astype(np.float64) if fmt == "int8" else e4m3_value(codes)
     return v * np.asarray(scales, dtype=np.float64)[..., None]
+
+
+# ------------------------------------------------------------------ 4-bit rows
+E2M1 = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])      # sign apart: 2 exponent bits (bias 1), 1 mantissa bit
+
+
+def e2m1_code(y):
+    """Nearest E2M1 code (4 bits), ties to the even code; |y| beyond 6 is 6."""
+    away = np.abs(np.abs(y)[..., None] - E2M1)
+    best = away == away.min(axis=-1, keepdims=True)                # one, or two neighbours
+    even = best & (np.arange(8) % 2 == 0)
+    return np.where(even.any(axis=-1), even.argmax(axis=-1), best.argmax(axis=-1)) | np.where(np.signbit(y), 8, 0)
+
+
+def quantise4(x):
+    """(codes uint8 [.., d / 2], bytes uint8 [.., 4]) of the rows of x (float64 values of bf16): element 2 i in the low
+    half of byte i, a power of two 2^(byte - 127) per quarter of the row."""
+    x = np.asarray(x, dtype=np.float64)
+    d = x.shape[-1]
+    x = x.reshape(x.shape[:-1] + (4, d // 4))
+    bad = ~np.isfinite(x).all(axis=-1)
+    x = np.where(bad[..., None], 0.0, x)
+    a = np.abs(x).max(axis=-1)
+    live = a >= 2.0 ** -100
+    e = np.full(a.shape, 125)
+    for k in range(124, -104, -1):                                # the least that fits
+        e = np.where((e == k + 1) & (a <= np.ldexp(6.0, k)), k, e)
+    codes = np.where(live[..., None], e2m1_code(np.ldexp(x, -e[..., None])), 0).reshape(x.shape[:-2] + (d,))
+    unit = np.where(bad, 255, np.where(live, e + 127, 0)).astype(np.uint8)
+    return (codes[..., 0::2] | codes[..., 1::2] << 4).astype(np.uint8), unit
+
+
+def dequantise4(codes, unit):
+    d = 2 * codes.shape[-1]
+    both = np.stack([codes & 15, codes >> 4], axis=-1).reshape(codes.shape[:-1] + (4, d // 4)).astype(np.int64)
+    v = np.where(both & 8, -E2M1[both & 7], E2M1[both & 7])
+    scale = np.where(unit == 255, np.nan, np.ldexp(1.0, unit.astype(np.int64) - 127))
+    return (v * scale[..., None]).reshape(codes.shape[:-1] + (d,))
 
 
 # ------------------------------------------------------------------ attention

@@ -312,6 +312,7 @@ def pallas_decode_step_static(h, tokens, positions: Sequence[int], block_tables,
 # more than needed, so each is asked once: shape and stride as tuples, the device as an
 # index (-1: host).
 _torch = None
+_formats = None
 
 
 def _load_torch():
@@ -398,17 +399,28 @@ def pallas_rope_apply(plan: RopePlan, x, positions, out=None, inverse: bool = Fa
     return out
 
 
-def quant_pool_struct(codes, scales) -> QuantPoolC:
-    """``codes``: float8_e4m3fn or int8 [L, 2, P, page, Hkv, d]; ``scales``: float32 [L, 2, P, page, Hkv]."""
+def _quant_formats():
     torch = _torch or _load_torch()
+    # dtype of the codes -> format, codes to a value of the tensor, the scales' dtype and rank
+    return {torch.float8_e4m3fn: (1, 1, torch.float32, 5), torch.int8: (2, 1, torch.float32, 5),
+            torch.float4_e2m1fn_x2: (4, 2, torch.float8_e8m0fnu, 6)}
+
+
+def quant_pool_struct(codes, scales) -> QuantPoolC:
+    """``codes``: float8_e4m3fn or int8 [L, 2, P, page, Hkv, d] with ``scales`` float32 [L, 2, P, page, Hkv], or
+    float4_e2m1fn_x2 [L, 2, P, page, Hkv, d / 2] with float8_e8m0fnu [L, 2, P, page, Hkv, 4]."""
+    global _formats
+    if _formats is None:
+        _formats = _quant_formats()
     dtype, dev = codes.dtype, codes.get_device()
-    fmt = 1 if dtype is torch.float8_e4m3fn else 2 if dtype is torch.int8 else 0
-    if not fmt:
-        _bad(f"quant pool: codes of {dtype}, wanted float8_e4m3fn or int8")
+    kind = _formats.get(dtype)
+    if kind is None:
+        _bad(f"quant pool: codes of {dtype}, wanted float8_e4m3fn, int8 or float4_e2m1fn_x2")
+    fmt, per, of, rank = kind
     L, two, P, page, hkv, d = shape = _whole(codes, "quant pool: codes", dtype, 6, dev)
-    if two != 2 or _whole(scales, "quant pool: scales", torch.float32, 5, dev) != shape[:5]:
+    if two != 2 or _whole(scales, "quant pool: scales", of, rank, dev) != (shape[:5] if rank == 5 else shape[:5] + (4,)):
         _bad(f"quant pool: codes {tuple(shape)}, scales {tuple(scales.shape)}")
-    return QuantPoolC(codes.data_ptr(), scales.data_ptr(), P, page, L, hkv, d, fmt)
+    return QuantPoolC(codes.data_ptr(), scales.data_ptr(), P, page, L, hkv, d * per, fmt)
 
 
 def _quant_call(what, call, codes, scales, layer, k, v, positions, block_tables, seq_ids, err, stream):
@@ -474,7 +486,7 @@ def pallas_attend_kv(pool, layer: int, q, lengths, max_length: int, block_tables
 
 def pallas_attend_quant(codes, scales, layer: int, q, lengths, max_length: int, block_tables, scale: float, out,
                         workspace, lse=None, err=None, stream=None):
-    """The same over an 8-bit pool (quant_pool_struct)."""
+    """The same over an 8- or 4-bit pool (quant_pool_struct)."""
     _attend_call(lib().pallas_attend_quant, quant_pool_struct(codes, scales), codes.get_device(), layer, q, lengths,
                  max_length, block_tables, scale, out, workspace, lse, err, stream)
 

@@ -1,5 +1,5 @@
-// Attention of one new token per sequence over a paged KV cache (bf16, E4M3 or
-// INT8 rows).
+// Attention of one new token per sequence over a paged KV cache (bf16, E4M3, INT8 or
+// E2M1 rows).
 //
 // Calls that fill the chip live off the K/V stream, so the stream is what is divided: the 32-key
 // blocks of all sequences, one behind the other, are cut into ranges of equal length
@@ -34,6 +34,7 @@
 #include "common.h"
 #include "kernels.h"
 #include "paged_attn.h"
+#include "quant_rows.h"
 
 namespace pallas {
 
@@ -50,17 +51,19 @@ constexpr uint32_t kOutside = 0xFFFFFFF0u;   // a buffer offset past any range: 
 
 template <int D, CacheType T>
 struct Shape {
-  static constexpr int kElem = T == kCacheBf16 ? 2 : 1;
-  static constexpr int kRow = D * kElem;              // bytes of a head row
+  static constexpr int kRow = T == kCacheBf16 ? D * 2 : T == kCacheE2m1 ? D / 2 : D;   // bytes of a head row
   static constexpr int kCh = kRow / 16;               // 16-byte chunks of it
   static constexpr int kRowsPerLoad = 64 / kCh;       // rows per load instruction
-  static constexpr int kPerPage = kPage / kRowsPerLoad;
+  static constexpr int kPerPage = std::max(kPage / kRowsPerLoad, 1);
+  static constexpr int kPageSlots = kPerPage * 64;    // 16-byte slots of a page (E2M1 rows of 64: half of them rows)
   static constexpr int kScaleSlots = T == kCacheBf16 ? 0 : 16;   // 32 K scales, 32 V scales
-  static constexpr int kSlots = 2 * kBlk * kCh + kScaleSlots;    // 16-byte slots of a stage
+  static constexpr int kSlots = 4 * kPageSlots + kScaleSlots;    // of a stage
   static constexpr int kLoads = 4 * kPerPage + (T == kCacheBf16 ? 0 : 1);   // instructions per block
-  static constexpr int kRing = kStages * kSlots;                 // of a wave
+  static constexpr int kRing = kStages * kSlots;
+  static constexpr int kTurn = T == kCacheE2m1 ? kBlk * 4 : 0;   // 32 dimensions of V as bf16
+  static constexpr int kWaveSlots = kRing + kTurn;               // of a wave
   // attend_ranges counts on the waves that a CU's 160 KiB of LDS hold.
-  static_assert(160 * 1024 / (4 * kRing * 16) * 4 >= attend_waves(kRow), "resident waves");
+  static_assert(160 * 1024 / (4 * kWaveSlots * 16) * 4 >= attend_waves(T, D), "resident waves");
 };
 
 // Chunk swizzles of 8-bit rows of CH chunks (8 rows of 128 bytes, or 16 of 64, fill the
@@ -73,14 +76,20 @@ template <int CH>
 __device__ __forceinline__ int swz8_v(int row) {
   return CH == 8 ? ((row >> 1) & 3) | ((row >> 2) & 4) : ((row >> 2) & 1) | ((row >> 3) & 2);
 }
+// 4-bit rows of CH chunks (4 rows of 64 bytes fill the banks, or 8 of 32): the 16 rows of
+// a K read at one chunk, or, of 32 bytes, at half a chunk; the 16 rows of half a V read.
+template <int CH>
+__device__ __forceinline__ int swz4(int row) { return CH == 4 ? (row >> 2) & 3 : (row >> 3) & 1; }
 template <CacheType T, int CH>
 __device__ __forceinline__ int k_slot(int row) {
   if constexpr (T == kCacheBf16) return swz_k<CH>(row);
+  else if constexpr (T == kCacheE2m1) return CH == 4 ? swz4<CH>(row) : 0;
   else return swz8_k<CH>(row);
 }
 template <CacheType T, int CH>
 __device__ __forceinline__ int v_slot(int row) {
   if constexpr (T == kCacheBf16) return swz_v<CH>(row);
+  else if constexpr (T == kCacheE2m1) return swz4<CH>(row);
   else return swz8_v<CH>(row);
 }
 
@@ -123,6 +132,27 @@ __device__ __forceinline__ void read_pv8(uint32_t vb, int dt0, u32x2* a) {
       : "memory");
   a[0] = r0, a[1] = r1, a[2] = r2, a[3] = r3;
 }
+
+// Two output tiles of the PV operand from 32 rows of 32 bf16 dimensions at LDS byte
+// address `vb` (read_pv4; tiles XOR 32 bytes, the second page 1024 bytes further).
+__device__ __forceinline__ void read_pv2(uint32_t vb, u32x4* a) {
+  const uint32_t x1 = vb ^ 32u;
+  u32x2 l0, l1, h0, h1;
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %4\n\t"
+      "ds_read_b64_tr_b16 %1, %4 offset:1024\n\t"
+      "ds_read_b64_tr_b16 %2, %5\n\t"
+      "ds_read_b64_tr_b16 %3, %5 offset:1024\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(l0), "=&v"(h0), "=&v"(l1), "=&v"(h1)
+      : "v"(vb), "v"(x1)
+      : "memory");
+  a[0] = u32x4{l0.x, l0.y, h0.x, h0.y};
+  a[1] = u32x4{l1.x, l1.y, h1.x, h1.y};
+}
+// Slot of chunk `c` of such a row: half a transposed read (8 rows, 2 chunks of each) falls
+// on all banks.
+__device__ __forceinline__ int turn_slot(int row, int c) { return row * 4 + (c ^ ((row >> 1) & 2)); }
 
 __device__ __forceinline__ int row_length(const AttendParams& p, int s) { return min(max(p.lengths[s], 0), p.max_length); }
 
@@ -177,9 +207,15 @@ struct Wave {
       koff[n] = r * rs + static_cast<uint32_t>((c ^ k_slot<T, CH>(r)) * 16);
       voff[n] = r * rs + static_cast<uint32_t>((c ^ v_slot<T, CH>(r)) * 16);
       voff[S::kPerPage + n] = r * rs + static_cast<uint32_t>((c ^ v_slot<T, CH>(kPage + r)) * 16);
+      if (S::kRowsPerLoad > kPage && r >= kPage) koff[n] = voff[n] = voff[S::kPerPage + n] = kOutside;   // (no such row)
     }
     kb0 = static_cast<uint32_t>(l16 * CH + (q4 ^ k_slot<T, CH>(l16)));
-    if constexpr (T == kCacheBf16) {
+    if constexpr (T == kCacheE2m1) {
+      // (K in units of what a lane reads of a row, 16 or 8 bytes; V from the turned rows)
+      if constexpr (CH == 2) kb0 = static_cast<uint32_t>(l16 * 4 + q4);
+      const int key = 4 * q4 + (l16 >> 2);
+      vb0 = static_cast<uint32_t>(turn_slot(key, (l16 & 3) >> 1) * 16 + (l16 & 1) * 8);
+    } else if constexpr (T == kCacheBf16) {
       const int key = 4 * q4 + (l16 >> 2);
       vb0 = static_cast<uint32_t>(key * D * 2 + ((v_slot<T, CH>(key) | ((l16 & 3) >> 1)) * 16) + (l16 & 1) * 8);
     } else {
@@ -190,13 +226,14 @@ struct Wave {
 
   // Q: the MFMA's B operand, column l16 = head h0 + l16 of nh (the last one again where
   // there are fewer).  Its dimensions follow what a lane reads of K: bf16, chunk 4 kk + q4;
-  // 8 bits, half kk % 2 of chunk 4 (kk / 2) + q4.
+  // 8 bits, half kk % 2 of chunk 4 (kk / 2) + q4; 4 bits, eight codes of quarter q4.
   __device__ __forceinline__ void load_q(const AttendParams& p, int s, int h0, int nh, u32x4* to) const {
     const int lane = threadIdx.x & 63, q4 = lane >> 4, l16 = lane & 15;
     const uint16_t* q = p.q + s * p.q_stride + int64_t(h0 + min(l16, nh - 1)) * D;
 #pragma unroll
     for (int kk = 0; kk < D / 32; ++kk)
-      to[kk] = *reinterpret_cast<const u32x4*>(q + (T == kCacheBf16 ? 32 * kk + 8 * q4 : 64 * (kk / 2) + 16 * q4 + 8 * (kk % 2)));
+      to[kk] = *reinterpret_cast<const u32x4*>(
+          q + (T == kCacheBf16 ? 32 * kk + 8 * q4 : T == kCacheE2m1 ? D / 4 * q4 + 8 * kk : 64 * (kk / 2) + 16 * q4 + 8 * (kk % 2)));
   }
   // Waited for once, where this stands, and not inside the stream.
   __device__ __forceinline__ void await_q() {
@@ -227,10 +264,10 @@ struct Wave {
       const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void*)(v + base), 0, range, kRsrcFlags);
 #pragma unroll
       for (int n = 0; n < S::kPerPage; ++n)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void*)(st + (h * S::kPerPage + n) * 64), 16, koff[n], 0, 0, kAuxStream);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void*)(st + h * S::kPageSlots + n * 64), 16, koff[n], 0, 0, kAuxStream);
 #pragma unroll
       for (int n = 0; n < S::kPerPage; ++n)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void*)(st + kBlk * CH + (h * S::kPerPage + n) * 64), 16,
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void*)(st + (2 + h) * S::kPageSlots + n * 64), 16,
                                                  voff[h * S::kPerPage + n], 0, 0, kAuxStream);
     }
     if constexpr (T != kCacheBf16) {
@@ -242,7 +279,7 @@ struct Wave {
       const bool live = key < (second ? nv[1] : nv[0]);
       const __amdgpu_buffer_rsrc_t scales = __builtin_amdgcn_make_buffer_rsrc(
           (void*)p.scales, 0, static_cast<uint32_t>(p.num_pages) * (2 * kPage * 4) * p.Hkv, kRsrcFlags);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(scales, (lds_void*)(st + 2 * kBlk * CH), 4, live ? row * 4 : kOutside, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(scales, (lds_void*)(st + 4 * S::kPageSlots), 4, live ? row * 4 : kOutside, 0, 0, 0);
     }
   }
 
@@ -256,37 +293,51 @@ struct Wave {
   // the end: what the wave stores and loads between two calls is behind the ring's loads, and
   // a wait at the head of a block would empty the ring to get past it.
   __device__ __forceinline__ void stream(const AttendParams& p, int& i, int stop, int blocks) {
-    const int lane = threadIdx.x & 63, q4 = lane >> 4;
+    const int lane = threadIdx.x & 63, q4 = lane >> 4, l16 = lane & 15;
 #pragma unroll 1
     do {
       const int stage = static_cast<int>(static_cast<unsigned>(i) % kStages);
       const u32x4* const Kst = ring + stage * S::kSlots;
-      const u32x4* const Vst = Kst + kBlk * CH;
+      const u32x4* const Vst = Kst + 2 * S::kPageSlots;
       f32x4 sc[2] = {f32x4{}, f32x4{}};
       if constexpr (T == kCacheBf16) {
 #pragma unroll
         for (int kk = 0; kk < D / 32; ++kk)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const bf16x8 a = __builtin_bit_cast(bf16x8, Kst[(kb0 ^ (kk * 4u)) + h * (kPage * CH)]);
+            const bf16x8 a = __builtin_bit_cast(bf16x8, Kst[(kb0 ^ (kk * 4u)) + h * S::kPageSlots]);
             sc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, qf[kk]), sc[h], 0, 0, 0);
           }
+      } else if constexpr (T == kCacheE2m1) {
+        // A lane's quarter of a row has one scale, which goes into the conversion.
+        const uint8_t* units = reinterpret_cast<const uint8_t*>(Kst + 4 * S::kPageSlots) + l16 * 4 + q4;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float unit = __uint_as_float(static_cast<uint32_t>(units[h * kPage * 4]) << 23);
+          uint32_t c[D / 32];
+          if constexpr (D == 128) *reinterpret_cast<u32x4*>(c) = Kst[kb0 + h * S::kPageSlots];
+          else *reinterpret_cast<u32x2*>(c) = reinterpret_cast<const u32x2*>(Kst + h * S::kPageSlots)[kb0];
+#pragma unroll
+          for (int kk = 0; kk < D / 32; ++kk)
+            sc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, e2m1_bf16(c[kk], unit)),
+                                                            __builtin_bit_cast(bf16x8, qf[kk]), sc[h], 0, 0, 0);
+        }
       } else {
 #pragma unroll
         for (int j = 0; j < D / 64; ++j)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const u32x4 a = Kst[(kb0 ^ (j * 4u)) + h * (kPage * CH)];
+            const u32x4 a = Kst[(kb0 ^ (j * 4u)) + h * S::kPageSlots];
             sc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_bf16<T>(a.x, a.y), __builtin_bit_cast(bf16x8, qf[2 * j]), sc[h], 0, 0, 0);
             sc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_bf16<T>(a.z, a.w), __builtin_bit_cast(bf16x8, qf[2 * j + 1]), sc[h], 0, 0, 0);
           }
       }
       float pr[8], vs[8];
-      if constexpr (T == kCacheBf16) {
+      if constexpr (T == kCacheBf16 || T == kCacheE2m1) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) pr[e] = sc[e / 4][e % 4] * p.scale_log2;
       } else {
-        const f32x4* f = reinterpret_cast<const f32x4*>(Kst + 2 * kBlk * CH);
+        const f32x4* f = reinterpret_cast<const f32x4*>(Kst + 4 * S::kPageSlots);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const f32x4 ks = f[4 * h + q4], w = f[8 + 4 * h + q4];
@@ -321,7 +372,7 @@ struct Wave {
       for (int e = 0; e < 8; ++e) {
         pr[e] = __builtin_amdgcn_exp2f(pr[e] - mc);
         lsum += pr[e];
-        if constexpr (T != kCacheBf16) pr[e] *= vs[e];
+        if constexpr (T == kCacheE4m3 || T == kCacheInt8) pr[e] *= vs[e];
       }
       bf16x8 pb[3];
 #pragma unroll
@@ -341,6 +392,30 @@ struct Wave {
 #pragma unroll
           for (int part = 2; part >= 0; --part)
             acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va[dt]), pb[part], acc[dt], 0, 0, 0);
+      } else if constexpr (T == kCacheE2m1) {
+        // 32 dimensions at a time: a pair of lanes turns 32 codes of a key into bf16, with
+        // their scales (a transposed word would hold keys of eight scales), and they are read
+        // back transposed.
+        const int key = lane >> 1, half = lane & 1;
+        const uint32_t w = reinterpret_cast<const uint32_t*>(Kst + 4 * S::kPageSlots)[kBlk + key] >> (D == 64 ? 8 * half : 0);
+        const u32x4* const row = Vst + key / kPage * S::kPageSlots + key % kPage * CH;
+        u32x4* const turn = ring + S::kRing;
+        const uint32_t vt = vb0 + static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)turn));
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+          const u32x2 c = reinterpret_cast<const u32x2*>(row + (i ^ v_slot<T, CH>(key)))[half];
+          constexpr int kStep = D == 64 ? 16 : 8;     // bits between the scales of two steps
+          const float unit = __uint_as_float(i * kStep < 24 ? w << (23 - i * kStep) : w >> 1);
+          turn[turn_slot(key, 2 * half)] = e2m1_bf16(c.x, unit);
+          turn[turn_slot(key, 2 * half + 1)] = e2m1_bf16(c.y, unit);
+          u32x4 va[2];
+          read_pv2(vt, va);
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int part = 2; part >= 0; --part)
+              acc[2 * i + t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va[t]), pb[part], acc[2 * i + t], 0, 0, 0);
+        }
       } else {
         u32x2 vc[DT];
 #pragma unroll
@@ -385,7 +460,7 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
   constexpr int DT = D / 16;
   // One array: with several, the compiler's alias scopes make LDS reads of a
   // stage wait for the loads in flight into the other.
-  __shared__ __attribute__((aligned(256))) u32x4 lds[kWaves * S::kRing];
+  __shared__ __attribute__((aligned(256))) u32x4 lds[kWaves * S::kWaveSlots];
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -406,7 +481,7 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
 
   const int h0 = kh * p.G + group * kAttendGroup, nh = min(kAttendGroup, p.G - group * kAttendGroup);
   Wave<D, T, 0> w;
-  w.init(p, kh, lds + wave * S::kRing);
+  w.init(p, kh, lds + wave * S::kWaveSlots);
 
   // All blocks of the call, and the ranges they make.  coarse: blocks of the first (lane +
   // 1) 64ths of the sequences.
@@ -548,7 +623,7 @@ template <int D, CacheType T, int kWaves>
 __global__ __launch_bounds__(kBoundThreads) void attend_split_kernel(AttendParams p, int groups, int splits, int per) {
   using S = Shape<D, T>;
   constexpr int DT = D / 16;
-  __shared__ __attribute__((aligned(256))) u32x4 lds[kWaves * S::kRing];
+  __shared__ __attribute__((aligned(256))) u32x4 lds[kWaves * S::kWaveSlots];
   const int lane = threadIdx.x & 63, q4 = lane >> 4, l16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // Heads of a split on one XCD, where there are splits for all of them.
@@ -571,7 +646,7 @@ __global__ __launch_bounds__(kBoundThreads) void attend_split_kernel(AttendParam
   Wave<D, T, kWaves> w;
   w.load_q(p, s, h0, nh, w.qf);
   const int len = row_length(p, s);
-  w.init(p, kh, lds + wave * S::kRing);
+  w.init(p, kh, lds + wave * S::kWaveSlots);
   const int blocks_all = blocks_of(len), all = min(max(blocks_all - f0, 0), per);
   if (split > 0 && all == 0) return;
   const int each = (all + kWaves - 1) / kWaves;
@@ -613,14 +688,14 @@ __global__ __launch_bounds__(kBoundThreads) void attend_split_kernel(AttendParam
     f32x4 o{};
 #pragma unroll
     for (int n = 0; n < kWaves; ++n) {
-      ml[n] = reinterpret_cast<const f32x2*>(lds + n * S::kRing + kAttendGroup * D / 4)[g];
+      ml[n] = reinterpret_cast<const f32x2*>(lds + n * S::kWaveSlots + kAttendGroup * D / 4)[g];
       top = fmaxf(top, ml[n].x);
     }
 #pragma unroll
     for (int n = 0; n < kWaves; ++n) {
       const float f = join_weight(ml[n].x, ml[n].y, top);
       sum += f * ml[n].y;
-      o += f * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(lds + n * S::kRing) + g * D + d);
+      o += f * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(lds + n * S::kWaveSlots) + g * D + d);
     }
     if (whole) {
       write_row(p, s, h0 + g, d, o, top, sum);
@@ -739,7 +814,7 @@ constexpr int kSplitBlocks = 2;
 template <int D, CacheType T>
 hipError_t launch(const AttendParams& p, hipStream_t s) {
   const int groups = (p.G + kAttendGroup - 1) / kAttendGroup, heads = p.Hkv * groups;
-  constexpr int kFill = std::min(attend_waves(Shape<D, T>::kRow), 8);     // waves whose rings fill a CU's LDS
+  constexpr int kFill = std::min(attend_waves(T, D), 8);     // waves whose rings fill a CU's LDS
   const int64_t rows = int64_t(p.seqs) * heads;
   const int most = static_cast<int>(attend_total(1, p.max_length));       // blocks of a row
   if (p.max_length <= kShortKeys && rows <= kShortGroups)
@@ -760,6 +835,7 @@ template <int D>
 hipError_t launch(const AttendParams& p, CacheType type, hipStream_t s) {
   if (type == kCacheBf16) return launch<D, kCacheBf16>(p, s);
   if (type == kCacheE4m3) return launch<D, kCacheE4m3>(p, s);
+  if (type == kCacheE2m1) return launch<D, kCacheE2m1>(p, s);
   return launch<D, kCacheInt8>(p, s);
 }
 

@@ -1,4 +1,4 @@
-// C ABI of the cache operators (rotary positions, the 8-bit cache, attention of one
+// C ABI of the cache operators (rotary positions, the 8- and 4-bit cache, attention of one
 // new token): argument checks and launches.  Every check runs before anything is
 // enqueued.
 #include <algorithm>
@@ -24,7 +24,7 @@ int check_quant_pool(const pallas_quant_pool* p, int layer, const char* what) {
     return fail(PALLAS_ERR_INVALID_ARG, "%s: non-positive pool dimension", what);
   if (!aligned(p->codes, 16) || !aligned(p->scales, 16))
     return fail(PALLAS_ERR_INVALID_ARG, "%s: codes or scales not 16-byte aligned", what);
-  if (p->format != PALLAS_QUANT_E4M3 && p->format != PALLAS_QUANT_INT8)
+  if (p->format != PALLAS_QUANT_E4M3 && p->format != PALLAS_QUANT_INT8 && p->format != PALLAS_QUANT_E2M1)
     return fail(PALLAS_ERR_INVALID_ARG, "%s: format %d", what, p->format);
   if (layer < 0 || layer >= p->n_layers)
     return fail(PALLAS_ERR_OUT_OF_RANGE, "%s: layer %d of %d", what, layer, p->n_layers);
@@ -38,6 +38,11 @@ int check_quant_pool(const pallas_quant_pool* p, int layer, const char* what) {
 
 // Rows of one layer's K plane.
 int64_t plane_rows(const pallas_quant_pool* p) { return int64_t(p->num_pages) * p->page_size * p->n_kv_heads; }
+// Bytes of a row's codes.
+int code_bytes(const pallas_quant_pool* p) { return p->format == PALLAS_QUANT_E2M1 ? p->head_dim / 2 : p->head_dim; }
+pallas::CacheType cache_type(const pallas_quant_pool* p) {
+  return p->format == PALLAS_QUANT_E2M1 ? pallas::kCacheE2m1 : p->format == PALLAS_QUANT_INT8 ? pallas::kCacheInt8 : pallas::kCacheE4m3;
+}
 
 int quant_call(bool store, const pallas_quant_pool* pool, int32_t layer, int32_t num_tokens, const int32_t* d_seq_ids,
                const int32_t* d_positions, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
@@ -62,12 +67,12 @@ int quant_call(bool store, const pallas_quant_pool* pool, int32_t layer, int32_t
     return fail(PALLAS_ERR_UNSUPPORTED, "%s: %d tokens of %lld K and V elements (below 2^35 in all)", what, num_tokens,
                 (long long)(2 * row));
   pallas::QuantParams p{};
-  p.codes = static_cast<uint8_t*>(pool->codes) + 2 * layer * plane_rows(pool) * pool->head_dim;
+  p.codes = static_cast<uint8_t*>(pool->codes) + 2 * layer * plane_rows(pool) * code_bytes(pool);
   p.scales = pool->scales + 2 * layer * plane_rows(pool);
   p.num_pages = pool->num_pages;
   p.Hkv = pool->n_kv_heads;
   p.d = pool->head_dim;
-  p.int8 = pool->format == PALLAS_QUANT_INT8;
+  p.format = pool->format;
   p.seq = d_seq_ids;
   p.pos = d_positions;
   p.bt = d_block_tables;
@@ -101,7 +106,10 @@ AttendSpace attend_space(int64_t seqs, int Hq, int d, int max_length, int ranges
   const size_t o_at = (seqs * 8 + 255) / 256 * 256, ml_at = o_at + size_t(records) * Hq * d * 4;
   return {int(records), o_at, ml_at, (ml_at + size_t(records) * Hq * 8 + 255) / 256 * 256};
 }
-int most_ranges(int Hq, int Hkv, int d) { return pallas::attend_ranges(d, pallas::attend_heads(Hq, Hkv)); }
+int most_ranges(int Hq, int Hkv, int d) {
+  const int waves = std::max(pallas::attend_waves(pallas::kCacheE4m3, d), pallas::attend_waves(pallas::kCacheE2m1, d));
+  return pallas::attend_ranges(waves, pallas::attend_heads(Hq, Hkv));
+}
 
 int check_attend(int32_t num_seqs, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_length,
                  const char* what) {
@@ -156,7 +164,7 @@ int attend_call(const char* what, pallas::CacheType type, pallas::AttendParams& 
   p.out = static_cast<uint16_t*>(d_out);
   p.out_stride = out_stride;
   p.lse = d_lse;
-  p.ranges = pallas::attend_ranges(type == pallas::kCacheBf16 ? 2 * p.d : p.d, pallas::attend_heads(n_q_heads, p.Hkv));
+  p.ranges = pallas::attend_ranges(pallas::attend_waves(type, p.d), pallas::attend_heads(n_q_heads, p.Hkv));
   p.records = sp.records;
   char* ws = static_cast<char*>(d_workspace);
   p.parts = reinterpret_cast<int32_t*>(ws);
@@ -314,20 +322,19 @@ int pallas_attend_quant(const pallas_quant_pool* pool, int32_t layer, int32_t nu
                         const int32_t* d_block_tables, int32_t max_pages, float scale, void* d_out,
                         int64_t out_stride, float* d_lse, void* d_workspace, size_t ws_bytes, int32_t* d_err,
                         void* stream) {
-  const char* what = "attend (8-bit)";
+  const char* what = "attend (quantised)";
   if (int rc = check_quant_pool(pool, layer, what)) return rc;
   const int64_t rows = plane_rows(pool);
   if (2 * rows * 4 > int64_t(0xFFFFFF00))   // addressed with 32-bit offsets
     return fail(PALLAS_ERR_UNSUPPORTED, "%s: a layer's scales of %lld bytes exceed 4 GiB", what, (long long)(2 * rows * 4));
   pallas::AttendParams p{};
-  p.k = static_cast<const uint8_t*>(pool->codes) + 2 * layer * rows * pool->head_dim;
-  p.v = static_cast<const uint8_t*>(pool->codes) + (2 * layer + 1) * rows * pool->head_dim;
+  p.k = static_cast<const uint8_t*>(pool->codes) + 2 * layer * rows * code_bytes(pool);
+  p.v = static_cast<const uint8_t*>(pool->codes) + (2 * layer + 1) * rows * code_bytes(pool);
   p.scales = pool->scales + 2 * layer * rows;
   p.num_pages = pool->num_pages;
   p.Hkv = pool->n_kv_heads;
   p.d = pool->head_dim;
-  return attend_call(what, pool->format == PALLAS_QUANT_INT8 ? pallas::kCacheInt8 : pallas::kCacheE4m3, p,
-                     pool->page_size, num_seqs, n_q_heads, d_q, q_stride, d_lengths, max_length, d_block_tables,
+  return attend_call(what, cache_type(pool), p, pool->page_size, num_seqs, n_q_heads, d_q, q_stride, d_lengths, max_length, d_block_tables,
                      max_pages, scale, d_out, out_stride, d_lse, d_workspace, ws_bytes, d_err, stream);
 }
 

@@ -369,12 +369,12 @@ struct RopeParams {
 };
 hipError_t launch_rope(const RopeParams& p, hipStream_t s);
 
-// quant_kv.hip: rows of one layer of an 8-bit pool, written and read back.
+// quant_kv.hip: rows of one layer of an 8- or 4-bit pool, written and read back.
 struct QuantParams {
-  uint8_t* codes;          // [2][num_pages][16][Hkv][d], K and V planes of the layer
-  float* scales;           // [2][num_pages][16][Hkv]
+  uint8_t* codes;          // [2][num_pages][16][Hkv][bytes of d codes], K and V planes of the layer
+  float* scales;           // [2][num_pages][16][Hkv] (E2M1: four bytes in place of each float)
   int num_pages, Hkv, d;
-  int int8;                // else E4M3
+  int format;              // pallas_quant_format
   const int32_t* seq;      // [tokens] or null (token t: sequence t)
   const int32_t* pos;      // [tokens]
   const int32_t* bt;       // [seqs][max_pages]
@@ -390,11 +390,11 @@ hipError_t launch_quant_store(const QuantParams& p, hipStream_t s);
 hipError_t launch_quant_load(const QuantParams& p, hipStream_t s);
 
 // attend.hip: one new token per sequence over a paged cache.
-enum CacheType { kCacheBf16 = 0, kCacheE4m3 = 1, kCacheInt8 = 2 };
+enum CacheType { kCacheBf16 = 0, kCacheE4m3 = 1, kCacheInt8 = 2, kCacheE2m1 = 3 };
 struct AttendParams {
   const void* k;           // [num_pages][16][Hkv][d] of the layer
   const void* v;
-  const float* scales;     // 8-bit: [2][num_pages][16][Hkv], K and V of the layer, below 4 GiB
+  const float* scales;     // 8 and 4 bits: [2][num_pages][16][Hkv], K and V of the layer, below 4 GiB
   int num_pages, Hkv, Hq, G, d;   // G = Hq / Hkv
   int seqs, max_length, max_pages;
   const uint16_t* q;
@@ -416,12 +416,14 @@ constexpr int kAttendBlock = 32;         // keys per block
 constexpr int kAttendGroup = 16;         // query heads that share one pass over a KV head
 // Blocks of a wave's range: at most one per pair of lanes.
 constexpr int kAttendMaxBlocks = 32;
-// Waves that a CU holds, by the bytes of a head row: each has a ring of two stages of 32
-// K and V rows, 128 KiB in all.
-constexpr int attend_waves(int row_bytes) { return 1024 / row_bytes; }
+// Waves that a CU holds: each has a ring of two stages of 32 K and V rows, 128 KiB in all,
+// and with 4-bit rows room to turn V besides.
+constexpr int attend_waves(CacheType type, int d) {
+  return type == kCacheE2m1 ? 12 : 1024 / (type == kCacheBf16 ? 2 * d : d);
+}
 // Ranges that run at once: a multiple of 8 (one XCD each in turn), at least 8.
-inline int attend_ranges(int row_bytes, int64_t heads) {
-  return int(std::max<int64_t>(256 * attend_waves(row_bytes) / heads / 8 * 8, 8));
+inline int attend_ranges(int waves, int64_t heads) {
+  return int(std::max<int64_t>(256 * waves / heads / 8 * 8, 8));
 }
 // KV heads, times the passes over each.
 inline int64_t attend_heads(int Hq, int Hkv) { return int64_t(Hkv) * ((Hq / Hkv + kAttendGroup - 1) / kAttendGroup); }
