@@ -20,6 +20,8 @@
  *   pallas_rope_*              rotary positions of Q and K rows
  *   pallas_quant_store, _load  an 8- or 4-bit cache: rows quantised as they are
  *                              written, and read back
+ *   pallas_append_*            new tokens' K and V into a paged cache, rotated on
+ *                              the way
  *   pallas_attend_*            attention of one new token per sequence over a
  *                              paged cache, bf16, 8- or 4-bit
  *   pallas_check_coverage      host-only [0, n) coverage check
@@ -330,12 +332,11 @@ int pallas_decode_step_static(pallas_model* m, int32_t num_seqs, const int32_t* 
 /* ------------------------------------------------------------------------
  * Operators on the cache, for callers that run a decoder's layers themselves
  * (another architecture, a long-context rotary, an 8- or 4-bit cache).  A new token
- * of each sequence takes pallas_rope_apply on its Q and K heads, the store
- * (pallas_quant_store, or the caller's own into a bf16 pool) and
- * pallas_attend_*; a prompt's rows take the first two.  Per-row arguments
+ * of each sequence takes pallas_append_* (or pallas_rope_apply on its Q and K heads and
+ * pallas_quant_store) and pallas_attend_*; a prompt's rows take the first.  Per-row arguments
  * (positions, sequence indices, lengths) live in device memory, so a captured
  * graph can be replayed as they grow.  Their launches are timed with the
- * classes PALLAS_K_QKV_EPI (rope, store), PALLAS_K_PACK (load) and
+ * classes PALLAS_K_QKV_EPI (rope, store, append), PALLAS_K_PACK (load) and
  * PALLAS_K_DECODE_ATTN (attend).
  * ------------------------------------------------------------------------ */
 
@@ -470,6 +471,33 @@ int pallas_quant_load(const pallas_quant_pool* pool, int32_t layer, int32_t num_
                       const int32_t* d_block_tables, int32_t max_pages, int32_t* d_err,
                       void* stream);
 
+/* Appends the K and V of num_tokens (>= 0) tokens to one layer of a bf16 pool (a
+ * pallas_quant_pool: quantised as pallas_quant_store does), K and the tokens' queries
+ * rotated on the way as pallas_rope_apply does: one launch in place of its two calls and
+ * the store.  Rows and places are pallas_quant_store's; d_q and d_q_out are
+ * bf16 [num_tokens] rows of [n_q_heads][head_dim], 16-byte aligned, strides a multiple of 8
+ * (d_q_out may be d_q with the same stride; otherwise neither overlaps what the call reads
+ * or writes).  Without queries n_q_heads is 0 and both are null.
+ *   The rotation is worked out in 64 bits and rounded to float32 and then to bf16, before a
+ * code is made of it: within 2^-8 of the exact value, where pallas_rope_apply adds up to
+ * 2^-22 of the pair's magnitudes.
+ *   Of a token of negative position (padding) nothing is written, of one that is skipped as
+ * in pallas_quant_store, with PALLAS_DEVERR_PAGE, the queries alone.  rotary_dim of the plan is at
+ * most head_dim (INVALID_ARG); head_dim 64 or 128, page_size 16, num_tokens below 2^24,
+ * n_q_heads and n_kv_heads at most 4096 (UNSUPPORTED otherwise). */
+int pallas_append_kv(const pallas_rope_plan* plan, const pallas_kv_pool* pool, int32_t layer,
+                     int32_t num_tokens, const int32_t* d_seq_ids, const int32_t* d_positions,
+                     int32_t n_q_heads, const void* d_q, int64_t q_stride, void* d_q_out,
+                     int64_t q_out_stride, const void* d_k, int64_t k_stride, const void* d_v,
+                     int64_t v_stride, int32_t num_seqs, const int32_t* d_block_tables,
+                     int32_t max_pages, int32_t* d_err, void* stream);
+int pallas_append_quant(const pallas_rope_plan* plan, const pallas_quant_pool* pool, int32_t layer,
+                        int32_t num_tokens, const int32_t* d_seq_ids, const int32_t* d_positions,
+                        int32_t n_q_heads, const void* d_q, int64_t q_stride, void* d_q_out,
+                        int64_t q_out_stride, const void* d_k, int64_t k_stride, const void* d_v,
+                        int64_t v_stride, int32_t num_seqs, const int32_t* d_block_tables,
+                        int32_t max_pages, int32_t* d_err, void* stream);
+
 /* Attention of one new token per sequence over one layer of a paged cache.
  * Sequence i has d_lengths[i] keys (int32, device), positions [0, length), its
  * own included once it is stored.  Query head h reads KV head h / (n_q_heads /
@@ -601,7 +629,7 @@ typedef enum {
   PALLAS_K_RMSNORM = 1,    /* prefill only: decode folds its norms into the projections */
   PALLAS_K_ROPE_TABLE = 2, /* none: the rotary factors come with PALLAS_K_EMBED */
   PALLAS_K_GEMM_QKV = 3,   /* prefill Q|K|V projection (K|V only in the last layer) */
-  PALLAS_K_QKV_EPI = 4,    /* prefill QK-norm, rotary, paged K/V store; pallas_rope_apply, pallas_quant_store */
+  PALLAS_K_QKV_EPI = 4,    /* prefill QK-norm, rotary, paged K/V store; pallas_rope_apply, pallas_quant_store, pallas_append_* */
   PALLAS_K_ATTN = 5,       /* prefill causal attention */
   PALLAS_K_GEMM_O = 6,     /* prefill output projection + residual */
   PALLAS_K_GEMM_GATE_UP = 7, /* prefill gate|up projection + SwiGLU */

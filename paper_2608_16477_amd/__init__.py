@@ -13,7 +13,7 @@ from .binding import (  # noqa: F401
     pallas_prefill_prefix, pallas_prefill_chunk, pallas_pack_suffix_blocks, pallas_assemble_kv,
     pallas_decode_step, pallas_decode_step_static, Model, ChunkDesc, ChunkHeader, EXPORTS, KERNEL_CLASSES,
     pallas_rope_init, pallas_rope_apply, RopePlan, ROPE_LAYOUTS, ROPE_SCALINGS,
-    pallas_quant_store, pallas_quant_load,
+    pallas_quant_store, pallas_quant_load, pallas_append_kv, pallas_append_quant,
     pallas_attend_kv, pallas_attend_quant, pallas_attend_workspace_size,
     pallas_profile_enable, pallas_profile_read, pallas_profile_reset, pallas_profile_clock,
     pallas_window_select, pallas_window_evaluate, pallas_ewma_update, pallas_admit,

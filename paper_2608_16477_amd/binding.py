@@ -134,6 +134,10 @@ EXPORTS = {
                                      _i32, _vp, _vp]),
     "pallas_quant_load": (C.c_int, [C.POINTER(QuantPoolC), _i32, _i32, _vp, _vp, _vp, _i64, _vp, _i64, _i32, _vp,
                                     _i32, _vp, _vp]),
+    "pallas_append_kv": (C.c_int, [C.POINTER(RopePlan), C.POINTER(KVPoolC), _i32, _i32, _vp, _vp, _i32, _vp, _i64, _vp, _i64,
+                                   _vp, _i64, _vp, _i64, _i32, _vp, _i32, _vp, _vp]),
+    "pallas_append_quant": (C.c_int, [C.POINTER(RopePlan), C.POINTER(QuantPoolC), _i32, _i32, _vp, _vp, _i32, _vp, _i64, _vp,
+                                      _i64, _vp, _i64, _vp, _i64, _i32, _vp, _i32, _vp, _vp]),
     "pallas_attend_kv": (C.c_int, [C.POINTER(KVPoolC), _i32, _i32, _i32, _vp, _i64, _vp, _i32, _vp, _i32, C.c_float,
                                    _vp, _i64, _vp, _vp, _sz, _vp, _vp]),
     "pallas_attend_quant": (C.c_int, [C.POINTER(QuantPoolC), _i32, _i32, _i32, _vp, _i64, _vp, _i32, _vp, _i32,
@@ -449,6 +453,49 @@ def pallas_quant_load(codes, scales, layer: int, k, v, positions, block_tables, 
     """Reads rows of a layer back into ``k``, ``v`` (bf16 [tokens, Hkv, d], any token stride)."""
     _quant_call("quant load", lib().pallas_quant_load, codes, scales, layer, k, v, positions, block_tables, seq_ids, err,
                 stream)
+
+
+def _append_call(call, plan, ps, dev, layer, k, v, positions, block_tables, q, q_out, seq_ids, err, stream):
+    i32 = _torch.int32
+    T, = n = _whole(positions, "append: positions", i32, 1, dev)
+    shape = (T, ps.n_kv_heads, ps.head_dim)
+    ks, vs = _packed_rows(k, "append: k", dev, shape), _packed_rows(v, "append: v", dev, shape)
+    heads, qp, qs, op, os_ = 0, None, 0, None, 0
+    if q is not None:
+        q_shape = q.shape
+        qs = _packed_rows(q, "append: q", dev, q_shape)
+        out = q if q_out is None else q_out
+        os_ = qs if q_out is None else _packed_rows(out, "append: q_out", dev, q_shape)
+        if q_shape[0] != T or q_shape[2] != ps.head_dim:
+            _bad(f"append: {tuple(q_shape)} queries of {T} tokens, a pool of head_dim {ps.head_dim}")
+        heads, qp, op = q_shape[1], q.data_ptr(), out.data_ptr()
+    elif q_out is not None:
+        _bad("append: q_out without q")
+    seqs, pages = _whole(block_tables, "append: block tables", i32, 2, dev)
+    if seq_ids is not None and _whole(seq_ids, "append: sequence ids", i32, 1, dev) != n:
+        _bad(f"append: {seq_ids.shape[0]} sequence ids of {T} tokens")
+    if err is not None and not _whole(err, "append: err", i32, 1, dev)[0]:
+        _bad("append: an empty err")
+    if T:
+        _launch(dev, stream, call, C.byref(plan), C.byref(ps), layer, T, _ptr(seq_ids), positions.data_ptr(), heads, qp, qs,
+                op, os_, k.data_ptr(), ks, v.data_ptr(), vs, seqs, block_tables.data_ptr(), pages, _ptr(err))
+
+
+def pallas_append_kv(plan: RopePlan, pool, layer: int, k, v, positions, block_tables, q=None, q_out=None, seq_ids=None,
+                     err=None, stream=None):
+    """Rotates ``k`` and ``q`` and stores ``k``, ``v`` (bf16 [tokens, Hkv, d], any token stride) into a layer of a bf16
+    pool; ``q`` (bf16 [tokens, Hq, d]) goes to ``q_out``, or in place without it."""
+    dev = pool.get_device()
+    _whole(pool, "append: pool", (_torch or _load_torch()).bfloat16, 6, dev)
+    _append_call(lib().pallas_append_kv, plan, kv_pool_struct(pool), dev, layer, k, v, positions, block_tables, q, q_out,
+                 seq_ids, err, stream)
+
+
+def pallas_append_quant(plan: RopePlan, codes, scales, layer: int, k, v, positions, block_tables, q=None, q_out=None,
+                        seq_ids=None, err=None, stream=None):
+    """The same into an 8- or 4-bit pool (quant_pool_struct)."""
+    _append_call(lib().pallas_append_quant, plan, quant_pool_struct(codes, scales), codes.get_device(), layer, k, v,
+                 positions, block_tables, q, q_out, seq_ids, err, stream)
 
 
 def pallas_attend_workspace_size(num_seqs: int, n_q_heads: int, n_kv_heads: int, head_dim: int, max_length: int) -> int:

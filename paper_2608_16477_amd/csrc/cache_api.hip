@@ -44,24 +44,53 @@ pallas::CacheType cache_type(const pallas_quant_pool* p) {
   return p->format == PALLAS_QUANT_E2M1 ? pallas::kCacheE2m1 : p->format == PALLAS_QUANT_INT8 ? pallas::kCacheInt8 : pallas::kCacheE4m3;
 }
 
-int quant_call(bool store, const pallas_quant_pool* pool, int32_t layer, int32_t num_tokens, const int32_t* d_seq_ids,
+// The rows of a call that writes or reads tokens of a cache, of n_kv_heads and head_dim.
+int check_rows(const char* what, int n_kv_heads, int head_dim, int32_t num_tokens, const int32_t* d_seq_ids,
                const int32_t* d_positions, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
-               int32_t num_seqs, const int32_t* d_block_tables, int32_t max_pages, int32_t* d_err, void* stream) {
-  const char* what = store ? "quant store" : "quant load";
-  if (int rc = check_quant_pool(pool, layer, what)) return rc;
+               int32_t num_seqs, const int32_t* d_block_tables, int32_t max_pages, const int32_t* d_err) {
   if (num_tokens < 0 || num_seqs <= 0 || max_pages <= 0)
     return fail(PALLAS_ERR_INVALID_ARG, "%s: negative num_tokens, or num_seqs or max_pages below 1", what);
   if (!d_positions || !k || !v || !d_block_tables)
     return fail(PALLAS_ERR_INVALID_ARG, "%s: null positions, rows or tables", what);
   if (!d_seq_ids && num_tokens > num_seqs)
     return fail(PALLAS_ERR_INVALID_ARG, "%s: %d tokens without sequence ids, of %d sequences", what, num_tokens, num_seqs);
-  const int64_t row = int64_t(pool->n_kv_heads) * pool->head_dim;
+  const int64_t row = int64_t(n_kv_heads) * head_dim;
   if (!aligned(k, 16) || !aligned(v, 16) || k_stride % 8 != 0 || v_stride % 8 != 0)
     return fail(PALLAS_ERR_INVALID_ARG, "%s: rows not 16-byte aligned", what);
   if (k_stride < row || v_stride < row)
     return fail(PALLAS_ERR_INVALID_ARG, "%s: row stride below the %lld elements of a row", what, (long long)row);
   if (!aligned(d_seq_ids, 4) || !aligned(d_positions, 4) || !aligned(d_block_tables, 4) || !aligned(d_err, 4))
     return fail(PALLAS_ERR_INVALID_ARG, "%s: sequence ids, positions, tables or d_err not 4-byte aligned", what);
+  return PALLAS_OK;
+}
+
+int check_kv_pool(const pallas_kv_pool* pool, int layer, const char* what) {
+  if (int rc = pallas::check_pool(pool, what)) return rc;
+  if (layer < 0 || layer >= pool->n_layers)
+    return fail(PALLAS_ERR_OUT_OF_RANGE, "%s: layer %d of %d", what, layer, pool->n_layers);
+  if (pool->page_size != 16)
+    return fail(PALLAS_ERR_UNSUPPORTED, "%s: page_size %d (supported: 16)", what, pool->page_size);
+  return PALLAS_OK;
+}
+
+int check_plan(const pallas_rope_plan* plan) {
+  if (!plan) return fail(PALLAS_ERR_INVALID_ARG, "rope: null plan");
+  const int r = plan->rotary_dim;
+  if (r < 2 || r > PALLAS_ROPE_MAX_DIM || r % 2 != 0 ||
+      (plan->layout != PALLAS_ROPE_HALF && plan->layout != PALLAS_ROPE_INTERLEAVED) || !(plan->magnitude > 0.f))
+    return fail(PALLAS_ERR_INVALID_ARG, "rope: not a plan that pallas_rope_init filled");
+  return PALLAS_OK;
+}
+
+int quant_call(bool store, const pallas_quant_pool* pool, int32_t layer, int32_t num_tokens, const int32_t* d_seq_ids,
+               const int32_t* d_positions, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+               int32_t num_seqs, const int32_t* d_block_tables, int32_t max_pages, int32_t* d_err, void* stream) {
+  const char* what = store ? "quant store" : "quant load";
+  if (int rc = check_quant_pool(pool, layer, what)) return rc;
+  if (int rc = check_rows(what, pool->n_kv_heads, pool->head_dim, num_tokens, d_seq_ids, d_positions, k, k_stride, v,
+                          v_stride, num_seqs, d_block_tables, max_pages, d_err))
+    return rc;
+  const int64_t row = int64_t(pool->n_kv_heads) * pool->head_dim;
   // A launch has fewer than 2^32 threads, 16 elements each.
   if (int64_t(num_tokens) * 2 * row >= (int64_t(1) << 35))
     return fail(PALLAS_ERR_UNSUPPORTED, "%s: %d tokens of %lld K and V elements (below 2^35 in all)", what, num_tokens,
@@ -93,6 +122,58 @@ int quant_call(bool store, const pallas_quant_pool* pool, int32_t layer, int32_t
   p.v_out = static_cast<uint16_t*>(const_cast<void*>(v));
   pallas::ProfScope ps(PALLAS_K_PACK, s);
   return launched(pallas::launch_quant_load(p, s), "quant load launch");
+}
+
+// Appending to either kind of cache; the caller has checked the pool and set what p says of it.
+int append_call(const char* what, const pallas_rope_plan* plan, pallas::AppendParams& p, int32_t num_tokens,
+                const int32_t* d_seq_ids, const int32_t* d_positions, int32_t n_q_heads, const void* d_q,
+                int64_t q_stride, void* d_q_out, int64_t q_out_stride, const void* d_k, int64_t k_stride,
+                const void* d_v, int64_t v_stride, int32_t num_seqs, const int32_t* d_block_tables, int32_t max_pages,
+                int32_t* d_err, void* stream) {
+  if (int rc = check_plan(plan)) return rc;
+  if (p.d != 64 && p.d != 128) return fail(PALLAS_ERR_UNSUPPORTED, "%s: head_dim %d (supported: 64, 128)", what, p.d);
+  if (plan->rotary_dim > p.d)
+    return fail(PALLAS_ERR_INVALID_ARG, "%s: rotary_dim %d of heads of %d", what, plan->rotary_dim, p.d);
+  if (int rc = check_rows(what, p.Hkv, p.d, num_tokens, d_seq_ids, d_positions, d_k, k_stride, d_v, v_stride, num_seqs,
+                          d_block_tables, max_pages, d_err))
+    return rc;
+  if (n_q_heads < 0 || (n_q_heads > 0) != (d_q != nullptr) || (n_q_heads > 0) != (d_q_out != nullptr))
+    return fail(PALLAS_ERR_INVALID_ARG, "%s: %d query heads with %s", what, n_q_heads, d_q && d_q_out ? "rows" : "null rows");
+  if (n_q_heads > 0) {
+    const int64_t row = int64_t(n_q_heads) * p.d;
+    if (!aligned(d_q, 16) || !aligned(d_q_out, 16) || q_stride % 8 != 0 || q_out_stride % 8 != 0)
+      return fail(PALLAS_ERR_INVALID_ARG, "%s: query rows not 16-byte aligned", what);
+    if (q_stride < row || q_out_stride < row)
+      return fail(PALLAS_ERR_INVALID_ARG, "%s: query row stride below the %lld elements of a row", what, (long long)row);
+    if (d_q == d_q_out && num_tokens > 1 && q_stride != q_out_stride)
+      return fail(PALLAS_ERR_INVALID_ARG, "%s: queries in place with another stride", what);
+  }
+  if (num_tokens >= (1 << 24) || n_q_heads > 4096 || p.Hkv > 4096)   // (a launch has fewer than 2^32 threads)
+    return fail(PALLAS_ERR_UNSUPPORTED, "%s: %d tokens (below 2^24), %d query and %d KV heads (at most 4096)", what,
+                num_tokens, n_q_heads, p.Hkv);
+  p.q = static_cast<const uint16_t*>(d_q);
+  p.q_out = static_cast<uint16_t*>(d_q_out);
+  p.k = static_cast<const uint16_t*>(d_k);
+  p.v = static_cast<const uint16_t*>(d_v);
+  p.q_stride = q_stride;
+  p.q_out_stride = q_out_stride;
+  p.k_stride = k_stride;
+  p.v_stride = v_stride;
+  p.Hq = n_q_heads;
+  p.seq = d_seq_ids;
+  p.pos = d_positions;
+  p.bt = d_block_tables;
+  p.tokens = num_tokens;
+  p.seqs = num_seqs;
+  p.max_pages = max_pages;
+  p.err = d_err;
+  p.r = plan->rotary_dim;
+  p.interleaved = plan->layout == PALLAS_ROPE_INTERLEAVED;
+  p.magnitude = plan->magnitude;
+  std::copy(plan->turns, plan->turns + p.r / 2, p.turns);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  pallas::ProfScope ps(PALLAS_K_QKV_EPI, s);
+  return launched(pallas::launch_append(p, s), "append launch");
 }
 
 // A call's workspace: two ints per sequence, then records of d + 2 floats per query head.
@@ -234,11 +315,8 @@ int pallas_rope_init(const pallas_rope_config* cfg, pallas_rope_plan* plan) {
 int pallas_rope_apply(const pallas_rope_plan* plan, int32_t inverse, int32_t num_tokens, int32_t n_heads,
                       int32_t head_dim, const int32_t* d_positions, const void* d_x, int64_t x_token_stride,
                       int64_t x_head_stride, void* d_y, int64_t y_token_stride, int64_t y_head_stride, void* stream) {
-  if (!plan) return fail(PALLAS_ERR_INVALID_ARG, "rope: null plan");
+  if (int rc = check_plan(plan)) return rc;
   const int r = plan->rotary_dim;
-  if (r < 2 || r > PALLAS_ROPE_MAX_DIM || r % 2 != 0 ||
-      (plan->layout != PALLAS_ROPE_HALF && plan->layout != PALLAS_ROPE_INTERLEAVED) || !(plan->magnitude > 0.f))
-    return fail(PALLAS_ERR_INVALID_ARG, "rope: not a plan that pallas_rope_init filled");
   if (num_tokens < 0 || n_heads < 1 || head_dim < r)
     return fail(PALLAS_ERR_INVALID_ARG, "rope: %d tokens of %d heads of %d (rotary_dim %d)", num_tokens, n_heads, head_dim, r);
   if (!d_positions || !d_x || !d_y) return fail(PALLAS_ERR_INVALID_ARG, "rope: null positions or rows");
@@ -295,16 +373,45 @@ int pallas_quant_load(const pallas_quant_pool* pool, int32_t layer, int32_t num_
                     d_block_tables, max_pages, d_err, stream);
 }
 
+int pallas_append_kv(const pallas_rope_plan* plan, const pallas_kv_pool* pool, int32_t layer, int32_t num_tokens,
+                     const int32_t* d_seq_ids, const int32_t* d_positions, int32_t n_q_heads, const void* d_q,
+                     int64_t q_stride, void* d_q_out, int64_t q_out_stride, const void* d_k, int64_t k_stride,
+                     const void* d_v, int64_t v_stride, int32_t num_seqs, const int32_t* d_block_tables,
+                     int32_t max_pages, int32_t* d_err, void* stream) {
+  if (int rc = check_kv_pool(pool, layer, "append")) return rc;
+  pallas::AppendParams p{};
+  const int64_t plane = int64_t(pool->num_pages) * pool->page_size * pool->n_kv_heads * pool->head_dim;
+  p.cache = static_cast<uint16_t*>(pool->base) + 2 * layer * plane;
+  p.num_pages = pool->num_pages;
+  p.Hkv = pool->n_kv_heads;
+  p.d = pool->head_dim;
+  return append_call("append", plan, p, num_tokens, d_seq_ids, d_positions, n_q_heads, d_q, q_stride, d_q_out,
+                     q_out_stride, d_k, k_stride, d_v, v_stride, num_seqs, d_block_tables, max_pages, d_err, stream);
+}
+
+int pallas_append_quant(const pallas_rope_plan* plan, const pallas_quant_pool* pool, int32_t layer, int32_t num_tokens,
+                        const int32_t* d_seq_ids, const int32_t* d_positions, int32_t n_q_heads, const void* d_q,
+                        int64_t q_stride, void* d_q_out, int64_t q_out_stride, const void* d_k, int64_t k_stride,
+                        const void* d_v, int64_t v_stride, int32_t num_seqs, const int32_t* d_block_tables,
+                        int32_t max_pages, int32_t* d_err, void* stream) {
+  if (int rc = check_quant_pool(pool, layer, "append (quantised)")) return rc;
+  pallas::AppendParams p{};
+  p.cache = static_cast<uint8_t*>(pool->codes) + 2 * layer * plane_rows(pool) * code_bytes(pool);
+  p.scales = pool->scales + 2 * layer * plane_rows(pool);
+  p.format = pool->format;
+  p.num_pages = pool->num_pages;
+  p.Hkv = pool->n_kv_heads;
+  p.d = pool->head_dim;
+  return append_call("append (quantised)", plan, p, num_tokens, d_seq_ids, d_positions, n_q_heads, d_q, q_stride, d_q_out,
+                     q_out_stride, d_k, k_stride, d_v, v_stride, num_seqs, d_block_tables, max_pages, d_err, stream);
+}
+
 int pallas_attend_kv(const pallas_kv_pool* pool, int32_t layer, int32_t num_seqs, int32_t n_q_heads, const void* d_q,
                      int64_t q_stride, const int32_t* d_lengths, int32_t max_length, const int32_t* d_block_tables,
                      int32_t max_pages, float scale, void* d_out, int64_t out_stride, float* d_lse, void* d_workspace,
                      size_t ws_bytes, int32_t* d_err, void* stream) {
   const char* what = "attend";
-  if (int rc = pallas::check_pool(pool, what)) return rc;
-  if (layer < 0 || layer >= pool->n_layers)
-    return fail(PALLAS_ERR_OUT_OF_RANGE, "%s: layer %d of %d", what, layer, pool->n_layers);
-  if (pool->page_size != 16)
-    return fail(PALLAS_ERR_UNSUPPORTED, "%s: page_size %d (supported: 16)", what, pool->page_size);
+  if (int rc = check_kv_pool(pool, layer, what)) return rc;
   const int64_t plane = int64_t(pool->num_pages) * pool->page_size * pool->n_kv_heads * pool->head_dim;
   pallas::AttendParams p{};
   p.k = static_cast<const uint16_t*>(pool->base) + 2 * layer * plane;

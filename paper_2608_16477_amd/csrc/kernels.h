@@ -389,6 +389,28 @@ struct QuantParams {
 hipError_t launch_quant_store(const QuantParams& p, hipStream_t s);
 hipError_t launch_quant_load(const QuantParams& p, hipStream_t s);
 
+// append.hip: rows of new tokens into a layer of a paged cache, Q and K rotated.
+struct AppendParams {
+  const uint16_t* q;       // [tokens] rows of [Hq][d]
+  uint16_t* q_out;
+  const uint16_t* k;       // [tokens] rows of [Hkv][d]
+  const uint16_t* v;
+  int64_t q_stride, q_out_stride, k_stride, v_stride;
+  void* cache;             // [2][num_pages][16][Hkv][d] bf16, or codes
+  float* scales;           // as QuantParams'
+  int format;              // 0: bf16, else pallas_quant_format
+  int num_pages, Hq, Hkv, d;
+  const int32_t* seq;      // as QuantParams'
+  const int32_t* pos;
+  const int32_t* bt;
+  int tokens, seqs, max_pages;
+  int32_t* err;
+  int r, interleaved;
+  float magnitude;
+  uint64_t turns[64];      // of pairs i < r / 2, units of 2^-64 turn
+};
+hipError_t launch_append(const AppendParams& p, hipStream_t s);
+
 // attend.hip: one new token per sequence over a paged cache.
 enum CacheType { kCacheBf16 = 0, kCacheE4m3 = 1, kCacheInt8 = 2, kCacheE2m1 = 3 };
 struct AttendParams {
