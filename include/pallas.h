@@ -24,6 +24,9 @@
  *                              the way
  *   pallas_attend_*            attention of one new token per sequence over a
  *                              paged cache, bf16, 8- or 4-bit
+ *   pallas_bounds_*, pallas_select_blocks, pallas_attend_blocks_*
+ *                              the same over the blocks of a long context that a
+ *                              score of the query selects
  *   pallas_check_coverage      host-only [0, n) coverage check
  *   pallas_window_*, pallas_ewma_update, pallas_admit, pallas_waste_bound
  *                              host-only Scheduler Engine (when to migrate)
@@ -542,6 +545,93 @@ int pallas_attend_quant(const pallas_quant_pool* pool, int32_t layer, int32_t nu
 size_t pallas_attend_workspace_size(int32_t num_seqs, int32_t n_q_heads, int32_t n_kv_heads,
                                     int32_t head_dim, int32_t max_length);
 
+/* Attention over selected blocks.  A block is 16 positions, one entry of a block table.
+ * A long context's new token attends to a budget of its blocks: pallas_bounds_* keeps
+ * bounds of each block's keys up to date as they are written, pallas_select_blocks scores
+ * the blocks of a sequence against its queries and lists the best for each KV head,
+ * pallas_attend_blocks_* attends to the blocks listed.
+ *
+ * Bounds of a cache's keys, by page, KV head and layer: the elementwise largest and smallest key,
+ * as whole numbers that stand for code * scale:
+ *   codes  [n_layers][num_pages][n_kv_heads][2 (largest, smallest)][head_dim] int8
+ *   scales [n_layers][num_pages][n_kv_heads] float32
+ * (device, 16-byte aligned): with a = the largest magnitude among both, scale = a / 127, code = x *
+ * (127 / a) rounded to nearest even (float32 arithmetic); a < 2^-100 counts as zero (scale 0); a
+ * block with an infinity or a NaN has scale NaN and codes 0. */
+typedef struct {
+  void* codes;
+  float* scales;
+  int32_t num_pages;
+  int32_t n_layers;
+  int32_t n_kv_heads;
+  int32_t head_dim;   /* 64 or 128 */
+} pallas_bounds_pool;
+
+/* Bounds, from the cache, of the blocks that hold positions [d_start[i], d_lengths[i]) of
+ * sequence i (int32, device, [num_seqs]): each over its keys below the length, also those that
+ * it had before.  `bounds` has the pool's pages, layers, heads and head_dim.  After a new token
+ * start is its position; after an assembly or a prefill, where it began.  A negative start is
+ * padding: nothing of the sequence is written; as where start >= length.  max_new (>= 1) is the most
+ * positions of a sequence; where there are more the call raises
+ * PALLAS_DEVERR_LENGTH, and the blocks behind floor((max_new + 30) / 16) are left as they were.
+ * Blocks beyond the table or on pages outside [0, num_pages) are skipped and raise
+ * PALLAS_DEVERR_PAGE, in *d_err (nullable).  num_seqs up to 65535, page_size 16 (UNSUPPORTED
+ * otherwise). */
+int pallas_bounds_kv(const pallas_kv_pool* pool, const pallas_bounds_pool* bounds, int32_t layer,
+                     int32_t num_seqs, const int32_t* d_start, const int32_t* d_lengths,
+                     int32_t max_new, const int32_t* d_block_tables, int32_t max_pages,
+                     int32_t* d_err, void* stream);
+int pallas_bounds_quant(const pallas_quant_pool* pool, const pallas_bounds_pool* bounds, int32_t layer,
+                        int32_t num_seqs, const int32_t* d_start, const int32_t* d_lengths,
+                        int32_t max_new, const int32_t* d_block_tables, int32_t max_pages,
+                        int32_t* d_err, void* stream);
+
+/* Lists max_blocks blocks of each sequence for each KV head: d_blocks, int32
+ * [num_seqs][n_kv_heads][max_blocks], ascending, -1 behind the last; all blocks where a
+ * sequence has no more.  Those are its `first` first and `last` last blocks (first + last <=
+ * max_blocks), then the ones that score highest, of equal ones the earliest.
+ *   Query head h of the KV head is rounded to whole numbers c with a step t, as bounds are
+ * (alone: a is its largest magnitude); with a block's codes M (largest) and m (smallest) and
+ * scale u
+ *   score_h = (float32(sum_i max(c_i, 0) M_i + min(c_i, 0) m_i) * u) * t
+ * which is at least q . k of each key of the block, but for the rounding to whole numbers; the
+ * block's score is the largest over the query heads of the KV head (NaN counts as larger than
+ * any number).  The sum is of whole numbers and the products are float32, so the lists are
+ * the same however the work is divided, and in any other program that follows this.
+ *   Query rows, lengths, max_length, tables and their limits and errors are pallas_attend_*'s; a
+ * block on a page outside [0, num_pages) scores lowest.  The workspace (device, 256-byte aligned,
+ * pallas_select_workspace_size bytes) holds nothing between calls; calls that may run at once need
+ * one each. */
+int pallas_select_blocks(const pallas_bounds_pool* bounds, int32_t layer, int32_t num_seqs,
+                         int32_t n_q_heads, const void* d_q, int64_t q_stride,
+                         const int32_t* d_lengths, int32_t max_length,
+                         const int32_t* d_block_tables, int32_t max_pages, int32_t max_blocks,
+                         int32_t first, int32_t last, int32_t* d_blocks, void* d_workspace,
+                         size_t ws_bytes, int32_t* d_err, void* stream);
+size_t pallas_select_workspace_size(int32_t num_seqs, int32_t n_kv_heads, int32_t max_length);
+
+/* pallas_attend_* over the keys of listed blocks alone: those below the length of each block
+ * that d_blocks (int32, device, [num_seqs][n_kv_heads][max_blocks], max_blocks >= 1) names
+ * for the KV head.  Of a list the first min(max_blocks, blocks of the length) entries are read;
+ * one that names no block of the length (a negative one, say) adds nothing, a block that is
+ * named twice counts twice, the order changes last bits alone.  The lse is that of the keys
+ * attended to.  The workspace is that of pallas_attend_* with max_length min(max_length, 16
+ * max_blocks). */
+int pallas_attend_blocks_kv(const pallas_kv_pool* pool, int32_t layer, int32_t num_seqs,
+                            int32_t n_q_heads, const void* d_q, int64_t q_stride,
+                            const int32_t* d_lengths, int32_t max_length,
+                            const int32_t* d_block_tables, int32_t max_pages,
+                            const int32_t* d_blocks, int32_t max_blocks, float scale, void* d_out,
+                            int64_t out_stride, float* d_lse, void* d_workspace, size_t ws_bytes,
+                            int32_t* d_err, void* stream);
+int pallas_attend_blocks_quant(const pallas_quant_pool* pool, int32_t layer, int32_t num_seqs,
+                               int32_t n_q_heads, const void* d_q, int64_t q_stride,
+                               const int32_t* d_lengths, int32_t max_length,
+                               const int32_t* d_block_tables, int32_t max_pages,
+                               const int32_t* d_blocks, int32_t max_blocks, float scale, void* d_out,
+                               int64_t out_stride, float* d_lse, void* d_workspace, size_t ws_bytes,
+                               int32_t* d_err, void* stream);
+
 /* Coverage check (Section 4.3, "State consistency"), host only: returns
  * PALLAS_OK iff [0, prefix_len) and the ranges [h_starts[j], h_starts[j] +
  * h_lens[j]) together cover [0, n) exactly once (empty ranges are ignored),
@@ -629,7 +719,7 @@ typedef enum {
   PALLAS_K_RMSNORM = 1,    /* prefill only: decode folds its norms into the projections */
   PALLAS_K_ROPE_TABLE = 2, /* none: the rotary factors come with PALLAS_K_EMBED */
   PALLAS_K_GEMM_QKV = 3,   /* prefill Q|K|V projection (K|V only in the last layer) */
-  PALLAS_K_QKV_EPI = 4,    /* prefill QK-norm, rotary, paged K/V store; pallas_rope_apply, pallas_quant_store, pallas_append_* */
+  PALLAS_K_QKV_EPI = 4,    /* prefill QK-norm, rotary, paged K/V store; pallas_rope_apply, pallas_quant_store, pallas_append_*, pallas_bounds_* */
   PALLAS_K_ATTN = 5,       /* prefill causal attention */
   PALLAS_K_GEMM_O = 6,     /* prefill output projection + residual */
   PALLAS_K_GEMM_GATE_UP = 7, /* prefill gate|up projection + SwiGLU */
@@ -637,7 +727,7 @@ typedef enum {
   PALLAS_K_PACK = 9,       /* and pallas_quant_load */
   PALLAS_K_ASSEMBLE = 10,
   PALLAS_K_DECODE_PROJ = 11, /* decode projections and lm_head */
-  PALLAS_K_DECODE_ATTN = 12, /* with QK-norm, rotary and the K/V store; pallas_attend_* */
+  PALLAS_K_DECODE_ATTN = 12, /* with QK-norm, rotary and the K/V store; pallas_attend_*, pallas_select_blocks */
   PALLAS_K_COUNT = 13
 } pallas_kernel_class;
 

@@ -1,5 +1,6 @@
 """Operators on the cache, in float64: rotary positions (layouts, partial heads,
-long-context scaling), the 8- and 4-bit row formats, attention of one new token.
+long-context scaling), the 8- and 4-bit row formats, attention of one new token, the
+selection of blocks.
 
 Written from the formulas that ``include/pallas.h`` states.
 """
@@ -152,3 +153,58 @@ def attend(q, k, v, scale):
         out[h], mag[h] = p @ v[:, kh], p @ np.abs(v[:, kh])
         terms[h] = abs(scale) * (np.abs(k[:, kh]) @ np.abs(q[h])).max()
     return out, lse, mag, terms
+
+
+# ------------------------------------------------------------------ blocks
+def steps(x):
+    """(whole numbers of at most 127, float32 step) of the rows of x, which float32 holds; the products are float32
+    ones, as stated."""
+    x = np.asarray(x, dtype=np.float64)
+    bad = ~np.isfinite(x).all(axis=-1)
+    x = np.where(bad[..., None], 0.0, x)
+    a = np.abs(x).max(axis=-1).astype(np.float32)
+    live = a >= np.float32(2.0 ** -100)
+    a = np.where(live, a, np.float32(1))
+    with np.errstate(under="ignore"):
+        y = x.astype(np.float32) * (np.float32(127) / a)[..., None]
+    codes = np.where(live[..., None], np.clip(np.rint(y), -127, 127), 0).astype(np.int64)
+    return codes, np.where(bad, np.float32(np.nan), np.where(live, a / np.float32(127), np.float32(0)))
+
+
+def block_bounds(k):
+    """(codes [blocks, Hkv, 2, d], steps [blocks, Hkv]) of keys k [n, Hkv, d] by blocks of 16."""
+    n, hkv, d = k.shape
+    both = np.zeros((-(-n // 16), hkv, 2, d))
+    for j in range(len(both)):
+        part = k[16 * j:16 * j + 16]
+        both[j, :, 0], both[j, :, 1] = part.max(axis=0), part.min(axis=0)      # (NaN stays)
+    codes, step = steps(both.reshape(len(both), hkv, 2 * d))
+    return codes.reshape(both.shape), step
+
+
+def block_scores(q, codes, step):
+    """float32 [Hkv, blocks]: q [Hq, d] against bounds."""
+    blocks, hkv = step.shape
+    c, t = steps(q)
+    group = len(q) // hkv
+    out = np.empty((hkv, blocks), dtype=np.float32)
+    for h in range(hkv):
+        per = []
+        for g in range(h * group, (h + 1) * group):
+            dot = np.where(c[g] > 0, c[g] * codes[:, h, 0], c[g] * codes[:, h, 1]).sum(axis=-1)
+            per.append(dot.astype(np.float32) * step[:, h] * t[g])
+        out[h] = np.max(per, axis=0)                                            # (NaN stays)
+    return out
+
+
+def select_blocks(scores, budget, first, last):
+    """Ascending lists [Hkv][<= budget] of the blocks: `first` first and `last` last ones, then the highest scores (NaN
+    above all), of equal ones the earliest."""
+    lists = []
+    for row in scores:
+        n = len(row)
+        always = [j for j in range(n) if j < first or j >= n - last]
+        key = np.where(np.isnan(row), np.inf, row)
+        rest = sorted((j for j in range(n) if j not in set(always)), key=lambda j: (not np.isnan(row[j]), -key[j], j))
+        lists.append(sorted((always + rest)[:budget]) if n > budget else list(range(n)))
+    return lists

@@ -15,6 +15,8 @@ from .binding import (  # noqa: F401
     pallas_rope_init, pallas_rope_apply, RopePlan, ROPE_LAYOUTS, ROPE_SCALINGS,
     pallas_quant_store, pallas_quant_load, pallas_append_kv, pallas_append_quant,
     pallas_attend_kv, pallas_attend_quant, pallas_attend_workspace_size,
+    pallas_bounds_kv, pallas_bounds_quant, pallas_select_blocks, pallas_select_workspace_size,
+    pallas_attend_blocks_kv, pallas_attend_blocks_quant,
     pallas_profile_enable, pallas_profile_read, pallas_profile_reset, pallas_profile_clock,
     pallas_window_select, pallas_window_evaluate, pallas_ewma_update, pallas_admit,
     pallas_waste_bound, WindowParams, WindowDecision, Ewma,

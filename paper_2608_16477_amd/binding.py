@@ -104,6 +104,11 @@ class QuantPoolC(C.Structure):
                 ("n_layers", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("format", C.c_int32)]
 
 
+class BoundsPoolC(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("num_pages", C.c_int32), ("n_layers", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
 _vp, _i32, _u64, _sz = C.c_void_p, C.c_int32, C.c_uint64, C.c_size_t
 _i64 = C.c_int64
 _pi32 = C.POINTER(C.c_int32)
@@ -143,6 +148,17 @@ EXPORTS = {
     "pallas_attend_quant": (C.c_int, [C.POINTER(QuantPoolC), _i32, _i32, _i32, _vp, _i64, _vp, _i32, _vp, _i32,
                                       C.c_float, _vp, _i64, _vp, _vp, _sz, _vp, _vp]),
     "pallas_attend_workspace_size": (_sz, [_i32, _i32, _i32, _i32, _i32]),
+    "pallas_bounds_kv": (C.c_int, [C.POINTER(KVPoolC), C.POINTER(BoundsPoolC), _i32, _i32, _vp, _vp, _i32, _vp, _i32, _vp,
+                                   _vp]),
+    "pallas_bounds_quant": (C.c_int, [C.POINTER(QuantPoolC), C.POINTER(BoundsPoolC), _i32, _i32, _vp, _vp, _i32, _vp, _i32,
+                                      _vp, _vp]),
+    "pallas_select_blocks": (C.c_int, [C.POINTER(BoundsPoolC), _i32, _i32, _i32, _vp, _i64, _vp, _i32, _vp, _i32, _i32, _i32,
+                                       _i32, _vp, _vp, _sz, _vp, _vp]),
+    "pallas_select_workspace_size": (_sz, [_i32, _i32, _i32]),
+    "pallas_attend_blocks_kv": (C.c_int, [C.POINTER(KVPoolC), _i32, _i32, _i32, _vp, _i64, _vp, _i32, _vp, _i32, _vp, _i32,
+                                          C.c_float, _vp, _i64, _vp, _vp, _sz, _vp, _vp]),
+    "pallas_attend_blocks_quant": (C.c_int, [C.POINTER(QuantPoolC), _i32, _i32, _i32, _vp, _i64, _vp, _i32, _vp, _i32, _vp,
+                                             _i32, C.c_float, _vp, _i64, _vp, _vp, _sz, _vp, _vp]),
     "pallas_check_coverage": (C.c_int, [_i32, _pi32, _pi32, _i32, _i32]),
     "pallas_window_evaluate": (C.c_int, [C.POINTER(WindowParams), C.c_double, C.c_double, C.c_double,
                                          C.POINTER(WindowDecision)]),
@@ -502,7 +518,8 @@ def pallas_attend_workspace_size(num_seqs: int, n_q_heads: int, n_kv_heads: int,
     return int(lib().pallas_attend_workspace_size(num_seqs, n_q_heads, n_kv_heads, head_dim, max_length))
 
 
-def _attend_call(call, ps, dev, layer, q, lengths, max_length, block_tables, scale, out, workspace, lse, err, stream):
+def _attend_call(call, ps, dev, layer, q, lengths, max_length, block_tables, scale, out, workspace, lse, err, stream,
+                 blocks=None):
     i32, shape = _torch.int32, q.shape
     qs, os_ = _packed_rows(q, "attend: q", dev, shape), _packed_rows(out, "attend: out", dev, shape)
     S, H, d = shape
@@ -515,10 +532,16 @@ def _attend_call(call, ps, dev, layer, q, lengths, max_length, block_tables, sca
         _bad("attend: an empty err")
     if workspace.get_device() != dev or not workspace.is_contiguous():
         _bad("attend: workspace on another device, or not contiguous")
+    lists = ()
+    if blocks is not None:
+        got = _whole(blocks, "attend: blocks", i32, 3, dev)
+        if got[:2] != (S, ps.n_kv_heads):
+            _bad(f"attend: blocks {tuple(got)} of {S} sequences and {ps.n_kv_heads} KV heads")
+        lists = (blocks.data_ptr(), got[2])
     if S:
         _launch(dev, stream, call, C.byref(ps), layer, S, H, q.data_ptr(), qs, lengths.data_ptr(), max_length,
-                block_tables.data_ptr(), pages, scale, out.data_ptr(), os_, _ptr(lse), workspace.data_ptr(), workspace.nbytes,
-                _ptr(err))
+                block_tables.data_ptr(), pages, *lists, scale, out.data_ptr(), os_, _ptr(lse), workspace.data_ptr(),
+                workspace.nbytes, _ptr(err))
 
 
 def pallas_attend_kv(pool, layer: int, q, lengths, max_length: int, block_tables, scale: float, out, workspace, lse=None,
@@ -536,6 +559,95 @@ def pallas_attend_quant(codes, scales, layer: int, q, lengths, max_length: int, 
     """The same over an 8- or 4-bit pool (quant_pool_struct)."""
     _attend_call(lib().pallas_attend_quant, quant_pool_struct(codes, scales), codes.get_device(), layer, q, lengths,
                  max_length, block_tables, scale, out, workspace, lse, err, stream)
+
+
+def pallas_attend_blocks_kv(pool, layer: int, q, lengths, max_length: int, block_tables, blocks, scale: float, out,
+                            workspace, lse=None, err=None, stream=None):
+    """pallas_attend_kv over the blocks that ``blocks`` (int32 [num_seqs, Hkv, max_blocks]) lists for each KV head."""
+    dev = pool.get_device()
+    _whole(pool, "attend: pool", (_torch or _load_torch()).bfloat16, 6, dev)
+    if blocks is None:
+        _bad("attend: no blocks")
+    _attend_call(lib().pallas_attend_blocks_kv, kv_pool_struct(pool), dev, layer, q, lengths, max_length, block_tables,
+                 scale, out, workspace, lse, err, stream, blocks)
+
+
+def pallas_attend_blocks_quant(codes, scales, layer: int, q, lengths, max_length: int, block_tables, blocks, scale: float,
+                               out, workspace, lse=None, err=None, stream=None):
+    """The same over an 8- or 4-bit pool (quant_pool_struct)."""
+    if blocks is None:
+        _bad("attend: no blocks")
+    _attend_call(lib().pallas_attend_blocks_quant, quant_pool_struct(codes, scales), codes.get_device(), layer, q, lengths,
+                 max_length, block_tables, scale, out, workspace, lse, err, stream, blocks)
+
+
+def bounds_pool_struct(bounds, bound_scales) -> BoundsPoolC:
+    """``bounds``: int8 [L, P, Hkv, 2 (largest, smallest), d]; ``bound_scales``: float32 [L, P, Hkv]."""
+    torch = _torch or _load_torch()
+    dev = bounds.get_device()
+    L, P, hkv, two, d = shape = _whole(bounds, "bounds", torch.int8, 5, dev)
+    if two != 2 or _whole(bound_scales, "bounds: scales", torch.float32, 3, dev) != shape[:3]:
+        _bad(f"bounds: {tuple(shape)}, scales {tuple(bound_scales.shape)}")
+    return BoundsPoolC(bounds.data_ptr(), bound_scales.data_ptr(), P, L, hkv, d)
+
+
+def _bounds_call(call, ps, dev, layer, bounds, bound_scales, start, lengths, max_new, block_tables, err, stream):
+    i32 = _torch.int32
+    bs = bounds_pool_struct(bounds, bound_scales)
+    if bounds.get_device() != dev:
+        _bad("bounds: on another device than the cache")
+    seqs, pages = _whole(block_tables, "bounds: block tables", i32, 2, dev)
+    if _whole(start, "bounds: start", i32, 1, dev)[0] != seqs or _whole(lengths, "bounds: lengths", i32, 1, dev)[0] != seqs:
+        _bad(f"bounds: {start.shape[0]} starts, {lengths.shape[0]} lengths, {seqs} tables")
+    if err is not None and not _whole(err, "bounds: err", i32, 1, dev)[0]:
+        _bad("bounds: an empty err")
+    if seqs:
+        _launch(dev, stream, call, C.byref(ps), C.byref(bs), layer, seqs, start.data_ptr(), lengths.data_ptr(), max_new,
+                block_tables.data_ptr(), pages, _ptr(err))
+
+
+def pallas_bounds_kv(pool, layer: int, bounds, bound_scales, start, lengths, max_new: int, block_tables, err=None,
+                     stream=None):
+    """Bounds (bounds_pool_struct) of the blocks that hold positions [start, lengths) of a bf16 pool's sequences."""
+    dev = pool.get_device()
+    _whole(pool, "bounds: pool", (_torch or _load_torch()).bfloat16, 6, dev)
+    _bounds_call(lib().pallas_bounds_kv, kv_pool_struct(pool), dev, layer, bounds, bound_scales, start, lengths, max_new,
+                 block_tables, err, stream)
+
+
+def pallas_bounds_quant(codes, scales, layer: int, bounds, bound_scales, start, lengths, max_new: int, block_tables, err=None,
+                        stream=None):
+    """The same of an 8- or 4-bit pool (quant_pool_struct)."""
+    _bounds_call(lib().pallas_bounds_quant, quant_pool_struct(codes, scales), codes.get_device(), layer, bounds, bound_scales,
+                 start, lengths, max_new, block_tables, err, stream)
+
+
+def pallas_select_workspace_size(num_seqs: int, n_kv_heads: int, max_length: int) -> int:
+    return int(lib().pallas_select_workspace_size(num_seqs, n_kv_heads, max_length))
+
+
+def pallas_select_blocks(bounds, bound_scales, layer: int, q, lengths, max_length: int, block_tables, blocks, workspace,
+                         first: int = 1, last: int = 2, err=None, stream=None):
+    """Lists, in ``blocks`` (int32 [num_seqs, Hkv, max_blocks]), the blocks of each sequence that ``q`` (bf16 [num_seqs,
+    Hq, d], any row stride) scores highest, its ``first`` first and ``last`` last ones among them."""
+    bs, dev = bounds_pool_struct(bounds, bound_scales), bounds.get_device()
+    i32, shape = _torch.int32, q.shape
+    qs = _packed_rows(q, "select: q", dev, shape)
+    S, H, d = shape
+    seqs, pages = _whole(block_tables, "select: block tables", i32, 2, dev)
+    got = _whole(blocks, "select: blocks", i32, 3, dev)
+    if d != bs.head_dim or seqs != S or _whole(lengths, "select: lengths", i32, 1, dev)[0] != S or got[:2] != (
+            S, bs.n_kv_heads):
+        _bad(f"select: {tuple(shape)} queries, {lengths.shape[0]} lengths, {seqs} tables, blocks {tuple(got)}, bounds of "
+             f"{bs.n_kv_heads} heads of {bs.head_dim}")
+    if err is not None and not _whole(err, "select: err", i32, 1, dev)[0]:
+        _bad("select: an empty err")
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        _bad("select: workspace on another device, or not contiguous")
+    if S:
+        _launch(dev, stream, lib().pallas_select_blocks, C.byref(bs), layer, S, H, q.data_ptr(), qs, lengths.data_ptr(),
+                max_length, block_tables.data_ptr(), pages, got[2], first, last, blocks.data_ptr(), workspace.data_ptr(),
+                workspace.nbytes, _ptr(err))
 
 
 def _window_params(r_p, r_d, goodput, s_kv, t_load=0.0, t_0=0.0, alpha=0.8, t_max=5.0, dt=0.01):

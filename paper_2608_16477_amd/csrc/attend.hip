@@ -156,6 +156,18 @@ __device__ __forceinline__ int turn_slot(int row, int c) { return row * 4 + (c ^
 
 __device__ __forceinline__ int row_length(const AttendParams& p, int s) { return min(max(p.lengths[s], 0), p.max_length); }
 
+// What the work of a row is divided by: its keys, or 16 for each block of its list (as many
+// as it has blocks, at most; what the list holds behind them is not looked at).
+template <bool kListed>
+__device__ __forceinline__ int row_work(const AttendParams& p, int s) {
+  const int len = row_length(p, s);
+  return kListed ? min((len + kPage - 1) / kPage, p.listed) * kPage : len;
+}
+// Keys of a row's block (in its sixteen positions), 0 where the list names none of the row's.
+__device__ __forceinline__ int block_keys(int len, int block) {
+  return block >= 0 && block < (len + kPage - 1) / kPage ? min(len - block * kPage, kPage) : 0;
+}
+
 // Four outputs of a row, of weight sum l (0: no key; NaN stays), and at the first its
 // log-sum-exp.
 __device__ __forceinline__ void write_row(const AttendParams& p, int s, int h, int i, f32x4 o, float m, float l) {
@@ -434,10 +446,11 @@ struct Wave {
   }
 };
 
-// Lengths of 64 sequences from `at` on, one per lane, in 32-key blocks (0 behind the last).
+// Lengths of 64 sequences from `at` on, one per lane (0 behind the last).
+template <bool kListed>
 __device__ __forceinline__ int lane_length(const AttendParams& p, int at) {
   const int s = at + static_cast<int>(threadIdx.x & 63);
-  const int len = row_length(p, min(s, p.seqs - 1));
+  const int len = row_work<kListed>(p, min(s, p.seqs - 1));
   return s < p.seqs ? len : 0;
 }
 __device__ __forceinline__ int blocks_of(int len) { return static_cast<int>((static_cast<uint32_t>(len) + kBlk - 1) / kBlk); }
@@ -454,7 +467,7 @@ __device__ __forceinline__ int wave_prefix(int v) {
   return v;
 }
 
-template <int D, CacheType T>
+template <int D, CacheType T, bool kListed>
 __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, int groups, int head_shift) {
   using S = Shape<D, T>;
   constexpr int DT = D / 16;
@@ -476,11 +489,11 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
   // One sequence: the pages of this range, were it of one block (lanes 0, 1) or of two
   // (lanes 8 to 11), are read beside the length (a short call is a chain of loads).
   int ahead = 0;
-  if (p.seqs == 1) ahead = p.bt[min(lane < 8 ? 2 * r0 + lane : 4 * r0 + lane - 8, p.max_pages - 1)];
-  int win = 0, lens = lane_length(p, 0);        // lens: of sequences [win, win + 64)
+  if (!kListed && p.seqs == 1) ahead = p.bt[min(lane < 8 ? 2 * r0 + lane : 4 * r0 + lane - 8, p.max_pages - 1)];
+  int win = 0, lens = lane_length<kListed>(p, 0);        // lens: of sequences [win, win + 64)
 
   const int h0 = kh * p.G + group * kAttendGroup, nh = min(kAttendGroup, p.G - group * kAttendGroup);
-  Wave<D, T, 0> w;
+  Wave<D, T, kListed ? 1 : 0> w;
   w.init(p, kh, lds + wave * S::kWaveSlots);
 
   // All blocks of the call, and the ranges they make.  coarse: blocks of the first (lane +
@@ -492,7 +505,7 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
     int sum = 0;
 #pragma unroll 8
     for (int n = 0; n < share; ++n) {
-      const int q = lane * share + n, len = row_length(p, min(q, p.seqs - 1));
+      const int q = lane * share + n, len = row_work<kListed>(p, min(q, p.seqs - 1));
       sum += q < p.seqs ? blocks_of(len) : 0;
     }
     coarse = wave_prefix(sum);
@@ -502,7 +515,7 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
   auto window = [&](int s) {                    // makes s one of the 64
     if (s >= win && s < win + 64) return;
     win = s & ~63;
-    lens = lane_length(p, win);
+    lens = lane_length<kListed>(p, win);
     before = wave_prefix(blocks_of(lens));
   };
   auto length = [&](int s) {
@@ -563,11 +576,18 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
       break;
     }
     if (each == 2) ahead = __builtin_amdgcn_mov_dpp(ahead, 0x108, 0xF, 0xF, false);   // row_shl:8
+    if constexpr (kListed) {
+      if (w.keys > 0) {
+        const int block = p.lists[(int64_t(from) * p.Hkv + kh) * p.listed + key0 / kPage];
+        w.keys = block_keys(row_length(p, from), block);
+        key0 = w.keys > 0 ? block * kPage : 0;
+      }
+    }
     if (w.keys > 0) {
-      w.page = p.seqs == 1 && each <= 2 ? ahead : p.bt[int64_t(from) * p.max_pages + key0 / kPage];
+      w.page = !kListed && p.seqs == 1 && each <= 2 ? ahead : p.bt[int64_t(from) * p.max_pages + key0 / kPage];
       if (w.page < 0 || w.page >= p.num_pages) {
         w.page = w.keys = 0;
-        if (p.err && head == 0) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
+        if (p.err && (kListed || head == 0)) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
       }
     }
 #pragma unroll
@@ -619,7 +639,7 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
 // The same for calls of little work: a workgroup per split of `per` blocks of a sequence,
 // KV head and group of query heads, whose waves take equal runs of its blocks and merge
 // them through LDS.  A row of one split is written as it is (short rows: one launch).
-template <int D, CacheType T, int kWaves>
+template <int D, CacheType T, int kWaves, bool kListed>
 __global__ __launch_bounds__(kBoundThreads) void attend_split_kernel(AttendParams p, int groups, int splits, int per) {
   using S = Shape<D, T>;
   constexpr int DT = D / 16;
@@ -642,23 +662,30 @@ __global__ __launch_bounds__(kBoundThreads) void attend_split_kernel(AttendParam
   const int kh = groups == 1 ? head : head / groups, group = head - kh * groups;
   const int h0 = kh * p.G + group * kAttendGroup, nh = min(kAttendGroup, p.G - group * kAttendGroup);
   // The split's pages (at most 64) beside the row's length.
-  int page = p.bt[int64_t(s) * p.max_pages + min(2 * f0 + lane, p.max_pages - 1)];
-  Wave<D, T, kWaves> w;
+  int page;
+  if constexpr (kListed) page = p.lists[(int64_t(s) * p.Hkv + kh) * p.listed + min(2 * f0 + lane, p.listed - 1)];
+  else page = p.bt[int64_t(s) * p.max_pages + min(2 * f0 + lane, p.max_pages - 1)];
+  Wave<D, T, kListed ? kWaves + 1 : kWaves> w;
   w.load_q(p, s, h0, nh, w.qf);
   const int len = row_length(p, s);
   w.init(p, kh, lds + wave * S::kWaveSlots);
-  const int blocks_all = blocks_of(len), all = min(max(blocks_all - f0, 0), per);
+  const int work = row_work<kListed>(p, s), blocks_all = blocks_of(work), all = min(max(blocks_all - f0, 0), per);
   if (split > 0 && all == 0) return;
   const int each = (all + kWaves - 1) / kWaves;
   const int b0 = min(wave * each, all), blocks = min(each, all - b0);
+  int keys = min(max(work - (2 * f0 + lane) * kPage, 0), kPage);
+  if constexpr (kListed) {
+    const int block = page;
+    keys = keys > 0 ? block_keys(len, block) : 0;
+    page = p.bt[int64_t(s) * p.max_pages + (keys > 0 ? block : 0)];
+  }
   const bool bad = page < 0 || page >= p.num_pages;
-  const int key0 = (2 * f0 + lane) * kPage;
-  if (p.err && wave == 0 && head == 0) {
-    if (bad && key0 < len) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
-    if (split == 0 && lane == 0 && len != p.lengths[s]) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_LENGTH));
+  if (p.err && wave == 0 && (kListed || head == 0)) {
+    if (bad && keys > 0) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
+    if (split == 0 && head == 0 && lane == 0 && len != p.lengths[s]) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_LENGTH));
   }
   // (Lane 2 i + h: of the wave's block i.)
-  w.keys = __shfl(bad ? 0 : min(max(len - key0, 0), kPage), 2 * b0 + lane, 64);
+  w.keys = __shfl(bad ? 0 : keys, 2 * b0 + lane, 64);
   w.page = __shfl(page, 2 * b0 + lane, 64);
 #pragma unroll
   for (int i = 0; i < kStages; ++i) w.issue(p, i, i < blocks, i);
@@ -785,10 +812,10 @@ hipError_t launch_join(const AttendParams& p, int64_t most, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int D, CacheType T, int kWaves>
+template <int D, CacheType T, int kWaves, bool kListed>
 hipError_t launch_split(const AttendParams& p, int groups, int splits, int per, hipStream_t s) {
   const int64_t items = int64_t(p.seqs) * splits, all = items < 8 ? items : (items + 7) / 8 * 8;
-  attend_split_kernel<D, T, kWaves><<<static_cast<unsigned>(all * p.Hkv * groups), kWaves * 64, 0, s>>>(p, groups, splits, per);
+  attend_split_kernel<D, T, kWaves, kListed><<<static_cast<unsigned>(all * p.Hkv * groups), kWaves * 64, 0, s>>>(p, groups, splits, per);
   if (hipError_t e = hipGetLastError(); e != hipSuccess || splits == 1) return e;
   return launch_join<D>(p, splits, s);
 }
@@ -811,24 +838,29 @@ constexpr int kShortKeys = 512;
 constexpr int kShortGroups = 1536;
 constexpr int kSplitBlocks = 2;
 
-template <int D, CacheType T>
+template <int D, CacheType T, bool kListed>
 hipError_t launch(const AttendParams& p, hipStream_t s) {
   const int groups = (p.G + kAttendGroup - 1) / kAttendGroup, heads = p.Hkv * groups;
   constexpr int kFill = std::min(attend_waves(T, D), 8);     // waves whose rings fill a CU's LDS
   const int64_t rows = int64_t(p.seqs) * heads;
-  const int most = static_cast<int>(attend_total(1, p.max_length));       // blocks of a row
-  if (p.max_length <= kShortKeys && rows <= kShortGroups)
-    return rows <= 256 ? launch_split<D, T, kFill>(p, groups, 1, most, s) : launch_split<D, T, kFill / 2>(p, groups, 1, most, s);
+  const int most = static_cast<int>(attend_total(1, p.max_row));        // blocks of a row
+  if (p.max_row <= kShortKeys && rows <= kShortGroups)
+    return rows <= 256 ? launch_split<D, T, kFill, kListed>(p, groups, 1, most, s) : launch_split<D, T, kFill / 2, kListed>(p, groups, 1, most, s);
   for (int each = 1; each <= kSplitBlocks; each *= 2) {
     // (Records, seqs * splits <= 256 / heads: fewer than attend_ranges, so there is room.)
     const int per = kFill * each, splits = (most + per - 1) / per;
-    if (rows * splits <= 256) return launch_split<D, T, kFill>(p, groups, splits, per, s);
+    if (rows * splits <= 256) return launch_split<D, T, kFill, kListed>(p, groups, splits, per, s);
   }
   const int head_shift = heads % 4 == 0 ? 2 : heads % 2 == 0 ? 1 : 0;
   const int per = kWaves >> head_shift;         // ranges of a workgroup
-  attend_kernel<D, T><<<dim3((p.ranges + per - 1) / per, heads >> head_shift), kWaves * 64, 0, s>>>(p, groups, head_shift);
+  attend_kernel<D, T, kListed><<<dim3((p.ranges + per - 1) / per, heads >> head_shift), kWaves * 64, 0, s>>>(p, groups, head_shift);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   return launch_join<D>(p, p.ranges / p.seqs < kJoinBatch * 256 / D ? 0 : attend_row_records(most, p.seqs, p.ranges), s);
+}
+
+template <int D, CacheType T>
+hipError_t launch(const AttendParams& p, hipStream_t s) {
+  return p.lists ? launch<D, T, true>(p, s) : launch<D, T, false>(p, s);
 }
 
 template <int D>

@@ -208,11 +208,19 @@ int check_attend(int32_t num_seqs, int32_t n_q_heads, int32_t n_kv_heads, int32_
   return PALLAS_OK;
 }
 
+// The blocks of a call's lists (attend_all: no lists, every block).
+struct BlockLists {
+  bool listed;
+  const int32_t* d_blocks;
+  int32_t max_blocks;
+};
+constexpr BlockLists attend_all{false, nullptr, 0};
+
 // Checks and parameters of both cache types; the caller has checked the pool.
 int attend_call(const char* what, pallas::CacheType type, pallas::AttendParams& p, int page_size, int32_t num_seqs,
                 int32_t n_q_heads, const void* d_q, int64_t q_stride, const int32_t* d_lengths, int32_t max_length,
-                const int32_t* d_block_tables, int32_t max_pages, float scale, void* d_out, int64_t out_stride,
-                float* d_lse, void* d_workspace, size_t ws_bytes, int32_t* d_err, void* stream) {
+                const int32_t* d_block_tables, int32_t max_pages, BlockLists lists, float scale, void* d_out,
+                int64_t out_stride, float* d_lse, void* d_workspace, size_t ws_bytes, int32_t* d_err, void* stream) {
   if (int rc = check_attend(num_seqs, n_q_heads, p.Hkv, p.d, max_length, what)) return rc;
   if (!d_q || !d_lengths || !d_block_tables || !d_out || max_pages <= 0)
     return fail(PALLAS_ERR_INVALID_ARG, "%s: null query, lengths, tables or output, or max_pages <= 0", what);
@@ -226,11 +234,16 @@ int attend_call(const char* what, pallas::CacheType type, pallas::AttendParams& 
   if (max_length > int64_t(max_pages) * page_size)
     return fail(PALLAS_ERR_OUT_OF_RANGE, "%s: max_length %d outside the table (%lld)", what, max_length,
                 (long long)(int64_t(max_pages) * page_size));
+  if (lists.listed && (!lists.d_blocks || !aligned(lists.d_blocks, 4) || lists.max_blocks < 1))
+    return fail(PALLAS_ERR_INVALID_ARG, "%s: blocks null or not 4-byte aligned, or max_blocks below 1", what);
   p.scale_log2 = static_cast<float>(double(scale) * 1.4426950408889634);
   if (!std::isfinite(p.scale_log2)) return fail(PALLAS_ERR_INVALID_ARG, "%s: scale is not finite", what);
   if (!d_workspace || !aligned(d_workspace, 256))
     return fail(PALLAS_ERR_INVALID_ARG, "%s: workspace null or not 256-byte aligned", what);
-  const AttendSpace sp = attend_space(num_seqs, n_q_heads, p.d, max_length, most_ranges(n_q_heads, p.Hkv, p.d));
+  p.lists = lists.d_blocks;
+  p.listed = lists.max_blocks;
+  p.max_row = lists.listed ? std::min((max_length - 1) / page_size + 1, lists.max_blocks) * page_size : max_length;
+  const AttendSpace sp = attend_space(num_seqs, n_q_heads, p.d, p.max_row, most_ranges(n_q_heads, p.Hkv, p.d));
   if (ws_bytes < sp.bytes)
     return fail(PALLAS_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", what, ws_bytes, sp.bytes);
   p.Hq = n_q_heads;
@@ -255,6 +268,102 @@ int attend_call(const char* what, pallas::CacheType type, pallas::AttendParams& 
   hipStream_t s = static_cast<hipStream_t>(stream);
   pallas::ProfScope ps(PALLAS_K_DECODE_ATTN, s);
   return launched(pallas::launch_attend(p, type, s), "attend launch");
+}
+
+int attend_kv(const char* what, const pallas_kv_pool* pool, int32_t layer, int32_t num_seqs, int32_t n_q_heads,
+              const void* d_q, int64_t q_stride, const int32_t* d_lengths, int32_t max_length,
+              const int32_t* d_block_tables, int32_t max_pages, BlockLists lists, float scale, void* d_out,
+              int64_t out_stride, float* d_lse, void* d_workspace, size_t ws_bytes, int32_t* d_err, void* stream) {
+  if (int rc = check_kv_pool(pool, layer, what)) return rc;
+  const int64_t plane = int64_t(pool->num_pages) * pool->page_size * pool->n_kv_heads * pool->head_dim;
+  pallas::AttendParams p{};
+  p.k = static_cast<const uint16_t*>(pool->base) + 2 * layer * plane;
+  p.v = static_cast<const uint16_t*>(pool->base) + (2 * layer + 1) * plane;
+  p.num_pages = pool->num_pages;
+  p.Hkv = pool->n_kv_heads;
+  p.d = pool->head_dim;
+  return attend_call(what, pallas::kCacheBf16, p, pool->page_size, num_seqs, n_q_heads, d_q, q_stride, d_lengths,
+                     max_length, d_block_tables, max_pages, lists, scale, d_out, out_stride, d_lse, d_workspace, ws_bytes,
+                     d_err, stream);
+}
+
+int attend_quant(const char* what, const pallas_quant_pool* pool, int32_t layer, int32_t num_seqs, int32_t n_q_heads,
+                 const void* d_q, int64_t q_stride, const int32_t* d_lengths, int32_t max_length,
+                 const int32_t* d_block_tables, int32_t max_pages, BlockLists lists, float scale, void* d_out,
+                 int64_t out_stride, float* d_lse, void* d_workspace, size_t ws_bytes, int32_t* d_err, void* stream) {
+  if (int rc = check_quant_pool(pool, layer, what)) return rc;
+  const int64_t rows = plane_rows(pool);
+  if (2 * rows * 4 > int64_t(0xFFFFFF00))   // addressed with 32-bit offsets
+    return fail(PALLAS_ERR_UNSUPPORTED, "%s: a layer's scales of %lld bytes exceed 4 GiB", what, (long long)(2 * rows * 4));
+  pallas::AttendParams p{};
+  p.k = static_cast<const uint8_t*>(pool->codes) + 2 * layer * rows * code_bytes(pool);
+  p.v = static_cast<const uint8_t*>(pool->codes) + (2 * layer + 1) * rows * code_bytes(pool);
+  p.scales = pool->scales + 2 * layer * rows;
+  p.num_pages = pool->num_pages;
+  p.Hkv = pool->n_kv_heads;
+  p.d = pool->head_dim;
+  return attend_call(what, cache_type(pool), p, pool->page_size, num_seqs, n_q_heads, d_q, q_stride, d_lengths,
+                     max_length, d_block_tables, max_pages, lists, scale, d_out, out_stride, d_lse, d_workspace, ws_bytes,
+                     d_err, stream);
+}
+
+// ------------------------------------------------------------ blocks
+int check_bounds(const pallas_bounds_pool* b, int layer, const char* what) {
+  if (!b) return fail(PALLAS_ERR_INVALID_ARG, "%s: null bounds", what);
+  if (!b->codes || !b->scales || !aligned(b->codes, 16) || !aligned(b->scales, 16))
+    return fail(PALLAS_ERR_INVALID_ARG, "%s: bounds' codes or scales null or not 16-byte aligned", what);
+  if (b->num_pages <= 0 || b->n_layers <= 0 || b->n_kv_heads <= 0 || b->head_dim <= 0)
+    return fail(PALLAS_ERR_INVALID_ARG, "%s: non-positive dimension of the bounds", what);
+  if (layer < 0 || layer >= b->n_layers)
+    return fail(PALLAS_ERR_OUT_OF_RANGE, "%s: layer %d of %d", what, layer, b->n_layers);
+  if (b->head_dim != 64 && b->head_dim != 128)
+    return fail(PALLAS_ERR_UNSUPPORTED, "%s: head_dim %d (supported: 64, 128)", what, b->head_dim);
+  if (b->n_kv_heads > 4096) return fail(PALLAS_ERR_UNSUPPORTED, "%s: %d KV heads (at most 4096)", what, b->n_kv_heads);
+  return PALLAS_OK;
+}
+
+int bounds_call(const char* what, pallas::CacheType type, pallas::BoundsParams& p, int n_layers,
+                const pallas_bounds_pool* bounds, int32_t layer, int32_t num_seqs, const int32_t* d_start,
+                const int32_t* d_lengths, int32_t max_new, const int32_t* d_block_tables, int32_t max_pages,
+                int32_t* d_err, void* stream) {
+  if (int rc = check_bounds(bounds, layer, what)) return rc;
+  if (bounds->num_pages != p.num_pages || bounds->n_layers != n_layers || bounds->n_kv_heads != p.Hkv || bounds->head_dim != p.d)
+    return fail(PALLAS_ERR_INVALID_ARG, "%s: bounds and cache of different pages, layers, heads or head_dim", what);
+  if (num_seqs < 1 || max_new < 1 || max_pages <= 0 || !d_start || !d_lengths || !d_block_tables)
+    return fail(PALLAS_ERR_INVALID_ARG, "%s: null start, lengths or tables, or num_seqs, max_new or max_pages below 1", what);
+  if (!aligned(d_start, 4) || !aligned(d_lengths, 4) || !aligned(d_block_tables, 4) || !aligned(d_err, 4))
+    return fail(PALLAS_ERR_INVALID_ARG, "%s: start, lengths, tables or d_err not 4-byte aligned", what);
+  if (num_seqs > 65535 || int64_t(std::min(pallas::bounds_blocks(max_new), max_pages)) * p.Hkv >= (1 << 26))
+    return fail(PALLAS_ERR_UNSUPPORTED, "%s: %d sequences (at most 65535), up to %d positions of %d heads (below 2^26 blocks and heads)",
+                what, num_seqs, max_new, p.Hkv);
+  const int64_t rows = int64_t(bounds->num_pages) * bounds->n_kv_heads;
+  p.bounds = static_cast<int8_t*>(bounds->codes) + 2 * layer * rows * bounds->head_dim;
+  p.bound_scales = bounds->scales + layer * rows;
+  p.start = d_start;
+  p.lengths = d_lengths;
+  p.most = max_new;
+  p.bt = d_block_tables;
+  p.seqs = num_seqs;
+  p.max_pages = max_pages;
+  p.err = d_err;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  pallas::ProfScope ps(PALLAS_K_QKV_EPI, s);
+  return launched(pallas::launch_bounds(p, type, s), "bounds launch");
+}
+
+int check_select(int32_t num_seqs, int32_t n_kv_heads, int32_t max_length, const char* what) {
+  if (num_seqs < 1 || max_length < 1)
+    return fail(PALLAS_ERR_INVALID_ARG, "%s: num_seqs and max_length must be at least 1", what);
+  if (num_seqs > 65535 || int64_t(num_seqs) * max_length > (int64_t(1) << 35) ||
+      (int64_t(max_length) / 256 + 1) * n_kv_heads >= (1 << 26))      // (a launch has fewer than 2^32 threads)
+    return fail(PALLAS_ERR_UNSUPPORTED, "%s: %d sequences (at most 65535) of up to %d keys (at most 2^35 in all, below 2^34 with the heads)",
+                what, num_seqs, max_length);
+  return PALLAS_OK;
+}
+// The scores of a call: one word per sequence, KV head and block.
+int64_t select_stride(int max_length) { return (int64_t(max_length) + 63) / 64 * 4; }
+size_t select_space(int64_t seqs, int Hkv, int max_length) {
+  return (size_t(seqs) * Hkv * select_stride(max_length) * 4 + 255) / 256 * 256;
 }
 
 }  // namespace
@@ -410,18 +519,8 @@ int pallas_attend_kv(const pallas_kv_pool* pool, int32_t layer, int32_t num_seqs
                      int64_t q_stride, const int32_t* d_lengths, int32_t max_length, const int32_t* d_block_tables,
                      int32_t max_pages, float scale, void* d_out, int64_t out_stride, float* d_lse, void* d_workspace,
                      size_t ws_bytes, int32_t* d_err, void* stream) {
-  const char* what = "attend";
-  if (int rc = check_kv_pool(pool, layer, what)) return rc;
-  const int64_t plane = int64_t(pool->num_pages) * pool->page_size * pool->n_kv_heads * pool->head_dim;
-  pallas::AttendParams p{};
-  p.k = static_cast<const uint16_t*>(pool->base) + 2 * layer * plane;
-  p.v = static_cast<const uint16_t*>(pool->base) + (2 * layer + 1) * plane;
-  p.num_pages = pool->num_pages;
-  p.Hkv = pool->n_kv_heads;
-  p.d = pool->head_dim;
-  return attend_call(what, pallas::kCacheBf16, p, pool->page_size, num_seqs, n_q_heads, d_q, q_stride, d_lengths,
-                     max_length, d_block_tables, max_pages, scale, d_out, out_stride, d_lse, d_workspace, ws_bytes,
-                     d_err, stream);
+  return attend_kv("attend", pool, layer, num_seqs, n_q_heads, d_q, q_stride, d_lengths, max_length, d_block_tables,
+                   max_pages, attend_all, scale, d_out, out_stride, d_lse, d_workspace, ws_bytes, d_err, stream);
 }
 
 int pallas_attend_quant(const pallas_quant_pool* pool, int32_t layer, int32_t num_seqs, int32_t n_q_heads,
@@ -429,20 +528,118 @@ int pallas_attend_quant(const pallas_quant_pool* pool, int32_t layer, int32_t nu
                         const int32_t* d_block_tables, int32_t max_pages, float scale, void* d_out,
                         int64_t out_stride, float* d_lse, void* d_workspace, size_t ws_bytes, int32_t* d_err,
                         void* stream) {
-  const char* what = "attend (quantised)";
-  if (int rc = check_quant_pool(pool, layer, what)) return rc;
-  const int64_t rows = plane_rows(pool);
-  if (2 * rows * 4 > int64_t(0xFFFFFF00))   // addressed with 32-bit offsets
-    return fail(PALLAS_ERR_UNSUPPORTED, "%s: a layer's scales of %lld bytes exceed 4 GiB", what, (long long)(2 * rows * 4));
-  pallas::AttendParams p{};
-  p.k = static_cast<const uint8_t*>(pool->codes) + 2 * layer * rows * code_bytes(pool);
-  p.v = static_cast<const uint8_t*>(pool->codes) + (2 * layer + 1) * rows * code_bytes(pool);
-  p.scales = pool->scales + 2 * layer * rows;
+  return attend_quant("attend (quantised)", pool, layer, num_seqs, n_q_heads, d_q, q_stride, d_lengths, max_length,
+                      d_block_tables, max_pages, attend_all, scale, d_out, out_stride, d_lse, d_workspace, ws_bytes,
+                      d_err, stream);
+}
+
+int pallas_attend_blocks_kv(const pallas_kv_pool* pool, int32_t layer, int32_t num_seqs, int32_t n_q_heads,
+                            const void* d_q, int64_t q_stride, const int32_t* d_lengths, int32_t max_length,
+                            const int32_t* d_block_tables, int32_t max_pages, const int32_t* d_blocks,
+                            int32_t max_blocks, float scale, void* d_out, int64_t out_stride, float* d_lse,
+                            void* d_workspace, size_t ws_bytes, int32_t* d_err, void* stream) {
+  return attend_kv("attend (blocks)", pool, layer, num_seqs, n_q_heads, d_q, q_stride, d_lengths, max_length,
+                   d_block_tables, max_pages, {true, d_blocks, max_blocks}, scale, d_out, out_stride, d_lse, d_workspace,
+                   ws_bytes, d_err, stream);
+}
+
+int pallas_attend_blocks_quant(const pallas_quant_pool* pool, int32_t layer, int32_t num_seqs, int32_t n_q_heads,
+                               const void* d_q, int64_t q_stride, const int32_t* d_lengths, int32_t max_length,
+                               const int32_t* d_block_tables, int32_t max_pages, const int32_t* d_blocks,
+                               int32_t max_blocks, float scale, void* d_out, int64_t out_stride, float* d_lse,
+                               void* d_workspace, size_t ws_bytes, int32_t* d_err, void* stream) {
+  return attend_quant("attend (blocks, quantised)", pool, layer, num_seqs, n_q_heads, d_q, q_stride, d_lengths,
+                      max_length, d_block_tables, max_pages, {true, d_blocks, max_blocks}, scale, d_out, out_stride,
+                      d_lse, d_workspace, ws_bytes, d_err, stream);
+}
+
+int pallas_bounds_kv(const pallas_kv_pool* pool, const pallas_bounds_pool* bounds, int32_t layer, int32_t num_seqs,
+                     const int32_t* d_start, const int32_t* d_lengths, int32_t max_new, const int32_t* d_block_tables,
+                     int32_t max_pages, int32_t* d_err, void* stream) {
+  if (int rc = check_kv_pool(pool, layer, "bounds")) return rc;
+  pallas::BoundsParams p{};
+  const int64_t plane = int64_t(pool->num_pages) * pool->page_size * pool->n_kv_heads * pool->head_dim;
+  p.k = static_cast<const uint16_t*>(pool->base) + 2 * layer * plane;
   p.num_pages = pool->num_pages;
   p.Hkv = pool->n_kv_heads;
   p.d = pool->head_dim;
-  return attend_call(what, cache_type(pool), p, pool->page_size, num_seqs, n_q_heads, d_q, q_stride, d_lengths, max_length, d_block_tables,
-                     max_pages, scale, d_out, out_stride, d_lse, d_workspace, ws_bytes, d_err, stream);
+  return bounds_call("bounds", pallas::kCacheBf16, p, pool->n_layers, bounds, layer, num_seqs, d_start, d_lengths, max_new,
+                     d_block_tables, max_pages, d_err, stream);
+}
+
+int pallas_bounds_quant(const pallas_quant_pool* pool, const pallas_bounds_pool* bounds, int32_t layer,
+                        int32_t num_seqs, const int32_t* d_start, const int32_t* d_lengths, int32_t max_new,
+                        const int32_t* d_block_tables, int32_t max_pages, int32_t* d_err, void* stream) {
+  if (int rc = check_quant_pool(pool, layer, "bounds (quantised)")) return rc;
+  pallas::BoundsParams p{};
+  p.k = static_cast<const uint8_t*>(pool->codes) + 2 * layer * plane_rows(pool) * code_bytes(pool);
+  p.scales = pool->scales + 2 * layer * plane_rows(pool);
+  p.num_pages = pool->num_pages;
+  p.Hkv = pool->n_kv_heads;
+  p.d = pool->head_dim;
+  return bounds_call("bounds (quantised)", cache_type(pool), p, pool->n_layers, bounds, layer, num_seqs, d_start,
+                     d_lengths, max_new, d_block_tables, max_pages, d_err, stream);
+}
+
+int pallas_select_blocks(const pallas_bounds_pool* bounds, int32_t layer, int32_t num_seqs, int32_t n_q_heads,
+                         const void* d_q, int64_t q_stride, const int32_t* d_lengths, int32_t max_length,
+                         const int32_t* d_block_tables, int32_t max_pages, int32_t max_blocks, int32_t first,
+                         int32_t last, int32_t* d_blocks, void* d_workspace, size_t ws_bytes, int32_t* d_err,
+                         void* stream) {
+  const char* what = "select";
+  if (int rc = check_bounds(bounds, layer, what)) return rc;
+  if (int rc = check_select(num_seqs, bounds->n_kv_heads, max_length, what)) return rc;
+  if (n_q_heads < 1 || n_q_heads % bounds->n_kv_heads != 0)
+    return fail(PALLAS_ERR_INVALID_ARG, "%s: query heads not a multiple of KV heads", what);
+  if (n_q_heads > 4096) return fail(PALLAS_ERR_UNSUPPORTED, "%s: %d query heads (at most 4096)", what, n_q_heads);
+  if (!d_q || !d_lengths || !d_block_tables || !d_blocks || max_pages <= 0)
+    return fail(PALLAS_ERR_INVALID_ARG, "%s: null query, lengths, tables or blocks, or max_pages <= 0", what);
+  if (!aligned(d_q, 16) || q_stride % 8 != 0) return fail(PALLAS_ERR_INVALID_ARG, "%s: query rows not 16-byte aligned", what);
+  if (q_stride < int64_t(n_q_heads) * bounds->head_dim)
+    return fail(PALLAS_ERR_INVALID_ARG, "%s: row stride below the %lld elements of a row", what,
+                (long long)(int64_t(n_q_heads) * bounds->head_dim));
+  if (!aligned(d_lengths, 4) || !aligned(d_block_tables, 4) || !aligned(d_blocks, 4) || !aligned(d_err, 4))
+    return fail(PALLAS_ERR_INVALID_ARG, "%s: lengths, tables, blocks or d_err not 4-byte aligned", what);
+  if (max_length > int64_t(max_pages) * 16)
+    return fail(PALLAS_ERR_OUT_OF_RANGE, "%s: max_length %d outside the table (%lld)", what, max_length,
+                (long long)(int64_t(max_pages) * 16));
+  if (max_blocks < 1 || first < 0 || last < 0 || int64_t(first) + last > max_blocks)
+    return fail(PALLAS_ERR_INVALID_ARG, "%s: %d blocks, of them the first %d and the last %d", what, max_blocks, first, last);
+  if (!d_workspace || !aligned(d_workspace, 256))
+    return fail(PALLAS_ERR_INVALID_ARG, "%s: workspace null or not 256-byte aligned", what);
+  const size_t need = select_space(num_seqs, bounds->n_kv_heads, max_length);
+  if (ws_bytes < need) return fail(PALLAS_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", what, ws_bytes, need);
+  const int64_t rows = int64_t(bounds->num_pages) * bounds->n_kv_heads;
+  pallas::SelectParams p{};
+  p.bounds = static_cast<const int8_t*>(bounds->codes) + 2 * layer * rows * bounds->head_dim;
+  p.bound_scales = bounds->scales + layer * rows;
+  p.num_pages = bounds->num_pages;
+  p.Hkv = bounds->n_kv_heads;
+  p.G = n_q_heads / p.Hkv;
+  p.d = bounds->head_dim;
+  p.q = static_cast<const uint16_t*>(d_q);
+  p.q_stride = q_stride;
+  p.lengths = d_lengths;
+  p.max_length = max_length;
+  p.bt = d_block_tables;
+  p.seqs = num_seqs;
+  p.max_pages = max_pages;
+  p.budget = max_blocks;
+  p.first = first;
+  p.last = last;
+  p.blocks = d_blocks;
+  p.order = static_cast<uint32_t*>(d_workspace);
+  p.stride = select_stride(max_length);
+  p.err = d_err;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  pallas::ProfScope ps(PALLAS_K_DECODE_ATTN, s);
+  return launched(pallas::launch_select(p, s), "select launch");
+}
+
+size_t pallas_select_workspace_size(int32_t num_seqs, int32_t n_kv_heads, int32_t max_length) {
+  if (n_kv_heads < 1 || n_kv_heads > 4096 || check_select(num_seqs, n_kv_heads, max_length, "select workspace") != PALLAS_OK)
+    return 0;
+  return select_space(num_seqs, n_kv_heads, max_length);
 }
 
 size_t pallas_attend_workspace_size(int32_t num_seqs, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,

@@ -423,6 +423,9 @@ struct AttendParams {
   int64_t q_stride;
   const int32_t* lengths;
   const int32_t* bt;
+  const int32_t* lists;    // [seqs][Hkv][listed] blocks of 16 positions, or null: all
+  int listed;
+  int max_row;             // keys, or 16 times the blocks, that a row can have: max_length, or what its list holds
   float scale_log2;        // scale * log2(e)
   uint16_t* out;
   int64_t out_stride;
@@ -477,6 +480,42 @@ inline int64_t attend_records(int64_t seqs, int max_length, int ranges) {
   return std::min(total, ranges + total / kAttendMaxBlocks) + seqs;
 }
 hipError_t launch_attend(const AttendParams& p, CacheType type, hipStream_t s);
+
+// blocks.hip: bounds of the keys of 16-position blocks, and the blocks that score highest.
+struct BoundsParams {
+  const void* k;           // [num_pages][16][Hkv][d] of the layer
+  const float* scales;     // of its K rows (8 and 4 bits)
+  int num_pages, Hkv, d;
+  int8_t* bounds;          // [num_pages][Hkv][2][d] of the layer
+  float* bound_scales;     // [num_pages][Hkv]
+  const int32_t* start;    // blocks of positions [start, length) are due, at most `most` positions
+  const int32_t* lengths;
+  int most;
+  const int32_t* bt;
+  int seqs, max_pages;
+  int32_t* err;
+};
+// The blocks that n positions lie in, at most.
+constexpr int bounds_blocks(int n) { return static_cast<int>((int64_t(n) + 30) / 16); }
+hipError_t launch_bounds(const BoundsParams& p, CacheType type, hipStream_t s);
+
+struct SelectParams {
+  const int8_t* bounds;
+  const float* bound_scales;
+  int num_pages, Hkv, G, d;
+  const uint16_t* q;
+  int64_t q_stride;
+  const int32_t* lengths;
+  int max_length;
+  const int32_t* bt;
+  int seqs, max_pages;
+  int budget, first, last;
+  int32_t* blocks;         // [seqs][Hkv][budget]
+  uint32_t* order;         // [seqs][Hkv][stride], stride >= blocks of max_length
+  int64_t stride;
+  int32_t* err;
+};
+hipError_t launch_select(const SelectParams& p, hipStream_t s);
 
 // ------------------------------------------------------------ skinny GEMM
 // C[m][n] (op) A[m] . B[n] for m < M <= 8 rows (gemv.hip); epilogues as
