@@ -42,28 +42,35 @@ namespace {
 
 constexpr int kPage = 16;
 constexpr int kBlk = 32;                 // keys per block: two pages
-constexpr int kStages = 2;               // blocks in flight per wave
 constexpr int kWaves = 4;                // per workgroup, each on its own
 constexpr int kBoundThreads = 512;       // (256 registers a wave, no accumulation registers)
 constexpr int kAuxStream = 2;            // nt: K and V are read once
+constexpr int kTurnStep = kBlk * 4;      // 16-byte slots of a block's 32 dimensions of V as bf16
 constexpr uint32_t kRsrcFlags = 0x00020000;
 constexpr uint32_t kOutside = 0xFFFFFFF0u;   // a buffer offset past any range: reads zero
 
-template <int D, CacheType T>
+// kPair: a step is a page of two KV heads, a row of the ring theirs of a token; else two pages
+// of one head.
+template <int D, CacheType T, bool kPair>
 struct Shape {
   static constexpr int kRow = T == kCacheBf16 ? D * 2 : T == kCacheE2m1 ? D / 2 : D;   // bytes of a head row
-  static constexpr int kCh = kRow / 16;               // 16-byte chunks of it
+  static constexpr int kSteps = kPair ? 2 : 1;        // of a 32-key block
+  static constexpr int kPages = kPair ? 1 : 2;        // of a step
+  static constexpr int kCh = kRow * kSteps / 16;      // 16-byte chunks of a ring's row
   static constexpr int kRowsPerLoad = 64 / kCh;       // rows per load instruction
   static constexpr int kPerPage = std::max(kPage / kRowsPerLoad, 1);
   static constexpr int kPageSlots = kPerPage * 64;    // 16-byte slots of a page (E2M1 rows of 64: half of them rows)
-  static constexpr int kScaleSlots = T == kCacheBf16 ? 0 : 16;   // 32 K scales, 32 V scales
-  static constexpr int kSlots = 4 * kPageSlots + kScaleSlots;    // of a stage
-  static constexpr int kLoads = 4 * kPerPage + (T == kCacheBf16 ? 0 : 1);   // instructions per block
+  static constexpr int kScales = 2 * kPages * kPageSlots;        // where a stage's scales are
+  static constexpr int kScaleSlots = T == kCacheBf16 ? 0 : 16;   // of 32 K rows, 32 V rows
+  static constexpr int kSlots = kScales + kScaleSlots;           // of a stage
+  static constexpr int kLoads = 2 * kPages * kPerPage + (T == kCacheBf16 ? 0 : 1);   // instructions per step
+  static constexpr int kStages = 2;                   // steps in flight per wave
   static constexpr int kRing = kStages * kSlots;
-  static constexpr int kTurn = T == kCacheE2m1 ? kBlk * 4 : 0;   // 32 dimensions of V as bf16
-  static constexpr int kWaveSlots = kRing + kTurn;               // of a wave
+  static constexpr int kTurn = T == kCacheE2m1 ? 2 * kTurnStep : 0;   // where V is turned, beside the stage itself
+  static constexpr int kMerge = kPair ? kAttendGroup / 2 : 0;    // maximum and sum of each query head
+  static constexpr int kWaveSlots = kRing + kTurn + kMerge;      // of a wave
   // attend_ranges counts on the waves that a CU's 160 KiB of LDS hold.
-  static_assert(160 * 1024 / (4 * kWaveSlots * 16) * 4 >= attend_waves(T, D), "resident waves");
+  static_assert(160 * 1024 / (4 * kWaveSlots * 16) * 4 >= (kPair ? 4 * kAttendPairGroups : attend_waves(T, D)), "resident waves");
 };
 
 // Chunk swizzles of 8-bit rows of CH chunks (8 rows of 128 bytes, or 16 of 64, fill the
@@ -76,14 +83,14 @@ template <int CH>
 __device__ __forceinline__ int swz8_v(int row) {
   return CH == 8 ? ((row >> 1) & 3) | ((row >> 2) & 4) : ((row >> 2) & 1) | ((row >> 3) & 2);
 }
-// 4-bit rows of CH chunks (4 rows of 64 bytes fill the banks, or 8 of 32): the 16 rows of
-// a K read at one chunk, or, of 32 bytes, at half a chunk; the 16 rows of half a V read.
+// 4-bit rows of CH chunks (2 rows of 128 bytes fill the banks, 4 of 64, or 8 of 32): the 16 rows of
+// a K read at one chunk, or, of heads of 32 bytes, at half a chunk; the 16 rows of half a V read.
 template <int CH>
-__device__ __forceinline__ int swz4(int row) { return CH == 4 ? (row >> 2) & 3 : (row >> 3) & 1; }
+__device__ __forceinline__ int swz4(int row) { return CH == 8 ? (row >> 1) & 7 : CH == 4 ? (row >> 2) & 3 : (row >> 3) & 1; }
 template <CacheType T, int CH>
 __device__ __forceinline__ int k_slot(int row) {
   if constexpr (T == kCacheBf16) return swz_k<CH>(row);
-  else if constexpr (T == kCacheE2m1) return CH == 4 ? swz4<CH>(row) : 0;
+  else if constexpr (T == kCacheE2m1) return CH > 2 ? swz4<CH>(row) : 0;
   else return swz8_k<CH>(row);
 }
 template <CacheType T, int CH>
@@ -133,22 +140,29 @@ __device__ __forceinline__ void read_pv8(uint32_t vb, int dt0, u32x2* a) {
   a[0] = r0, a[1] = r1, a[2] = r2, a[3] = r3;
 }
 
-// Two output tiles of the PV operand from 32 rows of 32 bf16 dimensions at LDS byte
-// address `vb` (read_pv4; tiles XOR 32 bytes, the second page 1024 bytes further).
-__device__ __forceinline__ void read_pv2(uint32_t vb, u32x4* a) {
+// Four output tiles of the PV operand from twice 32 rows of 32 bf16 dimensions, 2048 bytes
+// apart, at LDS byte address `vb` (read_pv4; the second tile XOR 32 bytes, the second page 1024
+// bytes further).
+__device__ __forceinline__ void read_turned4(uint32_t vb, u32x4* a) {
   const uint32_t x1 = vb ^ 32u;
-  u32x2 l0, l1, h0, h1;
+  u32x2 l0, l1, l2, l3, h0, h1, h2, h3;
   asm volatile(
-      "ds_read_b64_tr_b16 %0, %4\n\t"
-      "ds_read_b64_tr_b16 %1, %4 offset:1024\n\t"
-      "ds_read_b64_tr_b16 %2, %5\n\t"
-      "ds_read_b64_tr_b16 %3, %5 offset:1024\n\t"
+      "ds_read_b64_tr_b16 %0, %8\n\t"
+      "ds_read_b64_tr_b16 %1, %8 offset:1024\n\t"
+      "ds_read_b64_tr_b16 %2, %9\n\t"
+      "ds_read_b64_tr_b16 %3, %9 offset:1024\n\t"
+      "ds_read_b64_tr_b16 %4, %8 offset:2048\n\t"
+      "ds_read_b64_tr_b16 %5, %8 offset:3072\n\t"
+      "ds_read_b64_tr_b16 %6, %9 offset:2048\n\t"
+      "ds_read_b64_tr_b16 %7, %9 offset:3072\n\t"
       "s_waitcnt lgkmcnt(0)"
-      : "=&v"(l0), "=&v"(h0), "=&v"(l1), "=&v"(h1)
+      : "=&v"(l0), "=&v"(h0), "=&v"(l1), "=&v"(h1), "=&v"(l2), "=&v"(h2), "=&v"(l3), "=&v"(h3)
       : "v"(vb), "v"(x1)
       : "memory");
   a[0] = u32x4{l0.x, l0.y, h0.x, h0.y};
   a[1] = u32x4{l1.x, l1.y, h1.x, h1.y};
+  a[2] = u32x4{l2.x, l2.y, h2.x, h2.y};
+  a[3] = u32x4{l3.x, l3.y, h3.x, h3.y};
 }
 // Slot of chunk `c` of such a row: half a transposed read (8 rows, 2 chunks of each) falls
 // on all banks.
@@ -189,14 +203,15 @@ __device__ __forceinline__ float join_weight(float m, float l, float top) {
 // reads of a block, and the softmax of the sequence that it is in.  (kOf: a type for each
 // kernel.  Of kernels that share one, the compiler's host pass emits the stub of the first
 // alone.)
-template <int D, CacheType T, int kOf>
+template <int D, CacheType T, bool kPair, int kOf>
 struct Wave {
-  using S = Shape<D, T>;
-  static constexpr int CH = S::kCh, DT = D / 16;
+  using S = Shape<D, T, kPair>;
+  static constexpr int CH = S::kCh, DT = D / 16, kStages = S::kStages;
   const char* k;          // layer planes, at this KV head
   const char* v;
   uint32_t rs;            // bytes between tokens of a page
   int kh;
+  bool second;            // kPair: this lane's query head is of the second KV head
   int page, keys;         // lane 2 i + h: page of half h of block i, and the keys in it (0: none, or no page of the pool)
   uint32_t koff[S::kPerPage], voff[2 * S::kPerPage];   // byte offset in a page of what this lane loads in an instruction
   uint32_t kb0, vb0;      // where this lane reads: a K block at (row l16, chunk q4), a V block transposed
@@ -208,7 +223,8 @@ struct Wave {
 
   __device__ __forceinline__ void init(const AttendParams& p, int head, u32x4* at) {
     const int lane = threadIdx.x & 63, q4 = lane >> 4, l16 = lane & 15;
-    kh = head;
+    kh = kPair ? 2 * head : head;
+    second = kPair && l16 >= p.G;
     rs = static_cast<uint32_t>(p.Hkv) * S::kRow;
     k = static_cast<const char*>(p.k) + int64_t(kh) * S::kRow;
     v = static_cast<const char*>(p.v) + int64_t(kh) * S::kRow;
@@ -223,8 +239,9 @@ struct Wave {
     }
     kb0 = static_cast<uint32_t>(l16 * CH + (q4 ^ k_slot<T, CH>(l16)));
     if constexpr (T == kCacheE2m1) {
-      // (K in units of what a lane reads of a row, 16 or 8 bytes; V from the turned rows)
-      if constexpr (CH == 2) kb0 = static_cast<uint32_t>(l16 * 4 + q4);
+      // (K in bytes; kPair: of the first head, half a row before the second; V from the turned rows)
+      constexpr int kPart = D / 8;    // bytes of a lane's quarter
+      kb0 = static_cast<uint32_t>((l16 * CH + (q4 * kPart / 16 ^ k_slot<T, CH>(l16))) * 16 + q4 * kPart % 16);
       const int key = 4 * q4 + (l16 >> 2);
       vb0 = static_cast<uint32_t>(turn_slot(key, (l16 & 3) >> 1) * 16 + (l16 & 1) * 8);
     } else if constexpr (T == kCacheBf16) {
@@ -260,17 +277,17 @@ struct Wave {
     lsum = 0.f;
   }
 
-  // Loads of block `i` into a stage: rows that exist; everything else reads zeros, as do
-  // blocks that are not `in`.  Every step issues its loads, so that those in flight can be
+  // Loads of step `i` into a stage: rows that exist; everything else reads zeros, as do
+  // steps that are not `in`.  Every step issues its loads, so that those in flight can be
   // counted.
   __device__ __forceinline__ void issue(const AttendParams& p, int i, bool in, int stage) const {
     u32x4* const st = ring + stage * S::kSlots;
-    int pg[2], nv[2];
+    int pg[S::kPages], nv[S::kPages];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      pg[h] = __builtin_amdgcn_readlane(page, (i * 2 + h) & 63);
-      nv[h] = in ? __builtin_amdgcn_readlane(keys, (i * 2 + h) & 63) : 0;
-      const uint32_t range = nv[h] > 0 ? static_cast<uint32_t>(nv[h] - 1) * rs + S::kRow : 0;
+    for (int h = 0; h < S::kPages; ++h) {
+      pg[h] = __builtin_amdgcn_readlane(page, (i * S::kPages + h) & 63);
+      nv[h] = in ? __builtin_amdgcn_readlane(keys, (i * S::kPages + h) & 63) : 0;
+      const uint32_t range = nv[h] > 0 ? static_cast<uint32_t>(nv[h] - 1) * rs + S::kRow * S::kSteps : 0;
       const int64_t base = nv[h] > 0 ? pg[h] * (int64_t(kPage) * rs) : 0;
       const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc((void*)(k + base), 0, range, kRsrcFlags);
       const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void*)(v + base), 0, range, kRsrcFlags);
@@ -279,29 +296,40 @@ struct Wave {
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void*)(st + h * S::kPageSlots + n * 64), 16, koff[n], 0, 0, kAuxStream);
 #pragma unroll
       for (int n = 0; n < S::kPerPage; ++n)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void*)(st + (2 + h) * S::kPageSlots + n * 64), 16,
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void*)(st + (S::kPages + h) * S::kPageSlots + n * 64), 16,
                                                  voff[h * S::kPerPage + n], 0, 0, kAuxStream);
     }
     if constexpr (T != kCacheBf16) {
-      // Lane l: the K (below 32) or V scale of key l % 32.
-      const int lane = threadIdx.x & 63, key = lane % kPage;
-      const bool second = lane & kPage;
-      const uint32_t pgl = second ? pg[1] : pg[0];
-      const uint32_t row = ((lane < 32 ? pgl : pgl + p.num_pages) * kPage + key) * p.Hkv + kh;
-      const bool live = key < (second ? nv[1] : nv[0]);
+      // Lane l: the K (below 32) or V scale of key l % 32 (kPair: of key l % 32 / 2 and head l % 2).
+      const int lane = threadIdx.x & 63, key = kPair ? lane / 2 % kPage : lane % kPage;
+      const bool other = !kPair && (lane & kPage);
+      const uint32_t pgl = other ? pg[S::kPages - 1] : pg[0];
+      const uint32_t row = ((lane < 32 ? pgl : pgl + p.num_pages) * kPage + key) * p.Hkv + kh + (kPair ? lane % 2 : 0);
+      const bool live = key < (other ? nv[S::kPages - 1] : nv[0]);
       const __amdgpu_buffer_rsrc_t scales = __builtin_amdgcn_make_buffer_rsrc(
           (void*)p.scales, 0, static_cast<uint32_t>(p.num_pages) * (2 * kPage * 4) * p.Hkv, kRsrcFlags);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(scales, (lds_void*)(st + 4 * S::kPageSlots), 4, live ? row * 4 : kOutside, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(scales, (lds_void*)(st + S::kScales), 4, live ? row * 4 : kOutside, 0, 0, 0);
     }
   }
 
-  // The oldest of the kStages blocks whose loads were issued is here.
+  // The running maximum takes in mx.
+  __device__ __forceinline__ void rescale(float mx) {
+    if (__builtin_amdgcn_ballot_w64(mx > m) == 0) return;
+    const float m_new = fmaxf(m, mx);
+    const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+    m = m_new;
+    lsum *= alpha;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) acc[dt] *= alpha;
+  }
+
+  // The oldest of the kStages steps whose loads were issued is here.
   __device__ __forceinline__ void await_block() const {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kStages - 1) * S::kLoads) : "memory");
   }
 
-  // Blocks [i, stop), i below it, block n in stage n % kStages, the loads of the next kStages
-  // - 1 in flight; `blocks`: all that the wave takes.  Block i is here, and block `stop` at
+  // Steps [i, stop), i below it, step n in stage n % kStages, the loads of the next kStages
+  // - 1 in flight; `blocks`: all that the wave takes.  Step i is here, and step `stop` at
   // the end: what the wave stores and loads between two calls is behind the ring's loads, and
   // a wait at the head of a block would empty the ring to get past it.
   __device__ __forceinline__ void stream(const AttendParams& p, int& i, int stop, int blocks) {
@@ -310,7 +338,7 @@ struct Wave {
     do {
       const int stage = static_cast<int>(static_cast<unsigned>(i) % kStages);
       const u32x4* const Kst = ring + stage * S::kSlots;
-      const u32x4* const Vst = Kst + 2 * S::kPageSlots;
+      const u32x4* const Vst = Kst + S::kPages * S::kPageSlots;
       f32x4 sc[2] = {f32x4{}, f32x4{}};
       if constexpr (T == kCacheBf16) {
 #pragma unroll
@@ -322,18 +350,58 @@ struct Wave {
           }
       } else if constexpr (T == kCacheE2m1) {
         // A lane's quarter of a row has one scale, which goes into the conversion.
-        const uint8_t* units = reinterpret_cast<const uint8_t*>(Kst + 4 * S::kPageSlots) + l16 * 4 + q4;
+        const uint8_t* units = reinterpret_cast<const uint8_t*>(Kst + S::kScales) + l16 * (kPair ? 8 : 4) + q4;
+        uint32_t c[2][D / 32];
+        float unit[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float unit = __uint_as_float(static_cast<uint32_t>(units[h * kPage * 4]) << 23);
-          uint32_t c[D / 32];
-          if constexpr (D == 128) *reinterpret_cast<u32x4*>(c) = Kst[kb0 + h * S::kPageSlots];
-          else *reinterpret_cast<u32x2*>(c) = reinterpret_cast<const u32x2*>(Kst + h * S::kPageSlots)[kb0];
-#pragma unroll
-          for (int kk = 0; kk < D / 32; ++kk)
-            sc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, e2m1_bf16(c[kk], unit)),
-                                                            __builtin_bit_cast(bf16x8, qf[kk]), sc[h], 0, 0, 0);
+        for (int h = 0; h < 2; ++h) {      // the block's pages, or the heads
+          unit[h] = __uint_as_float(static_cast<uint32_t>(units[h * (kPair ? 4 : kPage * 4)]) << 23);
+          // (A head's row is half of CH chunks, which the swizzle keeps apart from the other's by one bit.)
+          const char* at = reinterpret_cast<const char*>(Kst) + (kPair ? kb0 ^ (h * S::kRow) : kb0 + h * (S::kPageSlots * 16));
+          if constexpr (D == 128) *reinterpret_cast<u32x4*>(c[h]) = *reinterpret_cast<const u32x4*>(at);
+          else *reinterpret_cast<u32x2*>(c[h]) = *reinterpret_cast<const u32x2*>(at);
         }
+        // V, 32 dimensions at a time: a pair of lanes turns 32 codes of a row into bf16 with their
+        // scales (a transposed word would hold rows of eight scales), and they are read back
+        // transposed; the first 64 from the wave's own room, the others from the stage,
+        // where K and V have been read.  Row n: of key n, or of key n % 16 of head n / 16.
+        const int row_n = lane >> 1, half = lane & 1, swap = (row_n >> 2) & 1;
+        const int key = kPair ? row_n % kPage : row_n, head = kPair ? row_n / kPage : 0;
+        uint32_t w = reinterpret_cast<const uint32_t*>(Kst + S::kScales)[kBlk + (kPair ? 2 * key + head : key)];
+        if constexpr (kPair) {
+          // A NaN of one head's V would reach the other head through its weight of zero: such a row counts
+          // as zeros, and its head's sums become NaN.
+          const uint32_t nan = ((w & 0x7F7F7F7Fu) + 0x01010101u) & w & 0x80808080u;
+          const uint64_t rows = __builtin_amdgcn_ballot_w64(nan != 0);
+          if (rows != 0) {
+            if (nan != 0) w = 0;
+            if (second ? rows >> 32 != 0 : static_cast<uint32_t>(rows) != 0) {
+#pragma unroll
+              for (int dt = 0; dt < DT; ++dt) acc[dt] += __uint_as_float(kNanScale);
+            }
+          }
+        }
+        if constexpr (D == 64) w >>= 8 * half;
+        const u32x4* const row = Vst + key / kPage * S::kPageSlots + key % kPage * CH;
+        u32x2 vc[D / 32];
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+          vc[i] = reinterpret_cast<const u32x2*>(row + ((head * (CH / 2) + i) ^ v_slot<T, CH>(key)))[half];
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+          u32x4* const turn = i < 2 ? ring + S::kRing + i * kTurnStep : ring + stage * S::kSlots + (i - 2) * kTurnStep;
+          constexpr int kStep = D == 64 ? 16 : 8;     // bits between the scales of two steps
+          const float vu = __uint_as_float(i * kStep < 24 ? w << (23 - i * kStep) : w >> 1);
+          // (Which half goes first is such that a write falls on all banks.)
+          turn[turn_slot(row_n, 2 * half + swap)] = e2m1_bf16(swap ? vc[i].y : vc[i].x, vu);
+          turn[turn_slot(row_n, 2 * half + 1 - swap)] = e2m1_bf16(swap ? vc[i].x : vc[i].y, vu);
+        }
+#pragma unroll
+        for (int kk = 0; kk < D / 32; ++kk)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            sc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, e2m1_bf16(c[h][kk], unit[h])),
+                                                            __builtin_bit_cast(bf16x8, qf[kk]), sc[h], 0, 0, 0);
       } else {
 #pragma unroll
         for (int j = 0; j < D / 64; ++j)
@@ -344,12 +412,38 @@ struct Wave {
             sc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_bf16<T>(a.z, a.w), __builtin_bit_cast(bf16x8, qf[2 * j + 1]), sc[h], 0, 0, 0);
           }
       }
+      bf16x8 pb[3];
+      if constexpr (kPair) {
+        // Four scores, of this lane's head; they weigh its rows of V, the first or the last four
+        // that a lane holds of the operand.
+        const int nv0 = __builtin_amdgcn_readlane(keys, i);
+        float pr[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) pr[e] = (second ? sc[1][e] : sc[0][e]) * p.scale_log2;
+        if (nv0 < kPage) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (4 * q4 + e >= nv0) pr[e] = -INFINITY;
+        }
+        rescale(rows_max(fmaxf(fmaxf(pr[0], pr[1]), fmaxf(pr[2], pr[3]))));
+        const float mc = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          pr[e] = __builtin_amdgcn_exp2f(pr[e] - mc);
+          lsum += pr[e];
+        }
+#pragma unroll
+        for (int part = 0; part < 3; ++part) {
+          const uint32_t a = take_bf2(pr[0], pr[1]), b = take_bf2(pr[2], pr[3]);
+          pb[part] = __builtin_bit_cast(bf16x8, u32x4{second ? 0 : a, second ? 0 : b, second ? a : 0, second ? b : 0});
+        }
+      } else {
       float pr[8], vs[8];
       if constexpr (T == kCacheBf16 || T == kCacheE2m1) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) pr[e] = sc[e / 4][e % 4] * p.scale_log2;
       } else {
-        const f32x4* f = reinterpret_cast<const f32x4*>(Kst + 4 * S::kPageSlots);
+        const f32x4* f = reinterpret_cast<const f32x4*>(Kst + S::kScales);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const f32x4 ks = f[4 * h + q4], w = f[8 + 4 * h + q4];
@@ -370,15 +464,7 @@ struct Wave {
             if (4 * q4 + e >= (h ? nv1 : nv0)) pr[h * 4 + e] = -INFINITY;
       }
       float mx = fmaxf(fmaxf(fmaxf(pr[0], pr[1]), fmaxf(pr[2], pr[3])), fmaxf(fmaxf(pr[4], pr[5]), fmaxf(pr[6], pr[7])));
-      mx = rows_max(mx);
-      if (__builtin_amdgcn_ballot_w64(mx > m) != 0) {
-        const float m_new = fmaxf(m, mx);
-        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
-        m = m_new;
-        lsum *= alpha;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) acc[dt] *= alpha;
-      }
+      rescale(rows_max(mx));
       const float mc = m == -INFINITY ? 0.f : m;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -386,13 +472,13 @@ struct Wave {
         lsum += pr[e];
         if constexpr (T == kCacheE4m3 || T == kCacheInt8) pr[e] *= vs[e];
       }
-      bf16x8 pb[3];
 #pragma unroll
       for (int part = 0; part < 3; ++part) {
         u32x4 w;
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] = take_bf2(pr[2 * e], pr[2 * e + 1]);
         pb[part] = __builtin_bit_cast(bf16x8, w);
+      }
       }
       const uint32_t vst = vb0 + static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)Vst));
       if constexpr (T == kCacheBf16) {
@@ -405,29 +491,14 @@ struct Wave {
           for (int part = 2; part >= 0; --part)
             acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va[dt]), pb[part], acc[dt], 0, 0, 0);
       } else if constexpr (T == kCacheE2m1) {
-        // 32 dimensions at a time: a pair of lanes turns 32 codes of a key into bf16, with
-        // their scales (a transposed word would hold keys of eight scales), and they are read
-        // back transposed.
-        const int key = lane >> 1, half = lane & 1;
-        const uint32_t w = reinterpret_cast<const uint32_t*>(Kst + 4 * S::kPageSlots)[kBlk + key] >> (D == 64 ? 8 * half : 0);
-        const u32x4* const row = Vst + key / kPage * S::kPageSlots + key % kPage * CH;
-        u32x4* const turn = ring + S::kRing;
-        const uint32_t vt = vb0 + static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)turn));
+        u32x4 va[DT];
+        read_turned4(vb0 + static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)(ring + S::kRing))), va);
+        if constexpr (D == 128) read_turned4(vb0 + static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)Kst)), va + 4);
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-          const u32x2 c = reinterpret_cast<const u32x2*>(row + (i ^ v_slot<T, CH>(key)))[half];
-          constexpr int kStep = D == 64 ? 16 : 8;     // bits between the scales of two steps
-          const float unit = __uint_as_float(i * kStep < 24 ? w << (23 - i * kStep) : w >> 1);
-          turn[turn_slot(key, 2 * half)] = e2m1_bf16(c.x, unit);
-          turn[turn_slot(key, 2 * half + 1)] = e2m1_bf16(c.y, unit);
-          u32x4 va[2];
-          read_pv2(vt, va);
+        for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-          for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int part = 2; part >= 0; --part)
-              acc[2 * i + t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va[t]), pb[part], acc[2 * i + t], 0, 0, 0);
-        }
+          for (int part = 2; part >= 0; --part)
+            acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va[dt]), pb[part], acc[dt], 0, 0, 0);
       } else {
         u32x2 vc[DT];
 #pragma unroll
@@ -467,9 +538,9 @@ __device__ __forceinline__ int wave_prefix(int v) {
   return v;
 }
 
-template <int D, CacheType T, bool kListed>
+template <int D, CacheType T, bool kListed, bool kPair>
 __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, int groups, int head_shift) {
-  using S = Shape<D, T>;
+  using S = Shape<D, T, kPair>;
   constexpr int DT = D / 16;
   // One array: with several, the compiler's alias scopes make LDS reads of a
   // stage wait for the loads in flight into the other.
@@ -482,18 +553,19 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
   // are not a multiple), whose rows are neighbours in memory and share scale lines and table
   // entries; workgroups of one blockIdx.x, the range's other heads, go to one XCD.  (64
   // sequences E4M3, first launch: 62 us; 65 to 72 with four ranges of one head.)
-  const int head = (static_cast<int>(blockIdx.y) << head_shift) + (wave & ((1 << head_shift) - 1));
+  // (kPair: they take the steps of one range in turn, and merge what they have of a sequence.)
+  const int head = kPair ? static_cast<int>(blockIdx.y) : (static_cast<int>(blockIdx.y) << head_shift) + (wave & ((1 << head_shift) - 1));
   const int kh = groups == 1 ? head : head / groups, group = head - kh * groups;
-  const int r0 = static_cast<int>(blockIdx.x) * (kWaves >> head_shift) + (wave >> head_shift);
+  const int r0 = kPair ? static_cast<int>(blockIdx.x) : static_cast<int>(blockIdx.x) * (kWaves >> head_shift) + (wave >> head_shift);
   if (r0 >= p.ranges) return;
   // One sequence: the pages of this range, were it of one block (lanes 0, 1) or of two
   // (lanes 8 to 11), are read beside the length (a short call is a chain of loads).
   int ahead = 0;
-  if (!kListed && p.seqs == 1) ahead = p.bt[min(lane < 8 ? 2 * r0 + lane : 4 * r0 + lane - 8, p.max_pages - 1)];
+  if (!kListed && !kPair && p.seqs == 1) ahead = p.bt[min(lane < 8 ? 2 * r0 + lane : 4 * r0 + lane - 8, p.max_pages - 1)];
   int win = 0, lens = lane_length<kListed>(p, 0);        // lens: of sequences [win, win + 64)
 
-  const int h0 = kh * p.G + group * kAttendGroup, nh = min(kAttendGroup, p.G - group * kAttendGroup);
-  Wave<D, T, kListed ? 1 : 0> w;
+  const int h0 = kPair ? 2 * kh * p.G : kh * p.G + group * kAttendGroup, nh = kPair ? 2 * p.G : min(kAttendGroup, p.G - group * kAttendGroup);
+  Wave<D, T, kPair, kListed ? 1 : 0> w;
   w.init(p, kh, lds + wave * S::kWaveSlots);
 
   // All blocks of the call, and the ranges they make.  coarse: blocks of the first (lane +
@@ -511,7 +583,7 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
     coarse = wave_prefix(sum);
   }
   const int total = __builtin_amdgcn_readlane(coarse, 63);
-  const int each = attend_blocks(total, p.seqs, p.ranges);
+  const int each = attend_blocks(total, p.seqs, p.ranges, kPair ? kWaves * kAttendMaxBlocks : kAttendMaxBlocks);
   auto window = [&](int s) {                    // makes s one of the 64
     if (s >= win && s < win + 64) return;
     win = s & ~63;
@@ -549,6 +621,8 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
     }
   };
 
+  // Steps that a wave takes of the first `blocks` of a range.
+  auto steps = [&](int blocks) { return kPair ? (2 * blocks - wave + kWaves - 1) / kWaves : blocks; };
   for (int r = r0; r * each < total; r += p.ranges) {
     const int f0 = r * each, f1 = min(f0 + each, total), blocks = f1 - f0;
     seek(f0);
@@ -556,13 +630,14 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
     w.load_q(p, s, h0, nh, w.qf);
     // Pages of the range's blocks.
     w.page = w.keys = 0;
-    const int f = f0 + lane / 2;
+    const int nth = kPair ? kWaves * lane + wave : lane;      // this lane's page, of the range's
+    const int f = f0 + nth / 2;
     int from = 0, key0 = -1;
     for (const int s0 = s, base0 = base;;) {
       const int len = length(s), nb = blocks_of(len);
       if (f >= base && f < base + nb && f < f1) {
         from = s;
-        key0 = ((f - base) * 2 + lane % 2) * kPage;
+        key0 = ((f - base) * 2 + nth % 2) * kPage;
         w.keys = min(max(len - key0, 0), kPage);
       }
       base += nb;
@@ -584,19 +659,19 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
       }
     }
     if (w.keys > 0) {
-      w.page = !kListed && p.seqs == 1 && each <= 2 ? ahead : p.bt[int64_t(from) * p.max_pages + key0 / kPage];
+      w.page = !kListed && !kPair && p.seqs == 1 && each <= 2 ? ahead : p.bt[int64_t(from) * p.max_pages + key0 / kPage];
       if (w.page < 0 || w.page >= p.num_pages) {
         w.page = w.keys = 0;
         if (p.err && (kListed || head == 0)) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
       }
     }
 #pragma unroll
-    for (int i = 0; i < kStages; ++i) w.issue(p, i, i < blocks, i);
+    for (int i = 0; i < S::kStages; ++i) w.issue(p, i, i < steps(blocks), i);
     w.await_q();
     w.await_block();
     w.begin();
-    for (int i = 0;;) {
-      const int cur = s, at = f0 + i - base, end = base + blocks_of(length(s));     // at: the sequence's block at i
+    for (int i = 0, done = 0;;) {
+      const int cur = s, at = f0 + done - base, end = base + blocks_of(length(s));     // at: the sequence's block at i
       const int stop = min(blocks, end - f0);
       // The next sequence that has keys, and its query, are there when this one ends (us;
       // found and read after it, 1000 rows of 100 keys E4M3 57 (60), 200 of 700 bf16 34.1
@@ -607,13 +682,51 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
         more = s < p.seqs;
       }
       w.load_q(p, more ? s : cur, h0, nh, w.qn);
-      w.stream(p, i, stop, blocks);
+      if (!kPair || i < steps(stop)) w.stream(p, i, steps(stop), steps(blocks));
+      done = stop;
 #pragma unroll
       for (int kk = 0; kk < D / 32; ++kk) w.qf[kk] = w.qn[kk];
       w.await_q();
       const float l = rows_sum(w.lsum);
       const bool whole = at == 0 && end <= f1;
-      if (l16 < nh) {
+      if constexpr (kPair) {
+        // The waves' parts, 64 dimensions at a time through where V is turned: a head's sixteen
+        // 16-byte chunks, chunk c in slot c XOR head.
+        u32x4* const mine = w.ring + S::kRing;
+        if (q4 == 0) reinterpret_cast<f32x2*>(mine + S::kTurn)[l16] = f32x2{w.m, l};
+#pragma unroll
+        for (int d0 = 0; d0 < DT; d0 += 4) {
+#pragma unroll
+          for (int dt = 0; dt < 4; ++dt) mine[l16 * 16 + ((4 * dt + q4) ^ l16)] = __builtin_bit_cast(u32x4, w.acc[d0 + dt]);
+          asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+          const int g = static_cast<int>(threadIdx.x) / 16, c = threadIdx.x % 16;
+          f32x2 ml[kWaves];
+          float top = -INFINITY, sum = 0.f;
+          f32x4 o{};
+#pragma unroll
+          for (int n = 0; n < kWaves; ++n) {
+            ml[n] = reinterpret_cast<const f32x2*>(lds + n * S::kWaveSlots + S::kRing + S::kTurn)[g];
+            top = fmaxf(top, ml[n].x);
+          }
+#pragma unroll
+          for (int n = 0; n < kWaves; ++n) {
+            const float f = join_weight(ml[n].x, ml[n].y, top);
+            sum += f * ml[n].y;
+            o += f * __builtin_bit_cast(f32x4, lds[n * S::kWaveSlots + S::kRing + g * 16 + (c ^ g)]);
+          }
+          asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+          const int d = 16 * d0 + 4 * c;
+          if (g < nh) {
+            if (whole) {
+              write_row(p, cur, h0 + g, d, o, top, sum);
+            } else {
+              const int64_t rec = (int64_t(r) + cur) * p.Hq + h0 + g;
+              __builtin_nontemporal_store(o, reinterpret_cast<f32x4*>(p.part_o + rec * D + d));
+              if (d == 0) *reinterpret_cast<f32x2*>(p.part_ml + rec * 2) = f32x2{top, sum};
+            }
+          }
+        }
+      } else if (l16 < nh) {
         if (whole) {
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt) write_row(p, cur, h0 + l16, 16 * dt + 4 * q4, w.acc[dt], w.m, l);
@@ -625,7 +738,7 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
           if (q4 == 0) *reinterpret_cast<f32x2*>(p.part_ml + rec * 2) = f32x2{w.m, l};
         }
       }
-      if (at == 0 && head == 0 && lane == 0) {
+      if (at == 0 && head == 0 && lane == 0 && (!kPair || wave == 0)) {
         // The row's records: none, or from here to the range of its last block.
         reinterpret_cast<int2*>(p.parts)[cur] = int2{r, whole ? 0 : (end - 1) / each - r + 1};
       }
@@ -641,7 +754,7 @@ __global__ __launch_bounds__(kBoundThreads) void attend_kernel(AttendParams p, i
 // them through LDS.  A row of one split is written as it is (short rows: one launch).
 template <int D, CacheType T, int kWaves, bool kListed>
 __global__ __launch_bounds__(kBoundThreads) void attend_split_kernel(AttendParams p, int groups, int splits, int per) {
-  using S = Shape<D, T>;
+  using S = Shape<D, T, false>;
   constexpr int DT = D / 16;
   __shared__ __attribute__((aligned(256))) u32x4 lds[kWaves * S::kWaveSlots];
   const int lane = threadIdx.x & 63, q4 = lane >> 4, l16 = lane & 15;
@@ -665,7 +778,7 @@ __global__ __launch_bounds__(kBoundThreads) void attend_split_kernel(AttendParam
   int page;
   if constexpr (kListed) page = p.lists[(int64_t(s) * p.Hkv + kh) * p.listed + min(2 * f0 + lane, p.listed - 1)];
   else page = p.bt[int64_t(s) * p.max_pages + min(2 * f0 + lane, p.max_pages - 1)];
-  Wave<D, T, kListed ? kWaves + 1 : kWaves> w;
+  Wave<D, T, false, kListed ? kWaves + 1 : kWaves> w;
   w.load_q(p, s, h0, nh, w.qf);
   const int len = row_length(p, s);
   w.init(p, kh, lds + wave * S::kWaveSlots);
@@ -688,7 +801,7 @@ __global__ __launch_bounds__(kBoundThreads) void attend_split_kernel(AttendParam
   w.keys = __shfl(bad ? 0 : keys, 2 * b0 + lane, 64);
   w.page = __shfl(page, 2 * b0 + lane, 64);
 #pragma unroll
-  for (int i = 0; i < kStages; ++i) w.issue(p, i, i < blocks, i);
+  for (int i = 0; i < S::kStages; ++i) w.issue(p, i, i < blocks, i);
   w.await_q();
   w.await_block();
   w.begin();
@@ -838,6 +951,15 @@ constexpr int kShortKeys = 512;
 constexpr int kShortGroups = 1536;
 constexpr int kSplitBlocks = 2;
 
+template <int D, CacheType T, bool kListed, bool kPair>
+void launch_ranges(const AttendParams& p, int groups, int heads, hipStream_t s) {
+  if constexpr (!kPair || (T == kCacheE2m1 && !kListed)) {
+    const int head_shift = kPair ? 0 : heads % 4 == 0 ? 2 : heads % 2 == 0 ? 1 : 0;
+    const int per = kPair ? 1 : kWaves >> head_shift;         // ranges of a workgroup
+    attend_kernel<D, T, kListed, kPair><<<dim3((p.ranges + per - 1) / per, heads >> head_shift), kWaves * 64, 0, s>>>(p, groups, head_shift);
+  }
+}
+
 template <int D, CacheType T, bool kListed>
 hipError_t launch(const AttendParams& p, hipStream_t s) {
   const int groups = (p.G + kAttendGroup - 1) / kAttendGroup, heads = p.Hkv * groups;
@@ -851,9 +973,8 @@ hipError_t launch(const AttendParams& p, hipStream_t s) {
     const int per = kFill * each, splits = (most + per - 1) / per;
     if (rows * splits <= 256) return launch_split<D, T, kFill, kListed>(p, groups, splits, per, s);
   }
-  const int head_shift = heads % 4 == 0 ? 2 : heads % 2 == 0 ? 1 : 0;
-  const int per = kWaves >> head_shift;         // ranges of a workgroup
-  attend_kernel<D, T, kListed><<<dim3((p.ranges + per - 1) / per, heads >> head_shift), kWaves * 64, 0, s>>>(p, groups, head_shift);
+  if (T == kCacheE2m1 && attend_pairs(T, p.Hq, p.Hkv, kListed)) launch_ranges<D, T, kListed, true>(p, 1, p.Hkv / 2, s);
+  else launch_ranges<D, T, kListed, false>(p, groups, heads, s);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   return launch_join<D>(p, p.ranges / p.seqs < kJoinBatch * 256 / D ? 0 : attend_row_records(most, p.seqs, p.ranges), s);
 }

@@ -187,9 +187,15 @@ AttendSpace attend_space(int64_t seqs, int Hq, int d, int max_length, int ranges
   const size_t o_at = (seqs * 8 + 255) / 256 * 256, ml_at = o_at + size_t(records) * Hq * d * 4;
   return {int(records), o_at, ml_at, (ml_at + size_t(records) * Hq * 8 + 255) / 256 * 256};
 }
+int attend_ranges(pallas::CacheType t, int Hq, int Hkv, int d, bool listed) {
+  if (pallas::attend_pairs(t, Hq, Hkv, listed)) return pallas::attend_ranges(pallas::kAttendPairGroups, Hkv / 2);
+  return pallas::attend_ranges(pallas::attend_waves(t, d), pallas::attend_heads(Hq, Hkv));
+}
 int most_ranges(int Hq, int Hkv, int d) {
-  const int waves = std::max(pallas::attend_waves(pallas::kCacheE4m3, d), pallas::attend_waves(pallas::kCacheE2m1, d));
-  return pallas::attend_ranges(waves, pallas::attend_heads(Hq, Hkv));
+  int most = 0;
+  for (pallas::CacheType t : {pallas::kCacheE4m3, pallas::kCacheE2m1})
+    for (bool listed : {false, true}) most = std::max(most, attend_ranges(t, Hq, Hkv, d, listed));
+  return most;
 }
 
 int check_attend(int32_t num_seqs, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_length,
@@ -258,7 +264,7 @@ int attend_call(const char* what, pallas::CacheType type, pallas::AttendParams& 
   p.out = static_cast<uint16_t*>(d_out);
   p.out_stride = out_stride;
   p.lse = d_lse;
-  p.ranges = pallas::attend_ranges(pallas::attend_waves(type, p.d), pallas::attend_heads(n_q_heads, p.Hkv));
+  p.ranges = attend_ranges(type, n_q_heads, p.Hkv, p.d, lists.listed);
   p.records = sp.records;
   char* ws = static_cast<char*>(d_workspace);
   p.parts = reinterpret_cast<int32_t*>(ws);

@@ -441,11 +441,18 @@ constexpr int kAttendBlock = 32;         // keys per block
 constexpr int kAttendGroup = 16;         // query heads that share one pass over a KV head
 // Blocks of a wave's range: at most one per pair of lanes.
 constexpr int kAttendMaxBlocks = 32;
+// 4-bit rows of two neighbouring KV heads share 128-byte lines (of four, for 64 dimensions): a
+// wave takes both where their query heads fit into one pass and they attend to the same keys.
+constexpr bool attend_pairs(CacheType type, int Hq, int Hkv, bool listed) {
+  return type == kCacheE2m1 && !listed && Hkv % 2 == 0 && 2 * (Hq / Hkv) <= 16;
+}
 // Waves that a CU holds: each has a ring of two stages of 32 K and V rows, 128 KiB in all,
 // and with 4-bit rows room to turn V besides.
 constexpr int attend_waves(CacheType type, int d) {
   return type == kCacheE2m1 ? 12 : 1024 / (type == kCacheBf16 ? 2 * d : d);
 }
+// Where pairs are taken the four waves of a workgroup share a range.
+constexpr int kAttendPairGroups = 3;      // workgroups that a CU holds
 // Ranges that run at once: a multiple of 8 (one XCD each in turn), at least 8.
 inline int attend_ranges(int waves, int64_t heads) {
   return int(std::max<int64_t>(256 * waves / heads / 8 * 8, 8));
@@ -458,10 +465,10 @@ inline int64_t attend_heads(int Hq, int Hkv) { return int64_t(Hkv) * ((Hq / Hkv 
 // us: 27 rows of 30 to 2000 keys 8.4, 9.2; 1 row of 4000 keys, in ranges, 13.7, 12.4: more
 // records to join).
 constexpr int kAttendShort = 32;         // blocks of a row
-__host__ __device__ inline int attend_blocks(int total, int seqs, int ranges) {
+__host__ __device__ inline int attend_blocks(int total, int seqs, int ranges, int per_range = kAttendMaxBlocks) {
   if (2 * int64_t(total) <= ranges && total <= int64_t(kAttendShort) * seqs) return 1;
   if (total <= 2 * ranges) return 2;
-  const uint32_t most = uint32_t(kAttendMaxBlocks) * ranges;             // total <= 2^30, most <= 2^17
+  const uint32_t most = uint32_t(per_range) * ranges;             // total <= 2^30, most <= 2^17
   const uint32_t rounds = std::max((total + most - 1) / most, 1u), all = rounds * ranges;
   return int((total + all - 1) / all);
 }
