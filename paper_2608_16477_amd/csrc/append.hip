@@ -19,6 +19,9 @@ namespace {
 constexpr int kThreads = 256;   // at most
 constexpr int kPage = 16;
 constexpr int kBf16 = 0;        // a cache of bf16 rows, beside the pallas_quant_formats
+// bf16 rows of this many bytes are stored non-temporally (3000 tokens of 72 heads: 23 us, 33 with
+// plain stores); fewer stay in the caches for what reads them next.
+constexpr int64_t kNtStoreBytes = int64_t(4) << 20;
 
 // (cos, sin) of an angle of `a` 2^-64 turns, times m.  What is left of a quarter, |x| <= pi / 4,
 // goes through Taylor's polynomials; the first terms left out are below 2^-53 (sine, x^17 / 17!)
@@ -82,11 +85,16 @@ __device__ __forceinline__ void read_pairs(const uint16_t* x, const Place& at, u
     }
   }
 }
-template <bool kFast>
+template <bool kNt, class V>
+__device__ __forceinline__ void put(V v, void* at) {
+  if constexpr (kNt) __builtin_nontemporal_store(v, static_cast<V*>(at));
+  else *static_cast<V*>(at) = v;
+}
+template <bool kFast, bool kNt>
 __device__ __forceinline__ void write_pairs(uint16_t* y, const Place& at, const uint32_t (&w)[4]) {
   if constexpr (kFast) {
-    *reinterpret_cast<u32x2*>(y + at.lo[0]) = u32x2{w[0], w[1]};
-    *reinterpret_cast<u32x2*>(y + at.hi[0]) = u32x2{w[2], w[3]};
+    put<kNt>(u32x2{w[0], w[1]}, y + at.lo[0]);
+    put<kNt>(u32x2{w[2], w[3]}, y + at.hi[0]);
   } else {
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
@@ -97,105 +105,137 @@ __device__ __forceinline__ void write_pairs(uint16_t* y, const Place& at, const 
 }
 
 // D / 8 lanes take a head; `slots` heads of a token go side by side (several tokens where a
-// token has fewer), in the order Q, K, V.  A lane keeps its four angles for all the heads
-// that it takes.
-template <int D, int kFormat, bool kFast>
+// token has fewer), in the order Q, K, V, kPasses times with their loads in flight together.
+// The workgroup works out the angles of its tokens once, each a thread's, while the first loads
+// are on their way.
+template <int D, int kFormat, bool kFast, bool kNt>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams p, int slots, int tokens_per, int heads_per) {
-  constexpr int kLanes = D / 8;
+  constexpr int kLanes = D / 8, kMost = kThreads / kLanes, kPasses = 3;
+  struct Turn {
+    double c, s;
+  };
+  __shared__ __attribute__((aligned(16))) Turn turns[kMost / 2 * (D / 2)];      // (at least two heads a token)
   __shared__ __attribute__((aligned(16))) uint16_t turned[kFormat == kBf16 ? 8 : kThreads * 8];   // a head's place: its lanes' 16 bytes
   const int j = threadIdx.x % kLanes, slot = threadIdx.x / kLanes;
   const int heads = p.Hq + 2 * p.Hkv;
-  const int t = blockIdx.x * tokens_per + (tokens_per > 1 ? slot / heads : 0);
+  const int t0 = blockIdx.x * tokens_per, mine = tokens_per > 1 ? slot / heads : 0, t = t0 + mine;
   int h = tokens_per > 1 ? slot % heads : slot + blockIdx.y * heads_per;
-  const int h1 = tokens_per > 1 ? heads : min(heads, static_cast<int>(blockIdx.y + 1) * heads_per);
-  if (slot >= (tokens_per > 1 ? tokens_per * heads : slots) || t >= p.tokens || h >= h1) return;
-  const int pos = p.pos[t], seq = p.seq ? p.seq[t] : t;
-  if (pos < 0) return;      // padding
+  int h1 = tokens_per > 1 ? heads : min(heads, static_cast<int>(blockIdx.y + 1) * heads_per);
+  if (slot >= (tokens_per > 1 ? tokens_per * heads : slots) || t >= p.tokens) h1 = h;      // (nothing, but the angles)
+  const int pos = p.pos[min(t, p.tokens - 1)];
+  if (pos < 0) h1 = h;      // padding
+  const Place at = place_of<kFast>(p, j);
+  uint32_t w[kPasses][4];
+  auto read = [&] {
+#pragma unroll
+    for (int k = 0; k < kPasses; ++k) {
+      const int hk = h + k * slots;
+      if (hk >= h1) continue;
+      if (hk >= p.Hq + p.Hkv) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(p.v + t * p.v_stride + (hk - p.Hq - p.Hkv) * D + j * 8);
+        w[k][0] = x.x, w[k][1] = x.y, w[k][2] = x.z, w[k][3] = x.w;
+      } else {
+        read_pairs<kFast>(hk < p.Hq ? p.q + t * p.q_stride + hk * D : p.k + t * p.k_stride + (hk - p.Hq) * D, at, w[k]);
+      }
+    }
+  };
+  read();
   int64_t row = -1;         // the token's first K row in its page slot, among the rows of both planes
-  {
+  if (h < h1) {
+    const int seq = p.seq ? p.seq[t] : t;
     int pg = -1;
     if (seq >= 0 && seq < p.seqs && pos / kPage < p.max_pages) pg = p.bt[static_cast<int64_t>(seq) * p.max_pages + pos / kPage];
     if (pg >= 0 && pg < p.num_pages) row = (static_cast<int64_t>(pg) * kPage + pos % kPage) * p.Hkv;
   }
-  const Place at = place_of<kFast>(p, j);
+  const int pairs = p.r / 2;
+  for (int i = threadIdx.x; i < tokens_per * pairs; i += blockDim.x) {
+    const int of = tokens_per > 1 ? i / pairs : 0, u = i - of * pairs;
+    const int64_t at_pos = tokens_per > 1 ? p.pos[min(t0 + of, p.tokens - 1)] : pos;
+    turn_cos_sin64(static_cast<uint64_t>(at_pos) * p.turns[u], p.magnitude, turns[of * (D / 2) + u].c, turns[of * (D / 2) + u].s);
+  }
+  __syncthreads();
+  if (h >= h1) return;
   double c[4], s[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const int u = 4 * j + e;
-    c[e] = 1.0, s[e] = 0.0;
-    if (2 * u < p.r) turn_cos_sin64(static_cast<uint64_t>(static_cast<int64_t>(pos)) * p.turns[u], p.magnitude, c[e], s[e]);
+    const Turn n = turns[mine * (D / 2) + min(u, pairs - 1)];
+    c[e] = n.c, s[e] = n.s;
   }
-  for (; h < h1; h += slots) {
-    const bool q = h < p.Hq, v = h >= p.Hq + p.Hkv;
-    const int hh = q ? h : v ? h - p.Hq - p.Hkv : h - p.Hq;
-    if (!q && row < 0) {
-      if (h == p.Hq && j == 0 && p.err) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
-      continue;
-    }
-    uint32_t w[4];
-    if (v) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(p.v + t * p.v_stride + hh * D + j * 8);
-      w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
-    } else {
-      read_pairs<kFast>((q ? p.q + t * p.q_stride : p.k + t * p.k_stride) + hh * D, at, w);
-      // w: first elements of the pairs, then second ones (fast, neighbours: pairs 0, 1 and 2, 3)
-      const bool beside = kFast && (p.interleaved || 8 * j >= p.r);
-      float y[8];
+  for (;;) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t wa = beside ? w[e] : w[e / 2] >> (16 * (e % 2)), wb = beside ? w[e] >> 16 : w[2 + e / 2] >> (16 * (e % 2));
-        const double x0 = bflo(wa), x1 = bflo(wb);
-        y[e] = static_cast<float>(__builtin_fma(x0, c[e], -(x1 * s[e])));
-        y[4 + e] = static_cast<float>(__builtin_fma(x1, c[e], x0 * s[e]));
+    for (int k = 0; k < kPasses; ++k) {
+      const int hk = h + k * slots;
+      if (hk >= h1) continue;
+      const bool q = hk < p.Hq, v = hk >= p.Hq + p.Hkv;
+      const int hh = q ? hk : v ? hk - p.Hq - p.Hkv : hk - p.Hq;
+      if (!q && row < 0) {
+        if (hk == p.Hq && j == 0 && p.err) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
+        continue;
       }
-      // (Elements behind the turned ones are copied, whatever their bits.)
-      uint32_t n[4];
-      if (beside) {
+      if (!v) {
+        // w: first elements of the pairs, then second ones (fast, neighbours: pairs 0, 1 and 2, 3)
+        const bool beside = kFast && (p.interleaved || 8 * j >= p.r);
+        float y[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) n[e] = pack_bf2(y[e], y[4 + e]);
-      } else {
-        n[0] = pack_bf2(y[0], y[1]), n[1] = pack_bf2(y[2], y[3]), n[2] = pack_bf2(y[4], y[5]), n[3] = pack_bf2(y[6], y[7]);
-      }
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t wa = beside ? w[k][e] : w[k][e / 2] >> (16 * (e % 2)), wb = beside ? w[k][e] >> 16 : w[k][2 + e / 2] >> (16 * (e % 2));
+          const double x0 = bflo(wa), x1 = bflo(wb);
+          y[e] = static_cast<float>(__builtin_fma(x0, c[e], -(x1 * s[e])));
+          y[4 + e] = static_cast<float>(__builtin_fma(x1, c[e], x0 * s[e]));
+        }
+        uint32_t n[4];
+        if (beside) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if constexpr (kFast) {
-          w[e] = 8 * j < p.r ? n[e] : w[e];
+          for (int e = 0; e < 4; ++e) n[e] = pack_bf2(y[e], y[4 + e]);
         } else {
-          const int u = 4 * j + 2 * (e % 2);      // pairs u and u + 1 in the halves of this word
-          w[e] = (2 * u < p.r ? n[e] & 0xFFFFu : w[e] & 0xFFFFu) | (2 * u + 2 < p.r ? n[e] & 0xFFFF0000u : w[e] & 0xFFFF0000u);
+          n[0] = pack_bf2(y[0], y[1]), n[1] = pack_bf2(y[2], y[3]), n[2] = pack_bf2(y[4], y[5]), n[3] = pack_bf2(y[6], y[7]);
+        }
+        // (Elements behind the turned ones are copied, whatever their bits.)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (kFast) {
+            w[k][e] = 8 * j < p.r ? n[e] : w[k][e];
+          } else {
+            const int u = 4 * j + 2 * (e % 2);      // pairs u and u + 1 in the halves of this word
+            w[k][e] = (2 * u < p.r ? n[e] & 0xFFFFu : w[k][e] & 0xFFFFu) | (2 * u + 2 < p.r ? n[e] & 0xFFFF0000u : w[k][e] & 0xFFFF0000u);
+          }
+        }
+      }
+      const int64_t to = row + hh + (v ? static_cast<int64_t>(p.num_pages) * kPage * p.Hkv : 0);
+      if (q) {
+        write_pairs<kFast, kNt>(p.q_out + t * p.q_out_stride + hh * D, at, w[k]);
+      } else if constexpr (kFormat == kBf16) {
+        uint16_t* y = static_cast<uint16_t*>(p.cache) + to * D;
+        if (v) put<kNt>(u32x4{w[k][0], w[k][1], w[k][2], w[k][3]}, y + j * 8);
+        else write_pairs<kFast, kNt>(y, at, w[k]);
+      } else {
+        if (!v) {
+          // Into the row's order, through LDS (a row's lanes are of one wave).
+          uint16_t* y = turned + threadIdx.x / kLanes * D;
+          write_pairs<kFast, false>(y, at, w[k]);
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          __builtin_amdgcn_wave_barrier();
+          const u32x4 x = *reinterpret_cast<const u32x4*>(y + j * 8);
+          w[k][0] = x.x, w[k][1] = x.y, w[k][2] = x.z, w[k][3] = x.w;
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          __builtin_amdgcn_wave_barrier();
+        }
+        const RowCodes<8> codes = quantise_row<kFormat, D, 8>(w[k]);
+        uint8_t* cache = static_cast<uint8_t*>(p.cache);
+        if constexpr (kFormat == PALLAS_QUANT_E2M1) {
+          constexpr int kGroup = D / 32;      // lanes of a quarter
+          *reinterpret_cast<uint32_t*>(cache + to * (D / 2) + j * 4) = codes.codes[0];
+          if (j % kGroup == 0) reinterpret_cast<uint8_t*>(p.scales)[to * 4 + j / kGroup] = static_cast<uint8_t>(codes.scale);
+        } else {
+          *reinterpret_cast<u32x2*>(cache + to * D + j * 8) = u32x2{codes.codes[0], codes.codes[1]};
+          if (j == 0) p.scales[to] = __uint_as_float(codes.scale);
         }
       }
     }
-    const int64_t to = row + hh + (v ? static_cast<int64_t>(p.num_pages) * kPage * p.Hkv : 0);
-    if (q) {
-      write_pairs<kFast>(p.q_out + t * p.q_out_stride + hh * D, at, w);
-    } else if constexpr (kFormat == kBf16) {
-      uint16_t* y = static_cast<uint16_t*>(p.cache) + to * D;
-      if (v) *reinterpret_cast<u32x4*>(y + j * 8) = u32x4{w[0], w[1], w[2], w[3]};
-      else write_pairs<kFast>(y, at, w);
-    } else {
-      if (!v) {
-        // Into the row's order, through LDS (a row's lanes are of one wave).
-        uint16_t* y = turned + threadIdx.x / kLanes * D;
-        write_pairs<kFast>(y, at, w);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        const u32x4 x = *reinterpret_cast<const u32x4*>(y + j * 8);
-        w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-      }
-      const RowCodes<8> codes = quantise_row<kFormat, D, 8>(w);
-      uint8_t* cache = static_cast<uint8_t*>(p.cache);
-      if constexpr (kFormat == PALLAS_QUANT_E2M1) {
-        constexpr int kGroup = D / 32;      // lanes of a quarter
-        *reinterpret_cast<uint32_t*>(cache + to * (D / 2) + j * 4) = codes.codes[0];
-        if (j % kGroup == 0) reinterpret_cast<uint8_t*>(p.scales)[to * 4 + j / kGroup] = static_cast<uint8_t>(codes.scale);
-      } else {
-        *reinterpret_cast<u32x2*>(cache + to * D + j * 8) = u32x2{codes.codes[0], codes.codes[1]};
-        if (j == 0) p.scales[to] = __uint_as_float(codes.scale);
-      }
-    }
+    h += kPasses * slots;
+    if (h >= h1) return;
+    read();
   }
 }
 
@@ -210,8 +250,9 @@ void launch(const AppendParams& p, hipStream_t s) {
   const int heads_per = p.tokens < 512 ? slots : heads;
   const dim3 grid((p.tokens + tokens_per - 1) / tokens_per, tokens_per > 1 ? 1 : (heads + heads_per - 1) / heads_per);
   const int threads = (D / 8 * slots + 63) / 64 * 64;
-  if (p.r % 8 == 0) append_kernel<D, kFormat, true><<<grid, threads, 0, s>>>(p, slots, tokens_per, heads_per);
-  else append_kernel<D, kFormat, false><<<grid, threads, 0, s>>>(p, slots, tokens_per, heads_per);
+  if (p.r % 8 != 0) append_kernel<D, kFormat, false, false><<<grid, threads, 0, s>>>(p, slots, tokens_per, heads_per);
+  else if (int64_t(p.tokens) * (p.Hq + p.Hkv) * D * 2 >= kNtStoreBytes) append_kernel<D, kFormat, true, true><<<grid, threads, 0, s>>>(p, slots, tokens_per, heads_per);
+  else append_kernel<D, kFormat, true, false><<<grid, threads, 0, s>>>(p, slots, tokens_per, heads_per);
 }
 
 template <int D>
