@@ -105,12 +105,13 @@ __device__ __forceinline__ void write_pairs(uint16_t* y, const Place& at, const 
 }
 
 // D / 8 lanes take a head; `slots` heads of a token go side by side (several tokens where a
-// token has fewer), in the order Q, K, V, kPasses times with their loads in flight together.
-// The workgroup works out the angles of its tokens once, each a thread's, while the first loads
-// are on their way.
+// token has fewer), in the order Q, K, V.  The workgroup works out the angles of its tokens once,
+// each a thread's, while the first loads are on their way.  (Three heads of a lane in flight
+// together, as in rope.hip, cost the chip's waves their registers: 12,000 tokens of 80 heads 99 us, 93;
+// 4000 of 48 21, 18.)
 template <int D, int kFormat, bool kFast, bool kNt>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams p, int slots, int tokens_per, int heads_per) {
-  constexpr int kLanes = D / 8, kMost = kThreads / kLanes, kPasses = 3;
+  constexpr int kLanes = D / 8, kMost = kThreads / kLanes;
   struct Turn {
     double c, s;
   };
@@ -125,21 +126,16 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams p, int sl
   const int pos = p.pos[min(t, p.tokens - 1)];
   if (pos < 0) h1 = h;      // padding
   const Place at = place_of<kFast>(p, j);
-  uint32_t w[kPasses][4];
+  uint32_t w[4];
   auto read = [&] {
-#pragma unroll
-    for (int k = 0; k < kPasses; ++k) {
-      const int hk = h + k * slots;
-      if (hk >= h1) continue;
-      if (hk >= p.Hq + p.Hkv) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(p.v + t * p.v_stride + (hk - p.Hq - p.Hkv) * D + j * 8);
-        w[k][0] = x.x, w[k][1] = x.y, w[k][2] = x.z, w[k][3] = x.w;
-      } else {
-        read_pairs<kFast>(hk < p.Hq ? p.q + t * p.q_stride + hk * D : p.k + t * p.k_stride + (hk - p.Hq) * D, at, w[k]);
-      }
+    if (h >= p.Hq + p.Hkv) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(p.v + t * p.v_stride + (h - p.Hq - p.Hkv) * D + j * 8);
+      w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+    } else {
+      read_pairs<kFast>(h < p.Hq ? p.q + t * p.q_stride + h * D : p.k + t * p.k_stride + (h - p.Hq) * D, at, w);
     }
   };
-  read();
+  if (h < h1) read();
   int64_t row = -1;         // the token's first K row in its page slot, among the rows of both planes
   if (h < h1) {
     const int seq = p.seq ? p.seq[t] : t;
@@ -163,77 +159,72 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams p, int sl
     c[e] = n.c, s[e] = n.s;
   }
   for (;;) {
+    const bool q = h < p.Hq, v = h >= p.Hq + p.Hkv;
+    const int hh = q ? h : v ? h - p.Hq - p.Hkv : h - p.Hq;
+    if (!q && row < 0) {      // (K and V rows are the last of a token)
+      if (p.err && j == 0) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
+      return;
+    }
+    if (!v) {
+      // w: first elements of the pairs, then second ones (fast, neighbours: pairs 0, 1 and 2, 3)
+      const bool beside = kFast && (p.interleaved || 8 * j >= p.r);
+      float y[8];
 #pragma unroll
-    for (int k = 0; k < kPasses; ++k) {
-      const int hk = h + k * slots;
-      if (hk >= h1) continue;
-      const bool q = hk < p.Hq, v = hk >= p.Hq + p.Hkv;
-      const int hh = q ? hk : v ? hk - p.Hq - p.Hkv : hk - p.Hq;
-      if (!q && row < 0) {
-        if (hk == p.Hq && j == 0 && p.err) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
-        continue;
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t wa = beside ? w[e] : w[e / 2] >> (16 * (e % 2)), wb = beside ? w[e] >> 16 : w[2 + e / 2] >> (16 * (e % 2));
+        const double x0 = bflo(wa), x1 = bflo(wb);
+        y[e] = static_cast<float>(__builtin_fma(x0, c[e], -(x1 * s[e])));
+        y[4 + e] = static_cast<float>(__builtin_fma(x1, c[e], x0 * s[e]));
       }
-      if (!v) {
-        // w: first elements of the pairs, then second ones (fast, neighbours: pairs 0, 1 and 2, 3)
-        const bool beside = kFast && (p.interleaved || 8 * j >= p.r);
-        float y[8];
+      uint32_t n[4];
+      if (beside) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t wa = beside ? w[k][e] : w[k][e / 2] >> (16 * (e % 2)), wb = beside ? w[k][e] >> 16 : w[k][2 + e / 2] >> (16 * (e % 2));
-          const double x0 = bflo(wa), x1 = bflo(wb);
-          y[e] = static_cast<float>(__builtin_fma(x0, c[e], -(x1 * s[e])));
-          y[4 + e] = static_cast<float>(__builtin_fma(x1, c[e], x0 * s[e]));
-        }
-        uint32_t n[4];
-        if (beside) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) n[e] = pack_bf2(y[e], y[4 + e]);
-        } else {
-          n[0] = pack_bf2(y[0], y[1]), n[1] = pack_bf2(y[2], y[3]), n[2] = pack_bf2(y[4], y[5]), n[3] = pack_bf2(y[6], y[7]);
-        }
-        // (Elements behind the turned ones are copied, whatever their bits.)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if constexpr (kFast) {
-            w[k][e] = 8 * j < p.r ? n[e] : w[k][e];
-          } else {
-            const int u = 4 * j + 2 * (e % 2);      // pairs u and u + 1 in the halves of this word
-            w[k][e] = (2 * u < p.r ? n[e] & 0xFFFFu : w[k][e] & 0xFFFFu) | (2 * u + 2 < p.r ? n[e] & 0xFFFF0000u : w[k][e] & 0xFFFF0000u);
-          }
-        }
-      }
-      const int64_t to = row + hh + (v ? static_cast<int64_t>(p.num_pages) * kPage * p.Hkv : 0);
-      if (q) {
-        write_pairs<kFast, kNt>(p.q_out + t * p.q_out_stride + hh * D, at, w[k]);
-      } else if constexpr (kFormat == kBf16) {
-        uint16_t* y = static_cast<uint16_t*>(p.cache) + to * D;
-        if (v) put<kNt>(u32x4{w[k][0], w[k][1], w[k][2], w[k][3]}, y + j * 8);
-        else write_pairs<kFast, kNt>(y, at, w[k]);
+        for (int e = 0; e < 4; ++e) n[e] = pack_bf2(y[e], y[4 + e]);
       } else {
-        if (!v) {
-          // Into the row's order, through LDS (a row's lanes are of one wave).
-          uint16_t* y = turned + threadIdx.x / kLanes * D;
-          write_pairs<kFast, false>(y, at, w[k]);
-          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-          __builtin_amdgcn_wave_barrier();
-          const u32x4 x = *reinterpret_cast<const u32x4*>(y + j * 8);
-          w[k][0] = x.x, w[k][1] = x.y, w[k][2] = x.z, w[k][3] = x.w;
-          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-          __builtin_amdgcn_wave_barrier();
-        }
-        const RowCodes<8> codes = quantise_row<kFormat, D, 8>(w[k]);
-        uint8_t* cache = static_cast<uint8_t*>(p.cache);
-        if constexpr (kFormat == PALLAS_QUANT_E2M1) {
-          constexpr int kGroup = D / 32;      // lanes of a quarter
-          *reinterpret_cast<uint32_t*>(cache + to * (D / 2) + j * 4) = codes.codes[0];
-          if (j % kGroup == 0) reinterpret_cast<uint8_t*>(p.scales)[to * 4 + j / kGroup] = static_cast<uint8_t>(codes.scale);
+        n[0] = pack_bf2(y[0], y[1]), n[1] = pack_bf2(y[2], y[3]), n[2] = pack_bf2(y[4], y[5]), n[3] = pack_bf2(y[6], y[7]);
+      }
+      // (Elements behind the turned ones are copied, whatever their bits.)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (kFast) {
+          w[e] = 8 * j < p.r ? n[e] : w[e];
         } else {
-          *reinterpret_cast<u32x2*>(cache + to * D + j * 8) = u32x2{codes.codes[0], codes.codes[1]};
-          if (j == 0) p.scales[to] = __uint_as_float(codes.scale);
+          const int u = 4 * j + 2 * (e % 2);      // pairs u and u + 1 in the halves of this word
+          w[e] = (2 * u < p.r ? n[e] & 0xFFFFu : w[e] & 0xFFFFu) | (2 * u + 2 < p.r ? n[e] & 0xFFFF0000u : w[e] & 0xFFFF0000u);
         }
       }
     }
-    h += kPasses * slots;
+    const int64_t to = row + hh + (v ? static_cast<int64_t>(p.num_pages) * kPage * p.Hkv : 0);
+    if (q) {
+      write_pairs<kFast, kNt>(p.q_out + t * p.q_out_stride + hh * D, at, w);
+    } else if constexpr (kFormat == kBf16) {
+      uint16_t* y = static_cast<uint16_t*>(p.cache) + to * D;
+      if (v) put<kNt>(u32x4{w[0], w[1], w[2], w[3]}, y + j * 8);
+      else write_pairs<kFast, kNt>(y, at, w);
+    } else {
+      if (!v) {
+        // Into the row's order, through LDS (a row's lanes are of one wave).
+        uint16_t* y = turned + threadIdx.x / kLanes * D;
+        write_pairs<kFast, false>(y, at, w);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        const u32x4 x = *reinterpret_cast<const u32x4*>(y + j * 8);
+        w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+      }
+      const RowCodes<8> codes = quantise_row<kFormat, D, 8>(w);
+      uint8_t* cache = static_cast<uint8_t*>(p.cache);
+      if constexpr (kFormat == PALLAS_QUANT_E2M1) {
+        constexpr int kGroup = D / 32;      // lanes of a quarter
+        *reinterpret_cast<uint32_t*>(cache + to * (D / 2) + j * 4) = codes.codes[0];
+        if (j % kGroup == 0) reinterpret_cast<uint8_t*>(p.scales)[to * 4 + j / kGroup] = static_cast<uint8_t>(codes.scale);
+      } else {
+        *reinterpret_cast<u32x2*>(cache + to * D + j * 8) = u32x2{codes.codes[0], codes.codes[1]};
+        if (j == 0) p.scales[to] = __uint_as_float(codes.scale);
+      }
+    }
+    h += slots;
     if (h >= h1) return;
     read();
   }
