@@ -573,7 +573,7 @@ typedef struct {
  * start is its position; after an assembly or a prefill, where it began.  A negative start is
  * padding: nothing of the sequence is written; as where start >= length.  max_new (>= 1) is the most
  * positions of a sequence; where there are more the call raises
- * PALLAS_DEVERR_LENGTH, and the blocks behind floor((max_new + 30) / 16) are left as they were.
+ * PALLAS_DEVERR_LENGTH, and of those blocks only the first floor((max_new + 30) / 16) are written.
  * Blocks beyond the table or on pages outside [0, num_pages) are skipped and raise
  * PALLAS_DEVERR_PAGE, in *d_err (nullable).  num_seqs up to 65535, page_size 16 (UNSUPPORTED
  * otherwise). */
@@ -598,7 +598,8 @@ int pallas_bounds_quant(const pallas_quant_pool* pool, const pallas_bounds_pool*
  * block's score is the largest over the query heads of the KV head (NaN counts as larger than
  * any number).  The sum is of whole numbers and the products are float32, so the lists are
  * the same however the work is divided, and in any other program that follows this.
- *   Query rows, lengths, max_length, tables and their limits and errors are pallas_attend_*'s; a
+ *   Query rows, lengths, max_length, tables and their limits and errors are pallas_attend_*'s
+ * (and max_length up to 2^30, below 2^34 times n_kv_heads, UNSUPPORTED beyond); a
  * block on a page outside [0, num_pages) scores lowest.  The workspace (device, 256-byte aligned,
  * pallas_select_workspace_size bytes) holds nothing between calls; calls that may run at once need
  * one each. */
@@ -615,7 +616,7 @@ size_t pallas_select_workspace_size(int32_t num_seqs, int32_t n_kv_heads, int32_
  * for the KV head.  Of a list the first min(max_blocks, blocks of the length) entries are read;
  * one that names no block of the length (a negative one, say) adds nothing, a block that is
  * named twice counts twice, the order changes last bits alone.  The lse is that of the keys
- * attended to.  The workspace is that of pallas_attend_* with max_length min(max_length, 16
+ * attended to.  max_length up to 2^30 (UNSUPPORTED).  The workspace is that of pallas_attend_* with max_length min(max_length, 16
  * max_blocks). */
 int pallas_attend_blocks_kv(const pallas_kv_pool* pool, int32_t layer, int32_t num_seqs,
                             int32_t n_q_heads, const void* d_q, int64_t q_stride,

@@ -295,7 +295,7 @@ __device__ __forceinline__ void score_runs(const SelectParams& p, int s, int kh,
 }
 
 __device__ __forceinline__ int row_blocks(const SelectParams& p, int s) {
-  return (min(max(p.lengths[s], 0), p.max_length) + kPage - 1) / kPage;
+  return (min(max(p.lengths[s], 0), p.max_length) + kPage - 1) / kPage;      // (max_length: at most 2^30)
 }
 
 // Scores of long rows, spread over the chip: waves of a workgroup take the heads of the same

@@ -221,6 +221,7 @@ struct BlockLists {
   int32_t max_blocks;
 };
 constexpr BlockLists attend_all{false, nullptr, 0};
+constexpr int32_t kMaxListedLength = 1 << 30;      // 16 times a number of blocks is an int
 
 // Checks and parameters of both cache types; the caller has checked the pool.
 int attend_call(const char* what, pallas::CacheType type, pallas::AttendParams& p, int page_size, int32_t num_seqs,
@@ -242,6 +243,8 @@ int attend_call(const char* what, pallas::CacheType type, pallas::AttendParams& 
                 (long long)(int64_t(max_pages) * page_size));
   if (lists.listed && (!lists.d_blocks || !aligned(lists.d_blocks, 4) || lists.max_blocks < 1))
     return fail(PALLAS_ERR_INVALID_ARG, "%s: blocks null or not 4-byte aligned, or max_blocks below 1", what);
+  if (lists.listed && max_length > kMaxListedLength)
+    return fail(PALLAS_ERR_UNSUPPORTED, "%s: max_length %d (at most 2^30)", what, max_length);
   p.scale_log2 = static_cast<float>(double(scale) * 1.4426950408889634);
   if (!std::isfinite(p.scale_log2)) return fail(PALLAS_ERR_INVALID_ARG, "%s: scale is not finite", what);
   if (!d_workspace || !aligned(d_workspace, 256))
@@ -360,9 +363,9 @@ int bounds_call(const char* what, pallas::CacheType type, pallas::BoundsParams& 
 int check_select(int32_t num_seqs, int32_t n_kv_heads, int32_t max_length, const char* what) {
   if (num_seqs < 1 || max_length < 1)
     return fail(PALLAS_ERR_INVALID_ARG, "%s: num_seqs and max_length must be at least 1", what);
-  if (num_seqs > 65535 || int64_t(num_seqs) * max_length > (int64_t(1) << 35) ||
+  if (num_seqs > 65535 || max_length > kMaxListedLength || int64_t(num_seqs) * max_length > (int64_t(1) << 35) ||
       (int64_t(max_length) / 256 + 1) * n_kv_heads >= (1 << 26))      // (a launch has fewer than 2^32 threads)
-    return fail(PALLAS_ERR_UNSUPPORTED, "%s: %d sequences (at most 65535) of up to %d keys (at most 2^35 in all, below 2^34 with the heads)",
+    return fail(PALLAS_ERR_UNSUPPORTED, "%s: %d sequences (at most 65535) of up to %d keys (at most 2^30, 2^35 in all, 2^34 times the KV heads)",
                 what, num_seqs, max_length);
   return PALLAS_OK;
 }

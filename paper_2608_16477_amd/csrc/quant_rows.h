@@ -2,6 +2,8 @@
 // elements lie over neighbouring lanes, a few to each.
 #pragma once
 
+#include <type_traits>
+
 #include "common.h"
 
 namespace pallas {

@@ -75,7 +75,8 @@ def test_select_refusals(P):
         assert "select" in P.pallas_last_error()
     for bad in (dict(layer=2), dict(layer=-1), dict(max_length=65)):
         assert select_rc(P, **bad) == S.OUT_OF_RANGE, bad
-    for bad in (dict(seqs=65536), dict(heads=8192, qs=1 << 20), dict(seqs=65535, max_length=1 << 20, max_pages=1 << 16)):
+    for bad in (dict(seqs=65536), dict(heads=8192, qs=1 << 20), dict(seqs=65535, max_length=1 << 20, max_pages=1 << 16),
+                dict(seqs=1, max_length=(1 << 30) + 1, max_pages=1 << 27)):
         assert select_rc(P, **bad) == S.UNSUPPORTED, bad
     assert select_rc(P, bounds_pool(head_dim=96), qs=4096) == S.UNSUPPORTED
     assert select_rc(P, bounds_pool(n_kv_heads=4097)) == S.UNSUPPORTED
@@ -117,6 +118,7 @@ def test_attend_refusals(P, quant):
         assert "attend" in P.pallas_last_error()
     for bad in (dict(layer=2), dict(max_length=65)):
         assert attend_rc(P, quant, **bad) == S.OUT_OF_RANGE, bad
+    assert attend_rc(P, quant, seqs=1, max_length=(1 << 30) + 1, max_pages=1 << 27) == S.UNSUPPORTED
     # room for what the lists hold is enough, and needed
     for blocks, keys in ((2, 32), (4, 64), (100, 64)):
         need = P.pallas_attend_workspace_size(3, 8, 4, 64, keys)
