@@ -62,10 +62,10 @@ __device__ __forceinline__ uint32_t ordered_bf2(uint32_t w) {
   return w ^ (__builtin_bit_cast(uint32_t, sign) & 0x7FFF7FFFu);
 }
 
-// A wave per block and KV head: D / 8 lanes take a row, eight values each.  Rows of bf16, E4M3
-// and E2M1 are (the last two, with their scales, exactly, but for magnitudes too small to be of a
-// block that is not zero) bf16 values, which order as integers: two to an instruction, and
-// infinities and NaN show at the end.  INT8 rows are products in float32.
+// A wave per block and KV head: D / 8 lanes take a row, eight values each.  Rows of bf16 and
+// E2M1 are (these, with their scales, exactly, but for magnitudes too small to be of a block that
+// is not zero) bf16 values, which order as integers: two to an instruction, and infinities and
+// NaN show at the end.  8-bit rows are products in float32.
 template <int D, CacheType T>
 __global__ __launch_bounds__(kThreads) void bounds_kernel(BoundsParams p, int per_seq) {
   constexpr int kLanes = D / 8, kRows = 64 / kLanes, kReads = kPage / kRows;
@@ -88,7 +88,8 @@ __global__ __launch_bounds__(kThreads) void bounds_kernel(BoundsParams p, int pe
   auto row = [&](int n) { return (static_cast<int64_t>(pg) * kPage + min(n * kRows + sub, keys - 1)) * p.Hkv + h; };
   float x[8];           // of the largest (lanes of the first row) or the smallest key
   float a;              // the largest magnitude of both, over the row
-  if constexpr (T == kCacheInt8) {
+  if constexpr (T == kCacheInt8 || T == kCacheE4m3) {
+    constexpr int kFormat = T == kCacheInt8 ? PALLAS_QUANT_INT8 : PALLAS_QUANT_E4M3;
     u32x2 c[kReads];
     float scale[kReads], top[8], low[8];
 #pragma unroll
@@ -100,10 +101,11 @@ __global__ __launch_bounds__(kThreads) void bounds_kernel(BoundsParams p, int pe
 #pragma unroll
     for (int n = 0; n < kReads; ++n) {
       odd |= !(scale[n] < INFINITY);
-      const f32x4 lo = code_values<PALLAS_QUANT_INT8>(c[n].x), hi = code_values<PALLAS_QUANT_INT8>(c[n].y);
+      const f32x4 lo = code_values<kFormat>(c[n].x), hi = code_values<kFormat>(c[n].y);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float v = (e < 4 ? lo[e % 4] : hi[e % 4]) * scale[n];
+        if constexpr (T == kCacheE4m3) odd |= v != v;      // (a code, too, can be NaN)
         top[e] = n == 0 ? v : fmaxf(top[e], v);
         low[e] = n == 0 ? v : fminf(low[e], v);
       }
@@ -128,9 +130,6 @@ __global__ __launch_bounds__(kThreads) void bounds_kernel(BoundsParams p, int pe
       } else if constexpr (T == kCacheE2m1) {
         w[n].x = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(p.k) + row(n) * (D / 2) + part * 4);
         w[n].y = static_cast<uint32_t>(reinterpret_cast<const uint8_t*>(p.scales)[row(n) * 4 + part / (D / 32)]);
-      } else {
-        const u32x2 c = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(p.k) + row(n) * D + part * 8);
-        w[n].x = c.x, w[n].y = c.y, w[n].z = __float_as_uint(p.scales[row(n)]);
       }
     }
     uint32_t top[4], low[4];
@@ -138,12 +137,6 @@ __global__ __launch_bounds__(kThreads) void bounds_kernel(BoundsParams p, int pe
     for (int n = 0; n < kReads; ++n) {
       if constexpr (T == kCacheE2m1) {
         w[n] = e2m1_bf16(w[n].x, __uint_as_float(w[n].y << 23));
-      } else if constexpr (T == kCacheE4m3) {
-        const float scale = __uint_as_float(w[n].z);
-        w[n] = u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[n].x, scale, false)),
-                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[n].x, scale, true)),
-                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[n].y, scale, false)),
-                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[n].y, scale, true))};
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {

@@ -270,6 +270,39 @@ def test_infinities_and_nan(P, fmt):
     equal_lists(cache.select(P, q, 10, 1, 2), lists)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_bounds_of_any_8_bit_rows(P, fmt, d):
+    """Scales that are no powers of two, and codes that no store writes, an E4M3 NaN among them."""
+    hkv, lens = 3, [16, 100, 1, 33]
+    rng = np.random.default_rng(d)
+    pages = sum(-(-n // 16) for n in lens)
+    codes = rng.integers(0, 256, (1, 2, pages, 16, hkv, d)).astype(np.uint8)
+    if fmt == "e4m3":
+        codes[codes % 128 == 127] = 0
+        codes[0, 0, 3, 5, 1, d - 1] = 0xFF              # of the second row of lengths; its block 2
+    scales = np.exp(rng.normal(0, 2, (1, 2, pages, 16, hkv))).astype(np.float32)
+    table = np.full((4, 7), -1, dtype=np.int32)
+    at = 0
+    for i, n in enumerate(lens):
+        table[i, :-(-n // 16)] = np.arange(at, at - (-n // 16))
+        at -= -n // 16
+    bounds, steps = torch.full((1, pages, hkv, 2, d), -128, dtype=torch.int8, device=DEV), torch.full((1, pages, hkv), -7.0, device=DEV)
+    kind = torch.float8_e4m3fn if fmt == "e4m3" else torch.int8
+    P.pallas_bounds_quant(torch.from_numpy(codes).to(DEV).view(kind), torch.from_numpy(scales).to(DEV), 0, bounds, steps,
+                          torch.zeros(4, dtype=torch.int32, device=DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), 100,
+                          torch.from_numpy(table).to(DEV))
+    nans = 0
+    for i, n in enumerate(lens):
+        t = np.arange(n)
+        rows = codes[0, 0, table[i, t // 16], t % 16], scales[0, 0, table[i, t // 16], t % 16]
+        c, s = co.block_bounds(co.dequantise(*rows, fmt))
+        pg = torch.from_numpy(table[i, :len(s)]).long()
+        assert np.array_equal(bounds[0, pg].cpu().numpy(), c) and np.array_equal(steps[0, pg].cpu().numpy(), s, equal_nan=True)
+        nans += int(np.isnan(s).sum())
+    assert nans == (fmt == "e4m3")
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("lens,n", [([300, 20, 0, 90], 12), ([3000, 2000, 900, 0], 90), ([9000] * 3, 300)])
 def test_any_lists(P, fmt, lens, n):
