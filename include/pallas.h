@@ -431,7 +431,8 @@ int pallas_rope_apply(const pallas_rope_plan* plan, int32_t inverse, int32_t num
  *         6 (OCP 4-bit float, 2 exponent bits and 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3,
  *         4, 6): reading back rounds nothing more; quarters with a < 2^-100 count as zero
  * A row (quarter) of zeros has scale 0 (b 0, codes 0).  A row (quarter) with an infinity
- * or a NaN has scale NaN (b 255) and codes 0: it reads back, and attends, as NaN.
+ * or a NaN has scale NaN (b 255) and codes 0: it reads back, and attends, as NaN.  (Bytes 253 and
+ * 254 are never written; attention may take such a quarter as NaN.)
  *   Codes and scales are moved by pallas_pack_suffix_blocks and
  * pallas_assemble_kv, which copy bits: the codes as a pallas_kv_pool of head_dim
  * / 2 (E2M1: / 4), the scales as one of head_dim 2 (n_kv_heads a multiple of 4). */

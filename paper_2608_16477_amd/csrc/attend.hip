@@ -369,15 +369,19 @@ struct Wave {
         const int key = kPair ? row_n % kPage : row_n, head = kPair ? row_n / kPage : 0;
         uint32_t w = reinterpret_cast<const uint32_t*>(Kst + S::kScales)[kBlk + (kPair ? 2 * key + head : key)];
         if constexpr (kPair) {
-          // A NaN of one head's V would reach the other head through its weight of zero: such a row counts
-          // as zeros, and its head's sums become NaN.
-          const uint32_t nan = ((w & 0x7F7F7F7Fu) + 0x01010101u) & w & 0x80808080u;
-          const uint64_t rows = __builtin_amdgcn_ballot_w64(nan != 0);
-          if (rows != 0) {
-            if (nan != 0) w = 0;
-            if (second ? rows >> 32 != 0 : static_cast<uint32_t>(rows) != 0) {
+          // A NaN of one head's V would reach the other head through its weight of zero, and so would an
+          // infinity, as values with a scale of 2^126 or 2^127 can become: such a quarter counts as zeros, and
+          // its head's sums of these dimensions become NaN.
+          const uint32_t nan = ((w & 0x7F7F7F7Fu) + 0x03030303u) & w & 0x80808080u;
+          if (__builtin_amdgcn_ballot_w64(nan != 0) != 0) {
+            w &= ~((nan >> 7) * 255u);
 #pragma unroll
-              for (int dt = 0; dt < DT; ++dt) acc[dt] += __uint_as_float(kNanScale);
+            for (int quarter = 0; quarter < 4; ++quarter) {
+              const uint64_t rows = __builtin_amdgcn_ballot_w64(nan >> (8 * quarter + 7) & 1);
+              if (second ? rows >> 32 != 0 : static_cast<uint32_t>(rows) != 0) {
+#pragma unroll
+                for (int dt = quarter * DT / 4; dt < (quarter + 1) * DT / 4; ++dt) acc[dt] += __uint_as_float(kNanScale);
+              }
             }
           }
         }

@@ -442,7 +442,7 @@ constexpr int kAttendGroup = 16;         // query heads that share one pass over
 // Blocks of a wave's range: at most one per pair of lanes.
 constexpr int kAttendMaxBlocks = 32;
 // 4-bit rows of two neighbouring KV heads share 128-byte lines (of four, for 64 dimensions): a
-// wave takes both where their query heads fit into one pass and they attend to the same keys.
+// workgroup takes both where their query heads fit into one pass and they attend to the same keys.
 constexpr bool attend_pairs(CacheType type, int Hq, int Hkv, bool listed) {
   return type == kCacheE2m1 && !listed && Hkv % 2 == 0 && 2 * (Hq / Hkv) <= 16;
 }
