@@ -369,7 +369,9 @@ __global__ __launch_bounds__(kWide) void select_kernel(SelectParams p) {
   uint32_t want = p.budget - p.first - p.last;
   bool all = want == 0;      // all of [low, high] are selected (none: it lies above every score)
   if (all) low = high = kAlways;
-  while (!all && low != high) {
+  // (Four rounds at most, 2^32 of 2^21 to begin with; counted, so that scores that another call changes
+  // meanwhile end too.)
+  for (int round = 0; round < 4 && !all && low < high; ++round) {
     // Of 2^shift scores each, at most kBins.
     const int shift = max(32 - __builtin_clz(high - low) - 11, 0);
     for (int pass = 0; pass < passes; ++pass) {
@@ -457,7 +459,8 @@ __global__ __launch_bounds__(kWide) void select_kernel(SelectParams p) {
       const bool m = more[k] >> lane & 1, e = same[k] >> lane & 1;
       const uint32_t ms = more0 + counts[0][k * kWaves + wave] + __builtin_popcountll(more[k] & below);
       const uint32_t es = same0 + counts[1][k * kWaves + wave] + __builtin_popcountll(same[k] & below);
-      if (m || (e && es < want)) out[ms + (all ? 0 : min(es, want))] = pass * kPass + k * kWide + t;
+      const uint32_t to = ms + (all ? 0 : min(es, want));
+      if ((m || (e && es < want)) && to < static_cast<uint32_t>(p.budget)) out[to] = pass * kPass + k * kWide + t;
     }
     more0 += found[0], same0 += found[1];
     if (pass + 1 < passes) __syncthreads();
