@@ -954,6 +954,14 @@ hipError_t launch_split(const AttendParams& p, int groups, int splits, int per, 
 constexpr int kShortKeys = 512;
 constexpr int kShortGroups = 1536;
 constexpr int kSplitBlocks = 2;
+// Rows of listed blocks are equally long, and a workgroup each up to twice that, but where
+// there are so few that they are cut (64 rows of 1024 keys bf16 16.1, 12.2 as splits), and bf16 ones
+// only where they do not fill the chip twice (1024 rows of 768 keys 70.3 (66.0), 512 of 1024 50.8
+// (50.3), 256 25.3 (29.7)).  512 rows of 1024 keys E4M3 33.0 (35.4), E2M1 30.5 (40.0), 96 of them 14.5 (13.5),
+// 12.9 (12.9); 1440 of 640 keys 53.8 (61.2), 50.0 (59.8).
+constexpr int kListedKeys = 1024;
+constexpr int kListedFew = 64;
+constexpr int kListedBf16 = 512;
 
 template <int D, CacheType T, bool kListed, bool kPair>
 void launch_ranges(const AttendParams& p, int groups, int heads, hipStream_t s) {
@@ -970,7 +978,9 @@ hipError_t launch(const AttendParams& p, hipStream_t s) {
   constexpr int kFill = std::min(attend_waves(T, D), 8);     // waves whose rings fill a CU's LDS
   const int64_t rows = int64_t(p.seqs) * heads;
   const int most = static_cast<int>(attend_total(1, p.max_row));        // blocks of a row
-  if (p.max_row <= kShortKeys && rows <= kShortGroups)
+  const bool row_each = p.max_row <= kShortKeys ? rows <= kShortGroups :
+                        kListed && p.max_row <= kListedKeys && rows > kListedFew && rows <= (T == kCacheBf16 ? kListedBf16 : kShortGroups);
+  if (row_each)
     return rows <= 256 ? launch_split<D, T, kFill, kListed>(p, groups, 1, most, s) : launch_split<D, T, kFill / 2, kListed>(p, groups, 1, most, s);
   for (int each = 1; each <= kSplitBlocks; each *= 2) {
     // (Records, seqs * splits <= 256 / heads: fewer than attend_ranges, so there is room.)

@@ -168,6 +168,8 @@ CASES = [
     (128, 4, 16, [330] * 40, 3, 1, 1),
     (128, 2, 2, [40000, 20], 100, 1, 4),         # more than 2048 blocks; ranges
     (64, 8, 8, [9000, 3000, 0, 8000, 500, 12000], 250, 3, 2),
+    (128, 2, 8, [2000, 1100, 0, 1, 900, 1024, 1040, 1023, 1500, 17, 1600], 64, 1, 2),      # a workgroup a row of 1024 keys
+    (64, 1, 8, [700, 1100, 600] * 24, 37, 0, 2),
 ]
 
 
