@@ -197,25 +197,34 @@ __device__ __forceinline__ uint32_t order_of(float x) {
 constexpr int kRun = 16;
 constexpr int kHeads = 16;
 constexpr int kAhead = 4;
-template <int D, class Put>
-__device__ __forceinline__ void score_runs(const SelectParams& p, int s, int kh, int blocks, int first, int step, int runs, Put put) {
-  const int lane = threadIdx.x & 63, q4 = lane >> 4, l16 = lane & 15;
-  for (int g0 = 0; g0 < p.G; g0 += kHeads) {
-    int pages[kAhead];
-    auto read_pages = [&](int from) {
+template <int D>
+struct Ahead {
+  int pages[kAhead];
+  u32x4 w[D / 64][2];      // 16 elements of each 64 of head l16 (the last again where there are fewer)
+
+  // (Entries behind the row's: no use, but within the table.)
+  __device__ __forceinline__ void read_pages(const SelectParams& p, int s, int first, int step) {
 #pragma unroll
-      for (int n = 0; n < kAhead; ++n)
-        pages[n] = p.bt[static_cast<int64_t>(s) * p.max_pages + min((first + (from + n) * step) * kRun + l16, blocks - 1)];
-    };
-    read_pages(0);
-    // Lane: 16 elements of each 64 of head l16 (the last again where there are fewer).
-    const int nh = min(kHeads, p.G - g0);
-    const uint16_t* q = p.q + s * p.q_stride + static_cast<int64_t>(kh * p.G + g0 + min(l16, nh - 1)) * D;
-    u32x4 w[D / 64][2];
+    for (int n = 0; n < kAhead; ++n)
+      pages[n] = p.bt[static_cast<int64_t>(s) * p.max_pages + min((first + n * step) * kRun + static_cast<int>(threadIdx.x & 15), p.max_pages - 1)];
+  }
+  __device__ __forceinline__ void read_q(const SelectParams& p, int s, int kh, int g0) {
+    const int lane = threadIdx.x & 63, q4 = lane >> 4, l16 = lane & 15;
+    const uint16_t* q = p.q + s * p.q_stride + static_cast<int64_t>(kh * p.G + g0 + min(l16, min(kHeads, p.G - g0) - 1)) * D;
 #pragma unroll
     for (int c = 0; c < D / 64; ++c)
 #pragma unroll
       for (int i = 0; i < 2; ++i) w[c][i] = *reinterpret_cast<const u32x4*>(q + 64 * c + 16 * q4 + 8 * i);
+  }
+};
+template <int D, class Put>
+__device__ __forceinline__ void score_runs(const SelectParams& p, Ahead<D>& a, int s, int kh, int blocks, int first, int step, int runs, Put put) {
+  const int lane = threadIdx.x & 63, q4 = lane >> 4, l16 = lane & 15;
+  for (int g0 = 0; g0 < p.G; g0 += kHeads) {
+    if (g0 > 0) {
+      a.read_pages(p, s, first, step);
+      a.read_q(p, s, kh, g0);
+    }
     i32x4 top[2][D / 64], low[2][D / 64];
     float scale[2];
     auto inside = [&](int pg) { return pg >= 0 && pg < p.num_pages; };
@@ -229,14 +238,14 @@ __device__ __forceinline__ void score_runs(const SelectParams& p, int s, int kh,
       }
       scale[to] = p.bound_scales[at];
     };
-    read(pages[0], 0);
+    read(a.pages[0], 0);
     uint32_t most = 0;
 #pragma unroll
     for (int c = 0; c < D / 64; ++c)
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) most = max_u16x2(most, w[c][i][e] & 0x7FFF7FFFu);
+        for (int e = 0; e < 4; ++e) most = max_u16x2(most, a.w[c][i][e] & 0x7FFF7FFFu);
     // (As bits, in which a NaN is larger than any number.)
     most = over_rows<16>(max(most & 0xFFFFu, most >> 16), [](uint32_t u, uint32_t v) { return max(u, v); });
     const Step st = step_of(__uint_as_float(most << 16));
@@ -245,7 +254,7 @@ __device__ __forceinline__ void score_runs(const SelectParams& p, int s, int kh,
     for (int c = 0; c < D / 64; ++c)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint32_t lo = w[c][e / 2][e % 2 * 2], hi = w[c][e / 2][e % 2 * 2 + 1];
+        const uint32_t lo = a.w[c][e / 2][e % 2 * 2], hi = a.w[c][e / 2][e % 2 * 2 + 1];
         const float x[4] = {bflo(lo), bfhi(lo), bflo(hi), bfhi(hi)};
         const uint32_t codes = step_codes(x, st.up), sign = (codes >> 7 & 0x01010101u) * 255u;
         up[c][e] = static_cast<int>(codes & ~sign);
@@ -257,13 +266,13 @@ __device__ __forceinline__ void score_runs(const SelectParams& p, int s, int kh,
     for (int from = 0; from < runs; from += kAhead) {
       int now[kAhead];
 #pragma unroll
-      for (int n = 0; n < kAhead; ++n) now[n] = pages[n];
-      if (from + kAhead < runs) read_pages(from + kAhead);
+      for (int n = 0; n < kAhead; ++n) now[n] = a.pages[n];
+      if (from + kAhead < runs) a.read_pages(p, s, first + (from + kAhead) * step, step);
 #pragma unroll
       for (int n = 0; n < kAhead; ++n) {
         if (from + n >= runs) break;
         if (n + 1 < kAhead) read(now[n + 1], (n + 1) % 2);
-        else if (from + kAhead < runs) read(pages[0], 0);
+        else if (from + kAhead < runs) read(a.pages[0], 0);
         i32x4 dot = {0, 0, 0, 0};
 #pragma unroll
         for (int c = 0; c < D / 64; ++c) {
@@ -295,12 +304,18 @@ __device__ __forceinline__ int row_blocks(const SelectParams& p, int s) {
 // blocks, which are neighbours in memory.
 template <int D>
 __global__ __launch_bounds__(kThreads) void score_kernel(SelectParams p, int per_wave) {
-  const int s = blockIdx.y, unit = static_cast<int>(blockIdx.x) * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int s = blockIdx.y;
+  // (Rotated from row to row: else an XCD takes the same blocks of all rows, and the one with the first
+  // blocks has more than that with the last; 64 rows of 2000 to 16,000 keys 29.1 us, 22.4.)
+  const int unit = static_cast<int>((blockIdx.x + blockIdx.y) % gridDim.x) * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kh = unit % p.Hkv, first = unit / p.Hkv * per_wave;
+  Ahead<D> a;
+  a.read_pages(p, s, first, 1);
+  a.read_q(p, s, kh, 0);
   const int blocks = row_blocks(p, s);
   if (blocks <= p.budget || first * kRun >= blocks) return;      // all are selected, or none here
   uint32_t* out = p.order + (static_cast<int64_t>(s) * p.Hkv + kh) * p.stride;
-  score_runs<D>(p, s, kh, blocks, first, 1, min((blocks + kRun - 1) / kRun - first, per_wave), [&](int b, uint32_t x, int pass) { out[b] = pass == 0 ? x : max(x, out[b]); });
+  score_runs<D>(p, a, s, kh, blocks, first, 1, min((blocks + kRun - 1) / kRun - first, per_wave), [&](int b, uint32_t x, int pass) { out[b] = pass == 0 ? x : max(x, out[b]); });
 }
 
 // ------------------------------------------------------------ selection
@@ -322,6 +337,11 @@ __global__ __launch_bounds__(kWide) void select_kernel(SelectParams p) {
   __shared__ uint32_t counts[2][kEach * kWaves];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int kh = blockIdx.x, s = blockIdx.y;
+  Ahead<D> a;
+  if constexpr (kScored) {
+    a.read_pages(p, s, wave, kWaves);
+    a.read_q(p, s, kh, 0);
+  }
   const int full = p.lengths[s], blocks = row_blocks(p, s);
   if (p.err && kh == 0 && t == 0 && full != min(max(full, 0), p.max_length)) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_LENGTH));
   int32_t* out = p.blocks + (static_cast<int64_t>(s) * p.Hkv + kh) * p.budget;
@@ -332,7 +352,7 @@ __global__ __launch_bounds__(kWide) void select_kernel(SelectParams p) {
   const uint32_t* in = p.order + (static_cast<int64_t>(s) * p.Hkv + kh) * p.stride;
   if constexpr (kScored) {
     const int runs = ((blocks + kRun - 1) / kRun - wave + kWaves - 1) / kWaves;
-    if (runs > 0) score_runs<D>(p, s, kh, blocks, wave, kWaves, runs, [&](int b, uint32_t x, int pass) { scored[b] = pass == 0 ? x : max(x, scored[b]); });
+    if (runs > 0) score_runs<D>(p, a, s, kh, blocks, wave, kWaves, runs, [&](int b, uint32_t x, int pass) { scored[b] = pass == 0 ? x : max(x, scored[b]); });
     in = scored;
     __syncthreads();
   }
