@@ -576,8 +576,9 @@ typedef struct {
  * positions of a sequence; where there are more the call raises
  * PALLAS_DEVERR_LENGTH, and of those blocks only the first floor((max_new + 30) / 16) are written.
  * Blocks beyond the table or on pages outside [0, num_pages) are skipped and raise
- * PALLAS_DEVERR_PAGE, in *d_err (nullable).  num_seqs up to 65535, page_size 16 (UNSUPPORTED
- * otherwise). */
+ * PALLAS_DEVERR_PAGE, in *d_err (nullable).  Bounds of a page that two sequences of a call hold to
+ * different lengths are of either.  num_seqs up to 65535, page_size 16, and as many blocks of max_new,
+ * times n_kv_heads, as are below 2^26 (UNSUPPORTED otherwise). */
 int pallas_bounds_kv(const pallas_kv_pool* pool, const pallas_bounds_pool* bounds, int32_t layer,
                      int32_t num_seqs, const int32_t* d_start, const int32_t* d_lengths,
                      int32_t max_new, const int32_t* d_block_tables, int32_t max_pages,
