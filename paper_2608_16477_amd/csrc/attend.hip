@@ -365,7 +365,7 @@ struct Wave {
         // scales (a transposed word would hold rows of eight scales), and they are read back
         // transposed; the first 64 from the wave's own room, the others from the stage,
         // where K and V have been read.  Row n: of key n, or of key n % 16 of head n / 16.
-        const int row_n = lane >> 1, half = lane & 1, swap = (row_n >> 2) & 1;
+        const int row_n = lane >> 1, half = lane & 1, swap = (row_n >> 1) & 1;
         const int key = kPair ? row_n % kPage : row_n, head = kPair ? row_n / kPage : 0;
         uint32_t w = reinterpret_cast<const uint32_t*>(Kst + S::kScales)[kBlk + (kPair ? 2 * key + head : key)];
         if constexpr (kPair) {
@@ -396,7 +396,7 @@ struct Wave {
           u32x4* const turn = i < 2 ? ring + S::kRing + i * kTurnStep : ring + stage * S::kSlots + (i - 2) * kTurnStep;
           constexpr int kStep = D == 64 ? 16 : 8;     // bits between the scales of two steps
           const float vu = __uint_as_float(i * kStep < 24 ? w << (23 - i * kStep) : w >> 1);
-          // (Which half goes first is such that a write falls on all banks.)
+          // (Which half goes first is such that the eight lanes of a 128-byte write fall on 32 banks.)
           turn[turn_slot(row_n, 2 * half + swap)] = e2m1_bf16(swap ? vc[i].y : vc[i].x, vu);
           turn[turn_slot(row_n, 2 * half + 1 - swap)] = e2m1_bf16(swap ? vc[i].x : vc[i].y, vu);
         }
