@@ -22,13 +22,27 @@
 // conflict.  Calls that do not fill the chip are a chain of loads, which the way to a range is
 // longer than: they keep a workgroup per split (attend_split_kernel).
 //
+// 4-bit rows of 128 are 64 bytes, half of a line, of a KV head, so a workgroup takes two
+// neighbouring heads whose query heads fit into one pass (attend_pairs): a step is one page of both, the
+// first sixteen rows of its operands one head's, the others the other's, with a weight of zero
+// where a query head meets a row of the other.  The four waves take the steps of one range in
+// turn and merge each sequence through LDS (us, without pairs in parentheses: 300 rows of 1500 keys, 64 / 8
+// heads of 128, 119 (171), 64 of 2000 40 (47), 200 of 700 50 (59); 64 of 500 to 8000, heads of 64, 37
+// (45); 16 of 2000, 32 / 32 heads, 38 (48)); a range to each wave would leave twice the records.  64
+// sequences of 500 to 7177 keys, 178 MB, 64 / 8 heads: 48, of them the join 5; the first launch
+// reads at 4.3 TB/s over all, and at 5.9 while it streams: start and ends take 11.  Vector
+// instructions, conversions mostly, take 0.57 of the issue slots, matrix pipes and LDS are busy for a
+// quarter of the time each; the same loads with nothing done to them take 42 in all.
+//
 // Each wave moves its blocks from memory straight into a private two-stage LDS ring,
 // with the rows' scales.  Scores are S^T = K Q^T with v_mfma_f32_16x16x32_bf16 (the
 // query heads are the columns): lane l holds keys 4 (l / 16) + r of head l mod 16.
 // O^T = V^T P^T takes those registers as its B operand as they are, with V read
 // transposed from LDS.  8-bit codes are turned into bf16, which holds them exactly,
 // between LDS and the MFMAs; a row's scale multiplies the score of its key (K) or its
-// weight (V), in float32.  Weights stay 32-bit: they go into the MFMA as three bf16 parts
+// weight (V), in float32.  4-bit codes are turned with the scale of their quarter, a power of
+// two, which bf16 holds too: K where a lane's part of a row is one quarter, V on its way into
+// LDS once more as bf16.  Weights stay 32-bit: they go into the MFMA as three bf16 parts
 // whose sum they are.  (Two parts, 2^-17 off, us: 1 row of 500 keys bf16 7.3 (7.6), 128 of 300
 // E4M3 21.8 (22.4), 64 of 500 to 8000 68.8 (69.3), 60,001 and 33,333 bf16 67.8 (68.2).)
 #include "common.h"

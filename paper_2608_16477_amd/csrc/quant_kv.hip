@@ -12,7 +12,8 @@
 //         goes into the conversion instruction.
 //
 // All are bound by memory: 2 d bytes and d + 4 (E2M1: d / 2 + 4) bytes per row (34,708
-// tokens of 8 heads of 128, E4M3, 217 MB each way: 42 us written, 42 read back, 5.2 TB/s).
+// tokens of 8 heads of 128, E4M3, 217 MB each way: 42 us written, 42 read back, 5.2 TB/s;
+// E2M1, 180 MB: 37 and 37, 4.8 TB/s).
 // Codes are stored plainly (with non-temporal stores 87 us for both, and loads 86, in place
 // of 84).  A lane takes 16 elements (two 16-byte vectors of bf16, one of 8-bit codes), d / 16
 // neighbouring lanes a row, and neighbouring rows are the heads of a token, contiguous on
