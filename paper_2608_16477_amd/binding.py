@@ -370,6 +370,9 @@ def _rows(t, what: str, dev: int):
 
 def _packed_rows(t, what: str, dev: int, shape):
     """The row stride of rows of this shape with their heads one behind the other."""
+    if t.is_contiguous() and t.shape == shape and len(shape) == 3 and t.get_device() == dev >= 0 and (
+            t.dtype is (_torch or _load_torch()).bfloat16):
+        return shape[1] * shape[2]
     got, stride = _rows(t, what, dev)
     if got != shape or (stride[1] != shape[2] and shape[1] > 1):
         _bad(f"{what}: {tuple(got)}, strides {stride}; wanted {tuple(shape)}, its heads contiguous")
@@ -378,14 +381,15 @@ def _packed_rows(t, what: str, dev: int, shape):
 
 def _launch(dev: int, stream, call, *args):
     """``call(*args, stream)`` with the tensors' GPU current, on its current stream unless one is given."""
-    cuda = _torch.cuda
-    # (The raw handle: a torch.cuda.Stream object costs 1 us of a call's 10.)
+    # (The raw handle: a torch.cuda.Stream object costs 1 us of a call's 9.)
     handle = _torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
-    if cuda.current_device() == dev:
-        _check(call(*args, handle))
+    if _torch._C._cuda_getDevice() == dev:
+        rc = call(*args, handle)
     else:
-        with cuda.device(dev):
-            _check(call(*args, handle))
+        with _torch.cuda.device(dev):
+            rc = call(*args, handle)
+    if rc:
+        _check(rc)
 
 
 def pallas_rope_init(rotary_dim: int, theta: float, layout: str = "half", scaling: str = "none", factor: float = 1.0,
@@ -439,7 +443,8 @@ def quant_pool_struct(codes, scales) -> QuantPoolC:
         _bad(f"quant pool: codes of {dtype}, wanted float8_e4m3fn, int8 or float4_e2m1fn_x2")
     fmt, per, of, rank = kind
     L, two, P, page, hkv, d = shape = _whole(codes, "quant pool: codes", dtype, 6, dev)
-    if two != 2 or _whole(scales, "quant pool: scales", of, rank, dev) != (shape[:5] if rank == 5 else shape[:5] + (4,)):
+    of_rows = (L, 2, P, page, hkv) if rank == 5 else (L, 2, P, page, hkv, 4)
+    if two != 2 or _whole(scales, "quant pool: scales", of, rank, dev) != of_rows:
         _bad(f"quant pool: codes {tuple(shape)}, scales {tuple(scales.shape)}")
     return QuantPoolC(codes.data_ptr(), scales.data_ptr(), P, page, L, hkv, d * per, fmt)
 
@@ -527,7 +532,7 @@ def _attend_call(call, ps, dev, layer, q, lengths, max_length, block_tables, sca
     seqs, pages = _whole(block_tables, "attend: block tables", i32, 2, dev)
     if d != ps.head_dim or seqs != S or _whole(lengths, "attend: lengths", i32, 1, dev)[0] != S:
         _bad(f"attend: {tuple(shape)} queries, {lengths.shape[0]} lengths, {seqs} tables, a pool of head_dim {ps.head_dim}")
-    if lse is not None and _whole(lse, "attend: lse", _torch.float32, 2, dev) != shape[:2]:
+    if lse is not None and _whole(lse, "attend: lse", _torch.float32, 2, dev) != (S, H):
         _bad(f"attend: lse {tuple(lse.shape)}")
     if err is not None and not _whole(err, "attend: err", i32, 1, dev)[0]:
         _bad("attend: an empty err")
@@ -536,7 +541,7 @@ def _attend_call(call, ps, dev, layer, q, lengths, max_length, block_tables, sca
     lists = ()
     if blocks is not None:
         got = _whole(blocks, "attend: blocks", i32, 3, dev)
-        if got[:2] != (S, ps.n_kv_heads):
+        if got != (S, ps.n_kv_heads, got[2]):
             _bad(f"attend: blocks {tuple(got)} of {S} sequences and {ps.n_kv_heads} KV heads")
         lists = (blocks.data_ptr(), got[2])
     if S:
@@ -587,7 +592,7 @@ def bounds_pool_struct(bounds, bound_scales) -> BoundsPoolC:
     torch = _torch or _load_torch()
     dev = bounds.get_device()
     L, P, hkv, two, d = shape = _whole(bounds, "bounds", torch.int8, 5, dev)
-    if two != 2 or _whole(bound_scales, "bounds: scales", torch.float32, 3, dev) != shape[:3]:
+    if two != 2 or _whole(bound_scales, "bounds: scales", torch.float32, 3, dev) != (L, P, hkv):
         _bad(f"bounds: {tuple(shape)}, scales {tuple(bound_scales.shape)}")
     return BoundsPoolC(bounds.data_ptr(), bound_scales.data_ptr(), P, L, hkv, d)
 
@@ -637,8 +642,8 @@ def pallas_select_blocks(bounds, bound_scales, layer: int, q, lengths, max_lengt
     S, H, d = shape
     seqs, pages = _whole(block_tables, "select: block tables", i32, 2, dev)
     got = _whole(blocks, "select: blocks", i32, 3, dev)
-    if d != bs.head_dim or seqs != S or _whole(lengths, "select: lengths", i32, 1, dev)[0] != S or got[:2] != (
-            S, bs.n_kv_heads):
+    if d != bs.head_dim or seqs != S or _whole(lengths, "select: lengths", i32, 1, dev)[0] != S or got != (
+            S, bs.n_kv_heads, got[2]):
         _bad(f"select: {tuple(shape)} queries, {lengths.shape[0]} lengths, {seqs} tables, blocks {tuple(got)}, bounds of "
              f"{bs.n_kv_heads} heads of {bs.head_dim}")
     if err is not None and not _whole(err, "select: err", i32, 1, dev)[0]:
