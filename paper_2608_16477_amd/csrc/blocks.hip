@@ -348,6 +348,13 @@ __global__ __launch_bounds__(kWide) void select_kernel(SelectParams p) {
     a.read_pages(p, s, wave, kWaves);
     a.read_q(p, s, kh, 0);
   }
+  // (Scores of the first pass are read beside the length; those behind the row count as none.)
+  const uint32_t* in = p.order + (static_cast<int64_t>(s) * p.Hkv + kh) * p.stride;
+  uint32_t x[kEach];
+  if constexpr (!kScored) {
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) x[k] = in[min(k * kWide + t, static_cast<int>(p.stride) - 1)];
+  }
   const int full = p.lengths[s], blocks = row_blocks(p, s);
   if (p.err && kh == 0 && t == 0 && full != min(max(full, 0), p.max_length)) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_LENGTH));
   int32_t* out = p.blocks + (static_cast<int64_t>(s) * p.Hkv + kh) * p.budget;
@@ -355,7 +362,6 @@ __global__ __launch_bounds__(kWide) void select_kernel(SelectParams p) {
     for (int i = t; i < p.budget; i += kWide) out[i] = i < blocks ? i : -1;
     return;
   }
-  const uint32_t* in = p.order + (static_cast<int64_t>(s) * p.Hkv + kh) * p.stride;
   if constexpr (kScored) {
     const int runs = ((blocks + kRun - 1) / kRun - wave + kWaves - 1) / kWaves;
     if (runs > 0) score_runs<D>(p, a, s, kh, blocks, wave, kWaves, runs, [&](int b, uint32_t x, int pass) { scored[b] = pass == 0 ? x : max(x, scored[b]); });
@@ -364,7 +370,6 @@ __global__ __launch_bounds__(kWide) void select_kernel(SelectParams p) {
   }
   // Score k of the thread in a pass is of block k kWide + t of it; those behind the row are 0.
   const int passes = (blocks + kPass - 1) / kPass;
-  uint32_t x[kEach];
   auto load = [&](int pass) {
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
@@ -372,7 +377,9 @@ __global__ __launch_bounds__(kWide) void select_kernel(SelectParams p) {
       x[k] = i < blocks ? in[i] : 0;
     }
   };
-  load(0);
+  if constexpr (kScored) load(0);
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) x[k] = k * kWide + t < blocks ? x[k] : 0;
   uint32_t low = kAlways, high = 0;
   for (int pass = 0; pass < passes; ++pass) {
     if (pass > 0) load(pass);

@@ -489,3 +489,44 @@ def test_strided_queries_and_other_streams(P):
     o2, l2 = cache.attend(P, q, blocks, 0.1, stream=side)
     side.synchronize()
     assert torch.equal(out, o2) and torch.equal(lse, l2)
+
+
+@pytest.mark.parametrize("room", [900, 9000])
+def test_two_graphs_share_the_workspaces(P, room):
+    """Selection and attention of two batches, replayed in turn with eager calls between them and over changing lengths."""
+    hq, hkv, d, budget = 8, 4, 64, 12
+    ws = torch.empty(P.pallas_attend_workspace_size(3, hq, hkv, d, 16 * budget), dtype=torch.uint8, device=DEV)
+    ws2 = torch.empty(P.pallas_select_workspace_size(3, hkv, room), dtype=torch.uint8, device=DEV)
+
+    class Batch:
+        def __init__(self, seed):
+            self.c = Cache("int8", hkv, d, [room, room // 2, room // 3], seed=seed)
+            self.c.update(P, [0] * 3)
+            self.q = queries(3, hq, d, seed)
+            self.lengths = self.c.lengths.clone()
+
+        def __call__(self):
+            blocks = torch.full((3, hkv, budget), -9, dtype=torch.int32, device=DEV)
+            out, lse = torch.zeros_like(self.q), torch.zeros((3, hq), device=DEV)
+            P.pallas_select_blocks(self.c.bounds, self.c.bound_scales, 1, self.q, self.lengths, room, self.c.bt, blocks, ws2)
+            P.pallas_attend_blocks_quant(*self.c.rows, 1, self.q, self.lengths, room, self.c.bt, blocks, 0.1, out, ws, lse=lse)
+            return blocks, out, lse
+
+    batches, graphs, results = [Batch(5), Batch(6)], [], []
+    for b in batches:
+        b()
+        side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(graph, stream=side):
+            results.append(b())
+        torch.cuda.current_stream().wait_stream(side)
+        graphs.append(graph)
+    for cut in (1.0, 0.2, 0.0, 0.6, 1.0):
+        for b in batches:
+            b.lengths.copy_((b.c.lengths.double() * cut).to(torch.int32))
+        for graph in graphs:
+            graph.replay()
+        batches[0]()
+        for b, kept in zip(batches, results):
+            for x, y in zip(b(), kept):
+                assert torch.equal(x, y), cut
