@@ -158,20 +158,21 @@ __device__ __forceinline__ void read_pv8(uint32_t vb, int dt0, u32x2* a) {
 // apart, at LDS byte address `vb` (read_pv4; the second tile XOR 32 bytes, the second page 1024
 // bytes further).
 __device__ __forceinline__ void read_turned4(uint32_t vb, u32x4* a) {
+  constexpr int kPageBytes = kPage * 32 * 2;
   const uint32_t x1 = vb ^ 32u;
   u32x2 l0, l1, l2, l3, h0, h1, h2, h3;
   asm volatile(
       "ds_read_b64_tr_b16 %0, %8\n\t"
-      "ds_read_b64_tr_b16 %1, %8 offset:1024\n\t"
+      "ds_read_b64_tr_b16 %1, %8 offset:%10\n\t"
       "ds_read_b64_tr_b16 %2, %9\n\t"
-      "ds_read_b64_tr_b16 %3, %9 offset:1024\n\t"
-      "ds_read_b64_tr_b16 %4, %8 offset:2048\n\t"
-      "ds_read_b64_tr_b16 %5, %8 offset:3072\n\t"
-      "ds_read_b64_tr_b16 %6, %9 offset:2048\n\t"
-      "ds_read_b64_tr_b16 %7, %9 offset:3072\n\t"
+      "ds_read_b64_tr_b16 %3, %9 offset:%10\n\t"
+      "ds_read_b64_tr_b16 %4, %8 offset:%11\n\t"
+      "ds_read_b64_tr_b16 %5, %8 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %6, %9 offset:%11\n\t"
+      "ds_read_b64_tr_b16 %7, %9 offset:%12\n\t"
       "s_waitcnt lgkmcnt(0)"
       : "=&v"(l0), "=&v"(h0), "=&v"(l1), "=&v"(h1), "=&v"(l2), "=&v"(h2), "=&v"(l3), "=&v"(h3)
-      : "v"(vb), "v"(x1)
+      : "v"(vb), "v"(x1), "n"(kPageBytes), "n"(2 * kPageBytes), "n"(3 * kPageBytes)
       : "memory");
   a[0] = u32x4{l0.x, l0.y, h0.x, h0.y};
   a[1] = u32x4{l1.x, l1.y, h1.x, h1.y};
