@@ -442,7 +442,7 @@ __global__ __launch_bounds__(kWide) void select_kernel(SelectParams p) {
     for (int e = 0; e < kMine; ++e) bins[kBins - 1 - kMine * t - e] = 0;
     __syncthreads();
     low += found[0] << shift;
-    high = min(high, low + ((1u << shift) - 1));
+    high = low + min(high - low, (1u << shift) - 1);      // (the topmost step can end behind 2^32)
     want = found[1];
     all = found[2] == want;
   }

@@ -1,0 +1,80 @@
+"""Selection from bounds that are written here, block by block, against the oracle: lists are equal to the last entry."""
+import numpy as np
+import pytest
+import torch
+
+from helpers import ensure_lib, to_np64
+from oracle import cache_ops as co
+from test_blocks_gpu import DEV, equal_lists, queries
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def P():
+    return ensure_lib()
+
+
+class Bounds:
+    """Layer 1 of two: bounds of `lens` keys per sequence, on shuffled pages.  `coarse`: few values, so that many scores are
+    equal."""
+
+    def __init__(self, hkv, d, lens, seed, coarse=False):
+        rng = np.random.default_rng(seed)
+        blocks = [-(-n // 16) for n in lens]
+        self.hkv, self.d, self.lens = hkv, d, list(lens)
+        order = rng.permutation(sum(blocks) + 3).astype(np.int32)
+        self.table = np.full((len(lens), max(1, *blocks)), -1, dtype=np.int32)
+        self.codes, self.steps = [], []
+        for i, n in enumerate(blocks):
+            self.table[i, :n] = order[sum(blocks[:i]):sum(blocks[:i + 1])]
+            if coarse:
+                codes = np.zeros((n, hkv, 2, d), dtype=np.int64)
+                codes[..., :2] = rng.integers(-1, 2, (n, hkv, 2, 2))
+                step = np.ones((n, hkv), dtype=np.float32)
+            else:
+                codes = np.sort(rng.integers(-127, 128, (n, hkv, 2, d)), axis=2)[:, :, ::-1]
+                step = np.exp(rng.normal(0, 1, (n, hkv))).astype(np.float32)
+            self.codes.append(codes)
+            self.steps.append(step)
+        self.pages = len(order)
+
+    def select(self, P, q, budget, first, last, max_length=None):
+        codes = np.full((2, self.pages, self.hkv, 2, self.d), -128, dtype=np.int8)
+        steps = np.full((2, self.pages, self.hkv), np.nan, dtype=np.float32)
+        for i, (c, s) in enumerate(zip(self.codes, self.steps)):
+            codes[1, self.table[i, :len(s)]], steps[1, self.table[i, :len(s)]] = c, s
+        max_length = max(1, *self.lens) if max_length is None else max_length
+        blocks = torch.full((len(self.lens), self.hkv, budget), 77, dtype=torch.int32, device=DEV)
+        ws = torch.full((P.pallas_select_workspace_size(len(self.lens), self.hkv, max_length),), 0xA5, dtype=torch.uint8, device=DEV)
+        err = torch.zeros(1, dtype=torch.int32, device=DEV)
+        P.pallas_select_blocks(torch.from_numpy(codes).to(DEV), torch.from_numpy(steps).to(DEV), 1, q,
+                               torch.tensor(self.lens, dtype=torch.int32, device=DEV), max_length,
+                               torch.from_numpy(self.table).to(DEV), blocks, ws, first=first, last=last, err=err)
+        assert int(err.item()) == 0
+        return blocks
+
+    def lists(self, q, budget, first, last):
+        qn = to_np64(q)
+        return [co.select_blocks(co.block_scores(qn[i], c, s), budget, first, last) if len(s) else [[]] * self.hkv
+                for i, (c, s) in enumerate(zip(self.codes, self.steps))]
+
+
+# blocks of a row: scored where they are selected; in a launch of their own; with the wide workgroup
+@pytest.mark.parametrize("blocks", [62, 128, 129, 700, 2049, 5000])
+@pytest.mark.parametrize("budget,first,last", [(12, 1, 2), (4, 1, 2), (9, 0, 0), (40, 3, 5), (3, 1, 2)])
+def test_nan_above_all(P, blocks, budget, first, last):
+    """Fewer blocks that score NaN than open places, as many, more, and all; the rest by their scores."""
+    places = budget - first - last
+    rng = np.random.default_rng(blocks + budget)
+    lens = [16 * blocks - 5] * 6
+    b = Bounds(2, 64, lens, seed=budget)
+    for i, n in enumerate((0, max(places - 1, 0), places, places + 1, blocks - 1, blocks)):
+        for h in range(2):
+            b.steps[i][rng.permutation(blocks)[:n], h] = np.nan
+    q = queries(6, 6, 64, seed=3)
+    lists = b.lists(q, budget, first, last)
+    # (at the last open place lies a NaN, and something else behind it)
+    scores = co.block_scores(to_np64(q)[3], b.codes[3], b.steps[3])
+    assert np.isnan(scores).sum() == 2 * (places + 1) and (~np.isnan(scores)).any()
+    equal_lists(b.select(P, q, budget, first, last), lists)
