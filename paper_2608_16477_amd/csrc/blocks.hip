@@ -81,7 +81,12 @@ __global__ __launch_bounds__(kThreads) void bounds_kernel(BoundsParams p, int pe
   if (nth >= per_seq) return;
   const int from = p.start[s], len = p.lengths[s];
   if (from < 0 || from >= len) return;              // padding, or nothing due
-  if (p.err && item == 0 && lane == 0 && len - from > p.most) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_LENGTH));
+  if (p.err && item == 0 && lane == 0) {
+    // (No wave has a block that lies behind `per_seq`, a table's width at most.)
+    const int last = min((len - 1) / kPage, from / kPage + bounds_blocks(p.most) - 1);
+    if (len - from > p.most) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_LENGTH));
+    if (last >= p.max_pages) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
+  }
   const int64_t j = from / kPage + nth;
   if (j * kPage >= len) return;
   const int pg = j < p.max_pages ? p.bt[static_cast<int64_t>(s) * p.max_pages + j] : -1;
