@@ -576,8 +576,10 @@ typedef struct {
  * positions of a sequence; where there are more the call raises
  * PALLAS_DEVERR_LENGTH, and of those blocks only the first floor((max_new + 30) / 16) are written.
  * Blocks beyond the table or on pages outside [0, num_pages) are skipped and raise
- * PALLAS_DEVERR_PAGE, in *d_err (nullable).  Bounds of a page that two sequences of a call hold to
- * different lengths are of either.  num_seqs up to 65535, page_size 16, and as many blocks of max_new,
+ * PALLAS_DEVERR_PAGE, in *d_err (nullable).  Sequences of a call may share pages that hold the same number of keys
+ * of each (all 16 of a common prefix).  Of a page that one sequence ends in and another goes further, both due,
+ * the bounds are undefined: such sequences go into calls one after the other, of which the last one's
+ * bounds stay.  num_seqs up to 65535, page_size 16, and as many blocks of max_new,
  * times n_kv_heads, as are below 2^26 (UNSUPPORTED otherwise). */
 int pallas_bounds_kv(const pallas_kv_pool* pool, const pallas_bounds_pool* bounds, int32_t layer,
                      int32_t num_seqs, const int32_t* d_start, const int32_t* d_lengths,

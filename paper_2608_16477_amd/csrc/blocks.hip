@@ -68,7 +68,9 @@ __device__ __forceinline__ uint32_t ordered_bf2(uint32_t w) {
   return w ^ (__builtin_bit_cast(uint32_t, sign) & 0x7FFF7FFFu);
 }
 
-// A wave per block and KV head: D / 8 lanes take a row, eight values each.  Rows of bf16 and
+// A wave per block and KV head, of each sequence: where two hold a page their waves write the same, or
+// the caller keeps them apart (codes and step are two stores, which nothing orders between workgroups).
+// D / 8 lanes take a row, eight values each.  Rows of bf16 and
 // E2M1 are (these, with their scales, exactly, but for magnitudes too small to be of a block that
 // is not zero) bf16 values, which order as integers: two to an instruction, and infinities and
 // NaN show at the end.  8-bit rows are products in float32.

@@ -5,7 +5,7 @@ import torch
 
 from helpers import ensure_lib
 from oracle import cache_ops as co
-from test_blocks_gpu import DEV, Cache
+from test_blocks_gpu import DEV, FORMATS, Cache
 
 pytestmark = pytest.mark.gpu
 PAGE, LENGTH = 1, 4
@@ -52,3 +52,23 @@ def test_one_of_many_reaches_beyond(P):
         err.zero_()
         cache.update(P, [0] * 5, lengths=lens, max_new=512, err=err)
         assert int(err.item()) == flags
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_shared_pages(P, fmt):
+    """Sequences of one call share full pages, and a page that they end in at the same length; at different lengths,
+    in calls of their own, the last one's bounds stay."""
+    cache = Cache(fmt, 2, 64, [500], seed=3)
+
+    def call(lens, start):
+        cache.bounds.fill_(-128)
+        for l, s in zip(lens, start):
+            cache.update(P, s, lengths=torch.tensor(l, dtype=torch.int32, device=DEV), max_new=500,
+                         bt=cache.bt.expand(len(l), -1).contiguous())
+        return cache.bounds.cpu().numpy()[1, cache.table[0]], cache.bound_scales.cpu().numpy()[1, cache.table[0]]
+
+    for last, lens, start in ((500, [[500, 500, 160, 496, 500] * 40], [[0, 480, 0, 100, 499] * 40]),
+                              (500, [[490], [500]], [[0], [490]]), (490, [[500], [490]], [[0], [0]])):
+        c, s = co.block_bounds(cache.kv[0][0][:last])
+        codes, steps = call(lens, start)
+        assert np.array_equal(codes[:len(s)], c) and np.array_equal(steps[:len(s)], s)      # (490 keys: one block fewer)
