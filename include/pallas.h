@@ -541,8 +541,9 @@ int pallas_attend_quant(const pallas_quant_pool* pool, int32_t layer, int32_t nu
                         int64_t out_stride, float* d_lse, void* d_workspace, size_t ws_bytes,
                         int32_t* d_err, void* stream);
 
-/* Bytes of workspace of a pallas_attend_* call; enough for fewer sequences and a
- * shorter max_length too.  0 where the call would be refused. */
+/* Bytes of workspace that are enough for a pallas_attend_* call over any cache, and for fewer
+ * sequences and a shorter max_length too.  (A call is refused where it has less than it uses
+ * itself, which over bf16 and 8-bit rows can be less than this.)  0 where the call would be refused. */
 size_t pallas_attend_workspace_size(int32_t num_seqs, int32_t n_q_heads, int32_t n_kv_heads,
                                     int32_t head_dim, int32_t max_length);
 

@@ -177,7 +177,7 @@ int append_call(const char* what, const pallas_rope_plan* plan, pallas::AppendPa
 }
 
 // A call's workspace: two ints per sequence, then records of d + 2 floats per query head.
-// `ranges`: of the call, or the most of any cache type.
+// `ranges`: of the call, or, where its cache is not known, the most of any.
 struct AttendSpace {
   int records;
   size_t o_at, ml_at, bytes;
@@ -252,7 +252,8 @@ int attend_call(const char* what, pallas::CacheType type, pallas::AttendParams& 
   p.lists = lists.d_blocks;
   p.listed = lists.max_blocks;
   p.max_row = lists.listed ? std::min((max_length - 1) / page_size + 1, lists.max_blocks) * page_size : max_length;
-  const AttendSpace sp = attend_space(num_seqs, n_q_heads, p.d, p.max_row, most_ranges(n_q_heads, p.Hkv, p.d));
+  p.ranges = attend_ranges(type, n_q_heads, p.Hkv, p.d, lists.listed);
+  const AttendSpace sp = attend_space(num_seqs, n_q_heads, p.d, p.max_row, p.ranges);
   if (ws_bytes < sp.bytes)
     return fail(PALLAS_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", what, ws_bytes, sp.bytes);
   p.Hq = n_q_heads;
@@ -267,7 +268,6 @@ int attend_call(const char* what, pallas::CacheType type, pallas::AttendParams& 
   p.out = static_cast<uint16_t*>(d_out);
   p.out_stride = out_stride;
   p.lse = d_lse;
-  p.ranges = attend_ranges(type, n_q_heads, p.Hkv, p.d, lists.listed);
   p.records = sp.records;
   char* ws = static_cast<char*>(d_workspace);
   p.parts = reinterpret_cast<int32_t*>(ws);
