@@ -78,3 +78,50 @@ def test_nan_above_all(P, blocks, budget, first, last):
     scores = co.block_scores(to_np64(q)[3], b.codes[3], b.steps[3])
     assert np.isnan(scores).sum() == 2 * (places + 1) and (~np.isnan(scores)).any()
     equal_lists(b.select(P, q, budget, first, last), lists)
+
+
+# A workgroup takes 8192 blocks at a time, 131,072 keys.
+@pytest.mark.parametrize("lens,hkv,d,group,budget,first,last", [
+    ([131073], 1, 64, 2, 50, 1, 2),                       # one block in the second pass, always listed
+    ([131073 + 16 * 60, 3000, 0], 2, 64, 3, 200, 0, 0),   # a short row and an empty one beside it
+    ([140001, 131072, 40], 1, 128, 1, 33, 4, 8),
+    ([300007, 290000], 1, 64, 4, 700, 2, 3),              # three passes
+    ([140001], 2, 64, 2, 9, 4, 5),                        # nothing but the first and the last ones
+    ([300007], 1, 64, 1, 9000, 1, 2),                     # a list longer than a pass
+    ([300007], 1, 64, 1, 18000, 8500, 9000),              # first and last ones reach into other passes
+])
+@pytest.mark.parametrize("coarse", [False, True])
+def test_more_blocks_than_a_pass_takes(P, lens, hkv, d, group, budget, first, last, coarse):
+    """coarse: hundreds of scores equal the last that is listed, on both sides of the passes' border."""
+    b = Bounds(hkv, d, lens, seed=budget, coarse=coarse)
+    q = queries(len(lens), hkv * group, d, seed=6)
+    if coarse:
+        q = q.clamp(-1, 1).round()
+        scores = co.block_scores(to_np64(q)[0], b.codes[0], b.steps[0])
+        assert len(np.unique(scores)) < 60 * hkv
+    lists = b.lists(q, budget, first, last)
+    blocks = b.select(P, q, budget, first, last)
+    equal_lists(blocks, lists)
+    # room for longer rows
+    b.table = np.pad(b.table, ((0, 0), (0, 9000)), constant_values=-1)
+    assert torch.equal(b.select(P, q, budget, first, last, max_length=16 * b.table.shape[1]), blocks)
+
+
+def test_equal_scores_around_a_border_of_passes(P):
+    """All scores equal but some of the second pass: the earliest, up to the border, on it and behind it."""
+    b = Bounds(1, 64, [16 * 20000], seed=7, coarse=True)
+    b.codes[0][...] = 0
+    b.codes[0][9000:9010, 0, :, 0] = 1
+    q = queries(1, 1, 64, seed=8).abs()
+    for budget in (8191, 8192, 8193, 8203, 8204, 16384, 16394, 16395, 19999):
+        lists = b.lists(q, budget, 0, 1)
+        assert lists[0][0][-1] == 19999 and set(range(9000, 9010)) <= set(lists[0][0])
+        equal_lists(b.select(P, q, budget, 0, 1), lists)
+
+
+@pytest.mark.parametrize("nan", [46, 47, 48, 20000])
+def test_nan_in_every_pass(P, nan):
+    b = Bounds(1, 64, [16 * 20000 - 3], seed=9)
+    b.steps[0][np.random.default_rng(nan).permutation(20000)[:nan]] = np.nan
+    q = queries(1, 2, 64, seed=10)
+    equal_lists(b.select(P, q, 50, 1, 2), b.lists(q, 50, 1, 2))
