@@ -34,7 +34,7 @@ constexpr int64_t kNtStoreBytes = int64_t(4) << 20;
 // and 2^-49 (cosine, x^16 / 16!).
 __device__ __forceinline__ void turn_cos_sin64(uint64_t a, double m, double& c, double& s) {
   const uint64_t quarter = (a + (uint64_t(1) << 61)) >> 62;
-  const double x = static_cast<double>(static_cast<int64_t>(a - (quarter << 62))) * 3.4061215800304874e-19;   // 2 pi 2^-64
+  const double x = static_cast<double>(static_cast<int64_t>(a - (quarter << 62))) * 0x1.921fb54442d18p-62;   // 2 pi 2^-64
   const double z = x * x;
   double sp = __builtin_fma(z, -7.6471637318198165e-13, 1.6059043836821613e-10);   // 1 / 15!, 1 / 13!, ..
   sp = __builtin_fma(z, sp, -2.5052108385441720e-08);
