@@ -483,8 +483,9 @@ int pallas_quant_load(const pallas_quant_pool* pool, int32_t layer, int32_t num_
  * (d_q_out may be d_q with the same stride; otherwise neither overlaps what the call reads
  * or writes).  Without queries n_q_heads is 0 and both are null.
  *   The rotation is worked out in 64 bits and rounded to float32 and then to bf16, before a
- * code is made of it: within 2^-8 of the exact value, where pallas_rope_apply adds up to
- * 2^-22 of the pair's magnitudes.
+ * code is made of it: within 2^-8 + 2^-24 of the exact value (half a step of both; m is the plan's
+ * float32) and position * 2^-61 + 2^-48 of the pair's magnitudes, where pallas_rope_apply adds up to
+ * 2^-22 of them.
  *   Of a token of negative position (padding) nothing is written, of one that is skipped as
  * in pallas_quant_store, with PALLAS_DEVERR_PAGE, the queries alone.  rotary_dim of the plan is at
  * most head_dim (INVALID_ARG); head_dim 64 or 128, page_size 16, num_tokens below 2^24,

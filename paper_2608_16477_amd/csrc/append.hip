@@ -7,7 +7,9 @@
 // What is stored in 8 or 4 bits is decided at borders between codes: a K value rounded to bf16
 // one way or the other, which float32 sums of two products do in one of some thousand values,
 // can be a whole code away.  So the rotation is in 64 bits (v_fma_f64 has float32's rate here)
-// and rounded to float32 and then to bf16: codes do not depend on how it was computed.
+// and rounded to float32 and then to bf16: codes do not depend on how it was computed, but
+// for values within position 2^-61 + 2^-48 (the plan's turns; the polynomials), times the
+// pair's magnitudes, of a border.
 //
 // Long calls are bound by memory: 3000 tokens of 64 / 8 heads of 128 to a bf16 cache (123 MB) 22.5 us, 5.5
 // TB/s; 12,000 of them 93.  1999 tokens of 20 / 4 heads to INT8 (27 MB) 9.4, with the launch and a

@@ -60,7 +60,7 @@ def cancelling(high, count, seed):
 
 
 @pytest.mark.parametrize("layout", ["half", "interleaved"])
-@pytest.mark.parametrize("high", [1 << 24, 1 << 17])
+@pytest.mark.parametrize("high", [1 << 31, 1 << 24, 1 << 17])
 def test_where_a_pair_cancels(P, layout, high):
     d, n = 64, 512
     pos, x0, x1, exact = cancelling(high, n, seed=1)
@@ -78,3 +78,5 @@ def test_where_a_pair_cancels(P, layout, high):
     off = np.abs(to_np64(out)[:, 0, first] - exact)
     pair = np.abs(x0) + np.abs(x1)
     assert np.all(off <= (2.0 ** -8 + 2.0 ** -24) * np.abs(exact) + (pos * 2.0 ** -61 + 2.0 ** -48) * pair + 2.0 ** -40)
+    # the nearest pairs are such that a term in the pair's magnitudes is needed at far positions
+    assert high < 1 << 31 or np.any(off > 2.0 ** -7 * np.abs(exact))
