@@ -427,8 +427,11 @@ def pallas_rope_apply(plan: RopePlan, x, positions, out=None, inverse: bool = Fa
 def _quant_formats():
     torch = _torch or _load_torch()
     # dtype of the codes -> format, codes to a value of the tensor, the scales' dtype and rank
-    return {torch.float8_e4m3fn: (1, 1, torch.float32, 5), torch.int8: (2, 1, torch.float32, 5),
-            torch.float4_e2m1fn_x2: (4, 2, torch.float8_e8m0fnu, 6)}
+    formats = {torch.float8_e4m3fn: (1, 1, torch.float32, 5), torch.int8: (2, 1, torch.float32, 5)}
+    packed, units = getattr(torch, "float4_e2m1fn_x2", None), getattr(torch, "float8_e8m0fnu", None)
+    if packed is not None and units is not None:      # (a torch without them has the 8-bit pools)
+        formats[packed] = 4, 2, units, 6
+    return formats
 
 
 def quant_pool_struct(codes, scales) -> QuantPoolC:

@@ -56,3 +56,14 @@ def test_binding_refusals(P):
         with pytest.raises(P.PallasError) as e:
             P.pallas_quant_store(c, s, 0, x, x, pos, bt)
         assert e.value.status == P.Status.INVALID_ARG
+
+
+@pytest.mark.parametrize("gone", [("float4_e2m1fn_x2",), ("float8_e8m0fnu",), ("float4_e2m1fn_x2", "float8_e8m0fnu")])
+def test_a_torch_without_the_4_bit_types_has_the_8_bit_pools(P, monkeypatch, gone):
+    import types
+    from paper_2608_16477_amd import binding
+    names = ("float8_e4m3fn", "int8", "float32", "float4_e2m1fn_x2", "float8_e8m0fnu")
+    monkeypatch.setattr(binding, "_torch", types.SimpleNamespace(**{n: getattr(torch, n) for n in names if n not in gone}))
+    assert binding._quant_formats() == {torch.float8_e4m3fn: (1, 1, torch.float32, 5), torch.int8: (2, 1, torch.float32, 5)}
+    monkeypatch.undo()
+    assert binding._quant_formats()[torch.float4_e2m1fn_x2] == (4, 2, torch.float8_e8m0fnu, 6)
