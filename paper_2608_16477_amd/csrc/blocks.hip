@@ -202,23 +202,23 @@ __device__ __forceinline__ uint32_t order_of(float x) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// A wave takes runs of 16 blocks of one KV head and up to 16 of its query heads (others in
-// further passes): Q as the MFMA's rows, blocks as its columns, so that lane l holds heads 4 (l /
+// A wave takes up to kRuns runs of 16 blocks of one KV head and up to 16 of its query heads (others
+// in further passes): Q as the MFMA's rows, blocks as its columns, so that lane l holds heads 4 (l /
 // 16) + r against block l mod 16.  `runs` runs of a row of `blocks`: first, first + step, ..;
-// put(block, score, pass) keeps a score, or the larger of two passes'.  Pages are read kAhead
-// runs at a time, bounds a run ahead, and the first of both before the query is worked on.
+// put(block, score, pass) keeps a score, or the larger of two passes'.  Pages of all runs are read
+// together, bounds a run ahead, and the first of both before the query is worked on.
 constexpr int kRun = 16;
 constexpr int kHeads = 16;
-constexpr int kAhead = 4;
+constexpr int kRuns = 4;
 template <int D>
 struct Ahead {
-  int pages[kAhead];
+  int pages[kRuns];
   u32x4 w[D / 64][2];      // 16 elements of each 64 of head l16 (the last again where there are fewer)
 
   // (Entries behind the row's: no use, but within the table.)
   __device__ __forceinline__ void read_pages(const SelectParams& p, int s, int first, int step) {
 #pragma unroll
-    for (int n = 0; n < kAhead; ++n)
+    for (int n = 0; n < kRuns; ++n)
       pages[n] = p.bt[static_cast<int64_t>(s) * p.max_pages + min((first + n * step) * kRun + static_cast<int>(threadIdx.x & 15), p.max_pages - 1)];
   }
   __device__ __forceinline__ void read_q(const SelectParams& p, int s, int kh, int g0) {
@@ -276,34 +276,27 @@ __device__ __forceinline__ void score_runs(const SelectParams& p, Ahead<D>& a, i
     float unit[4];      // steps of heads 4 q4 + r
 #pragma unroll
     for (int r = 0; r < 4; ++r) unit[r] = __shfl(st.step, 4 * q4 + r, 64);
-    for (int from = 0; from < runs; from += kAhead) {
-      int now[kAhead];
 #pragma unroll
-      for (int n = 0; n < kAhead; ++n) now[n] = a.pages[n];
-      if (from + kAhead < runs) a.read_pages(p, s, first + (from + kAhead) * step, step);
+    for (int n = 0; n < kRuns; ++n) {
+      if (n >= runs) break;
+      if (n + 1 < kRuns) read(a.pages[n + 1], (n + 1) % 2);
+      i32x4 dot = {0, 0, 0, 0};
 #pragma unroll
-      for (int n = 0; n < kAhead; ++n) {
-        if (from + n >= runs) break;
-        if (n + 1 < kAhead) read(now[n + 1], (n + 1) % 2);
-        else if (from + kAhead < runs) read(a.pages[0], 0);
-        i32x4 dot = {0, 0, 0, 0};
+      for (int c = 0; c < D / 64; ++c) {
+        dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(up[c], top[n % 2][c], dot, 0, 0, 0);
+        dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(down[c], low[n % 2][c], dot, 0, 0, 0);
+      }
+      uint32_t best = 0;
 #pragma unroll
-        for (int c = 0; c < D / 64; ++c) {
-          dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(up[c], top[n % 2][c], dot, 0, 0, 0);
-          dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(down[c], low[n % 2][c], dot, 0, 0, 0);
-        }
-        uint32_t best = 0;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) best = max(best, order_of(static_cast<float>(dot[r]) * scale[n % 2] * unit[r]));
-        best = over_rows<16>(best, [](uint32_t u, uint32_t v) { return max(u, v); });
-        const bool bad = !inside(now[n]);
-        if (bad) best = 0;      // (the keys of such a block are masked)
-        const int b = (first + (from + n) * step) * kRun + l16;
-        if (b < p.first || b >= blocks - p.last) best = kAlways;
-        if (q4 == 0 && b < blocks) {
-          put(b, best, g0);
-          if (p.err && bad && kh == 0 && g0 == 0) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
-        }
+      for (int r = 0; r < 4; ++r) best = max(best, order_of(static_cast<float>(dot[r]) * scale[n % 2] * unit[r]));
+      best = over_rows<16>(best, [](uint32_t u, uint32_t v) { return max(u, v); });
+      const bool bad = !inside(a.pages[n]);
+      if (bad) best = 0;      // (the keys of such a block are masked)
+      const int b = (first + n * step) * kRun + l16;
+      if (b < p.first || b >= blocks - p.last) best = kAlways;
+      if (q4 == 0 && b < blocks) {
+        put(b, best, g0);
+        if (p.err && bad && kh == 0 && g0 == 0) atomicOr(p.err, static_cast<int32_t>(PALLAS_DEVERR_PAGE));
       }
     }
   }
@@ -341,11 +334,13 @@ __global__ __launch_bounds__(kThreads) void score_kernel(SelectParams p, int per
 //   kScored: the scores of the row are worked out here first, into LDS.
 constexpr int kBins = 2048;
 constexpr int kEach = 8;        // scores that a thread keeps
+constexpr int kShortBlocks = 128;   // of a row that is scored where it is selected: two runs a wave
 template <int D, int kWide, bool kScored>
 __global__ __launch_bounds__(kWide) void select_kernel(SelectParams p) {
   constexpr int kWaves = kWide / 64, kPass = kWide * kEach;
+  static_assert(!kScored || kShortBlocks <= kWaves * kRuns * kRun, "a wave's runs");
   __shared__ uint32_t bins[kBins];
-  __shared__ uint32_t scored[kScored ? kPass : 1];
+  __shared__ uint32_t scored[kScored ? kShortBlocks : 1];
   __shared__ uint32_t lows[kWaves], highs[kWaves], sums[kWaves], found[3];
   __shared__ uint32_t counts[2][kEach * kWaves];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -511,7 +506,6 @@ __global__ __launch_bounds__(kWide) void select_kernel(SelectParams p) {
 // heads, 8.0 (10.7), 64 of them 10.8 (12.9), 128 of 1000 12.8 (13.7)); a workgroup that scores longer ones
 // is longer than the chip's way to the second launch (1 row of 4000 12.0 (10.8), 64 of 2000 to 16,000 31
 // (28.5)).
-constexpr int kShortBlocks = 128;
 template <int D>
 hipError_t launch_selection(const SelectParams& p, hipStream_t s) {
   const int most = (p.max_length + kPage - 1) / kPage;
@@ -525,7 +519,7 @@ hipError_t launch_selection(const SelectParams& p, hipStream_t s) {
     // 2 and 4: 1 row of 8000 keys 9.7, 10.0, 11.0; 8 of 1000 to 8000 11.0, 10.3, 11.3; 1 of 131,071 18.1,
     // 16.2, 15.3; 64 of 32,000 99, 80, 67, with 8 and 16 the same).
     const int64_t runs = (int64_t(most) + kRun - 1) / kRun, all = runs * p.Hkv * p.seqs;
-    const int per_wave = all < 2048 ? 1 : all < 4096 ? 2 : 4;
+    const int per_wave = all < 2048 ? 1 : all < 4096 ? 2 : kRuns;
     const int64_t units = (runs + per_wave - 1) / per_wave * p.Hkv;
     score_kernel<D><<<dim3(static_cast<unsigned>((units + 3) / 4), p.seqs), kThreads, 0, s>>>(p, per_wave);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
