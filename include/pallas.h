@@ -605,8 +605,9 @@ int pallas_bounds_quant(const pallas_quant_pool* pool, const pallas_bounds_pool*
  * any number).  The sum is of whole numbers and the products are float32, so the lists are
  * the same however the work is divided, and in any other program that follows this.
  *   Query rows, lengths, max_length, tables and their limits and errors are pallas_attend_*'s
- * (and max_length up to 2^30, below 2^34 times n_kv_heads, UNSUPPORTED beyond); a
- * block on a page outside [0, num_pages) scores lowest.  The workspace (device, 256-byte aligned,
+ * (and max_length up to 2^30; max_length times n_kv_heads below 2^34; UNSUPPORTED beyond); a
+ * block on a page outside [0, num_pages) scores lowest.  The table of a row of no more than max_blocks
+ * blocks is not looked at: attention flags its pages.  The workspace (device, 256-byte aligned,
  * pallas_select_workspace_size bytes) holds nothing between calls; calls that may run at once need
  * one each. */
 int pallas_select_blocks(const pallas_bounds_pool* bounds, int32_t layer, int32_t num_seqs,

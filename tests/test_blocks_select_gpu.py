@@ -125,3 +125,30 @@ def test_nan_in_every_pass(P, nan):
     b.steps[0][np.random.default_rng(nan).permutation(20000)[:nan]] = np.nan
     q = queries(1, 2, 64, seed=10)
     equal_lists(b.select(P, q, 50, 1, 2), b.lists(q, 50, 1, 2))
+
+
+@pytest.mark.parametrize("room", [16 * 9, 16 * 200])
+def test_rows_that_are_listed_whole_ask_no_table(P, room):
+    """Rows of as many blocks as are listed, or fewer, beside a longer one: pages outside the pool are flagged in that one alone."""
+    b = Bounds(2, 64, [16 * 9, 16 * 8, 5], seed=11)
+    q = queries(3, 4, 64, seed=12)
+    b.table = np.pad(b.table, ((0, 0), (0, room // 16 - 9)), constant_values=-1)
+    lists = b.lists(q, 8, 1, 1)
+    b.table[1:], keep = 1 << 20, b.table[1:].copy()
+    codes = torch.zeros((1, b.pages, 2, 2, 64), dtype=torch.int8, device=DEV)
+    steps = torch.zeros((1, b.pages, 2), device=DEV)
+    for i, (c, s) in enumerate(zip(b.codes, b.steps)):
+        at = torch.from_numpy(b.table[0, :9] if i == 0 else keep[i - 1][:len(s)]).long()
+        codes[0, at], steps[0, at] = torch.from_numpy(c.astype(np.int8)).to(DEV), torch.from_numpy(s).to(DEV)
+    ws = torch.empty(P.pallas_select_workspace_size(3, 2, room), dtype=torch.uint8, device=DEV)
+    for bad in (None, 4):
+        table = b.table.copy()
+        if bad is not None:
+            table[0, bad] = -1
+        err, blocks = torch.zeros(1, dtype=torch.int32, device=DEV), torch.full((3, 2, 8), 77, dtype=torch.int32, device=DEV)
+        P.pallas_select_blocks(codes, steps, 0, q, torch.tensor(b.lens, dtype=torch.int32, device=DEV), room,
+                               torch.from_numpy(table).to(DEV), blocks, ws, first=1, last=1, err=err)
+        assert int(err.item()) == (0 if bad is None else 1)
+        if bad is not None:
+            lists[0] = [[j for j in range(9) if j != bad]] * 2
+        equal_lists(blocks, lists)
