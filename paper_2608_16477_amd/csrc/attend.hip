@@ -972,8 +972,8 @@ constexpr int kSplitBlocks = 2;
 // Rows of listed blocks are equally long, and a workgroup each up to twice that, but where
 // there are so few that they are cut (64 rows of 1024 keys bf16 16.1, 12.2 as splits), and bf16 ones
 // only where they do not fill the chip twice (1024 rows of 768 keys 70.3 (66.0), 512 of 1024 50.8
-// (50.3), 256 25.3 (29.7)).  512 rows of 1024 keys E4M3 33.0 (35.4), E2M1 30.5 (40.0), 96 of them 14.5 (13.5),
-// 12.9 (12.9); 1440 of 640 keys 53.8 (61.2), 50.0 (59.8).
+// (50.3), 256 25.3 (29.7)).  512 rows of 1024 keys E4M3 33.0 (35.4), E2M1 30.5 (40.0), 96 of them 14.5 (13.5;
+// E4M3 loses there), 12.9 (12.9); 1440 of 640 keys 53.8 (61.2), 50.0 (59.8).
 constexpr int kListedKeys = 1024;
 constexpr int kListedFew = 64;
 constexpr int kListedBf16 = 512;
