@@ -518,7 +518,7 @@ int pallas_append_quant(const pallas_rope_plan* plan, const pallas_quant_pool* p
  *   head_dim 64 or 128 (UNSUPPORTED otherwise), page_size 16, any number of
  * query heads per KV head, num_seqs 1 to 65535, max_length (the longest length
  * the call can meet) at least 1 and at most max_pages * page_size; num_seqs *
- * max_length up to 2^35 (UNSUPPORTED beyond).  A length
+ * max_length, this rounded up to 32, up to 2^35 (UNSUPPORTED beyond).  A length
  * outside [0, max_length] is cut to it and raises PALLAS_DEVERR_LENGTH; keys on
  * pages outside [0, num_pages) are masked and raise PALLAS_DEVERR_PAGE, in *d_err
  * (nullable).  What is in slots behind a length has no effect.

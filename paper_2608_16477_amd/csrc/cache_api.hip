@@ -364,7 +364,7 @@ int check_select(int32_t num_seqs, int32_t n_kv_heads, int32_t max_length, const
   if (num_seqs < 1 || max_length < 1)
     return fail(PALLAS_ERR_INVALID_ARG, "%s: num_seqs and max_length must be at least 1", what);
   if (num_seqs > 65535 || max_length > kMaxListedLength || int64_t(num_seqs) * max_length > (int64_t(1) << 35) ||
-      (int64_t(max_length) / 256 + 1) * n_kv_heads >= (1 << 26))      // (a launch has fewer than 2^32 threads)
+      int64_t(max_length) * n_kv_heads >= (int64_t(1) << 34))      // (a launch has fewer than 2^32 threads)
     return fail(PALLAS_ERR_UNSUPPORTED, "%s: %d sequences (at most 65535) of up to %d keys (at most 2^30, 2^35 in all, 2^34 times the KV heads)",
                 what, num_seqs, max_length);
   return PALLAS_OK;

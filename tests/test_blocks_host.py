@@ -140,3 +140,11 @@ def test_binding_refusals(P):
         with pytest.raises(P.PallasError) as e:
             call()
         assert e.value.status == P.Status.INVALID_ARG
+
+
+def test_select_takes_all_that_is_below_its_limits(P):
+    size = P.pallas_select_workspace_size
+    for heads, n in ((4096, (1 << 22) - 1), (16, (1 << 30) - 1), (15, 1 << 30), (3000, ((1 << 34) - 1) // 3000)):
+        assert heads * n < 1 << 34 and size(1, heads, n) >= heads * -(-n // 16) * 4, (heads, n)
+        assert size(1, heads, min(n + 1, 1 << 30)) == 0 or heads * min(n + 1, 1 << 30) < 1 << 34
+    assert size(65535, 4, (1 << 35) // 65535) > 0 and size(65535, 4, (1 << 35) // 65535 + 1) == 0
